@@ -604,6 +604,119 @@ int hgca_append_weights_tiers(const hgca_shape *shape, const void *q, int32_t n_
                               const float *lse_pool, float *a_gpu, float *a_cpu,
                               void *hip_stream);
 
+/* ---- What a decoder layer's step needs beside its attention: queries and keys before
+ * they enter the cache, drafted tokens that are verified together, an older pool in
+ * 8 bits.  These calls keep to the conventions above (host-side checks, nothing
+ * allocated, nothing enqueued on error); device arrays are not read by the host. ---- */
+
+/* Queries and keys of a step: each head's row is normed, y = w * x / sqrt(mean x^2 +
+ * eps), and its first rot_dim columns are rotated in pairs by the token's position,
+ * (a, b) -> (a cos t - b sin t, a sin t + b cos t) with t = position *
+ * inv_freq[j] for pair j; the other columns are left as normed.  The angle is formed in
+ * fp64 (far positions keep their digits), all else in fp32, rounded once.
+ * q_in is [B, n_tokens, Hq, d], k_in [B, n_tokens, Hkv, d] in shape.dtype;
+ * q_token_stride / k_token_stride are elements from one token's row to the next (0:
+ * Hq * d and Hkv * d), a multiple of 16 bytes, so that both may be parts of one
+ * projection's rows.  q_weight / k_weight ([d], shape.dtype) may be NULL: no norm.
+ * inv_freq is device fp32 [rot_dim / 2]; rot_dim a multiple of 16, at most d.
+ * positions is device int32 [B, n_tokens], or NULL: first_pos[b] + i (first_pos device
+ * int32 [B], NULL: 0), any value of the type.  flags: HGCA_ROPE_INTERLEAVED pairs columns 2j and 2j + 1,
+ * without it j and j + rot_dim / 2.  q_out [B, n_tokens, Hq, d] and k_out
+ * [B, n_tokens, Hkv, d] may be q_in and k_in themselves where those are dense (stride
+ * 0 or equal to it); any other overlap is refused.  Only pointers, sizes and dtype of
+ * `shape` are used, not sm_scale.  head_dim 64 or 128, any number of heads that
+ * `shape` takes. */
+enum { HGCA_ROPE_INTERLEAVED = 1 };
+int hgca_qk_norm_rope(const hgca_shape *shape,
+                      const void *q_in, int64_t q_token_stride,
+                      const void *k_in, int64_t k_token_stride, int32_t n_tokens,
+                      const void *q_weight, const void *k_weight, float eps,
+                      const float *inv_freq, int32_t rot_dim,
+                      const int32_t *positions, const int32_t *first_pos, int32_t flags,
+                      void *q_out, void *k_out, void *hip_stream);
+
+/* Attention of n_q drafted tokens per sequence over one tier whose last n_q valid tokens
+ * they are: query i sees every earlier token of the tier, and of the drafted ones those
+ * whose bit is set in draft_mask[b, i] (device uint64 [B, n_q]; bit j is the j-th of the
+ * n_q, its own bit i among them if it is to see itself; bits from n_q on are ignored).
+ * NULL: every query sees every valid token.  A tier with fewer than n_q
+ * valid tokens holds the last of the drafted ones.  1 <= n_q <= HGCA_MAX_DRAFTS.
+ * q is [B, n_q, Hq, d]; o_out [B, n_q, Hq, d] in o_dtype, lse_out fp32 [B, n_q, Hq]; a
+ * query that sees nothing gives O = 0, lse = -inf.  A row that a query does not see has
+ * no part in its O, whatever the row holds (with draft_mask; without it all queries see
+ * all valid rows).  fp32 O is accurate to fp32: weights enter the second product
+ * in parts that add up to them.  bf16 O is rounded once.  Results of several
+ * tiers are combined with hgca_lse_merge (fp32 O, a shape whose batch is B * n_q).
+ * sm_scale must be positive and finite.  tier->cap is at most 2^30.  ws needs
+ * hgca_tree_workspace_bytes(shape, n_q, tier->cap), which also serves smaller capacities. */
+#define HGCA_MAX_DRAFTS 64
+size_t hgca_tree_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens);
+int hgca_tree_attn(const hgca_shape *shape, const void *q, int32_t n_q,
+                   const hgca_kv_view *tier, const uint64_t *draft_mask,
+                   void *o_out, int32_t o_dtype, float *lse_out,
+                   void *ws, size_t ws_bytes, void *hip_stream);
+
+/* The accepted ones of n_tokens drafted tokens enter a tier: rows path[b, i], i <
+ * cnt[b], of k_in / v_in ([B, n_tokens, Hkv, d] in shape.dtype, 16-byte aligned) are written to positions
+ * first[b] + i, and lens_out[b] = first[b] + cnt[b].  path is device int32 [B, n_tokens]
+ * or NULL (row i), values outside [0, n_tokens) are read as the nearest inside; cnt
+ * device int32 [B] or NULL (n_tokens); first device int32 [B] or NULL (0).  Drafts
+ * that the tier held from first[b] on are so replaced by the accepted ones; rows behind
+ * them stay as they are.  Tokens beyond the tier's capacity or table row are left out (bit
+ * HGCA_CACHE_CONTEXT_FULL of *status, optional).  tier->k / v are written and tier->seq_lens
+ * is not read; lens_out (device int32 [B]) may be the array behind it, but not `first`. */
+int hgca_kv_commit(const hgca_shape *shape, const hgca_kv_view *tier,
+                   const int32_t *first, const void *k_in, const void *v_in,
+                   int32_t n_tokens, const int32_t *path, const int32_t *cnt,
+                   int32_t *lens_out, int32_t *status, void *hip_stream);
+
+/* A tier in 8 bits: K and V rows as E4M3 values (bytes, laid out as a tier's rows: k, v =
+ * [B, Hkv, cap, d] or [n_blocks, Hkv, block_size, d]) and one scale byte per 32 adjacent
+ * columns (k_scale, v_scale = [..., d / 32], E8M0: 2^(byte - 127)), 1.03 bytes per element.
+ * A block's scale is the least 2^e, e >= -110, with its largest magnitude <= 448 * 2^e;
+ * values are rounded to the nearest (ties to even), an infinity or NaN becomes NaN and
+ * does not count for the scale, what would round to 2^128 is 240 * 2^120.  What the bytes stand for is exact in fp32 and bf16.
+ * k, v 16-byte, k_scale, v_scale 4-byte aligned.  Other fields as in hgca_kv_view: an 8-bit
+ * pool may share lengths and block table with the tier that it is written from. */
+typedef struct {
+    void          *k, *v;             /* E4M3 bytes                                        */
+    void          *k_scale, *v_scale; /* E8M0 bytes                                        */
+    const int32_t *seq_lens;          /* device [B] or NULL; not read by the two writes    */
+    const int32_t *block_table;
+    int32_t cap, block_size, max_blocks;
+    const int32_t *first_block;
+} hgca_kv8_view;
+
+/* Writes n_tokens new tokens' rows, k_in / v_in [B, n_tokens, Hkv, d] in shape.dtype, to
+ * positions first[b] .. (first device int32 [B], NULL: 0).  Tokens beyond the capacity or
+ * the table row are left out (HGCA_CACHE_CONTEXT_FULL in *status, optional). */
+int hgca_kv8_write_tokens(const hgca_shape *shape, const hgca_kv8_view *kv8,
+                          const int32_t *first, const void *k_in, const void *v_in,
+                          int32_t n_tokens, int32_t *status, void *hip_stream);
+
+/* The same from a tier in shape.dtype: its tokens first[b] .. seq_lens[b] - 1, at most
+ * max_tokens per sequence, go to the same positions (after hgca_kv_evict, with the pool's
+ * length of before as `first`: what has left the window). */
+int hgca_kv8_write_tier(const hgca_shape *shape, const hgca_kv8_view *kv8,
+                        const int32_t *first, const hgca_kv_view *src,
+                        int32_t max_tokens, int32_t *status, void *hip_stream);
+
+/* Reads tokens first[b] .. first[b] + n_tokens - 1 back as rows k_out / v_out
+ * [B, n_tokens, Hkv, d] in shape.dtype; rows of tokens beyond seq_lens[b] are left as
+ * they are. */
+int hgca_kv8_read(const hgca_shape *shape, const hgca_kv8_view *kv8,
+                  const int32_t *first, int32_t n_tokens, void *k_out, void *v_out,
+                  void *hip_stream);
+
+/* Attention of n_q queries per sequence over every valid token of an 8-bit tier: one
+ * token's (n_q = 1), drafted tokens', a prompt's (n_q <= 4096).  The same as hgca_tree_attn
+ * without a mask over the values that the bytes stand for; shape.dtype is the type of q.
+ * ws needs hgca_kv8_workspace_bytes(shape, n_q, kv8->cap). */
+size_t hgca_kv8_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens);
+int hgca_kv8_attn(const hgca_shape *shape, const void *q, int32_t n_q,
+                  const hgca_kv8_view *kv8, void *o_out, int32_t o_dtype, float *lse_out,
+                  void *ws, size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

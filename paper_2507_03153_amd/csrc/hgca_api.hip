@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
+#include <initializer_list>
 
 #include "hgca_launch.hpp"
 
@@ -237,6 +238,83 @@ Partials partials_at(void *ws, const WsLayout &w, int n_splits)
 }
 
 int from_hip(hipError_t e) { return e == hipSuccess ? HGCA_OK : HGCA_ERR_DEVICE; }
+
+// ---- a few queries per sequence over one tier (hgca_tree_attn, hgca_kv8_attn) ----
+
+constexpr int32_t kMaxRowsCap = 1 << 30;         // positions and step counts of these calls stay clear of 2^31
+constexpr int32_t kMaxKv8Queries = 4096;
+
+// Splits of a (sequence, KV head, block of rows) whose tier holds up to `cap` tokens: about 1024 workgroups, two rounds of the two
+// that a compute unit holds, of 128 tokens at least (a step of each of a workgroup's four waves).
+#ifndef HGCA_TARGET_WGS_TREE
+#define HGCA_TARGET_WGS_TREE 1024
+#endif
+struct TreeLayout {
+    int32_t row_blocks, n_splits;
+    size_t part_o, part_m, part_l, total;
+};
+
+TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, int32_t cap)
+{
+    TreeLayout t{};
+    const int64_t rows = (int64_t)n_q * group_of(s), per_block = 16 * tree_row_tiles((int)rows);
+    t.row_blocks = (int32_t)((rows + per_block - 1) / per_block);
+    const int64_t units = std::max<int64_t>(1, (int64_t)s->batch * s->n_kv_heads * t.row_blocks);
+    t.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HGCA_TARGET_WGS_TREE / units, ((int64_t)cap + 127) / 128));
+    const size_t parts = t.n_splits > 1 ? (size_t)s->batch * n_q * s->n_q_heads * t.n_splits : 0;
+    t.part_m = align_up(parts * s->head_dim * sizeof(float));
+    t.part_l = t.part_m + align_up(parts * sizeof(float));
+    t.total = std::max(t.part_l + align_up(parts * sizeof(float)), kAlign);
+    return t;
+}
+
+int check_rows_call(const hgca_shape *s, const void *q, int32_t n_q, int32_t most, const hgca_kv_view *tier, const void *o,
+                    int32_t o_dtype, const float *lse)
+{
+    int rc = check_shape(s);
+    if (rc != HGCA_OK) return rc;
+    if ((rc = check_view(s, tier, true)) != HGCA_OK) return rc;
+    if (n_q < 1 || !(s->sm_scale > 0.f) || s->sm_scale > 3.0e38f) return HGCA_ERR_INVALID_ARG;
+    if (n_q > most || tier->cap > kMaxRowsCap || (o_dtype != HGCA_F32 && o_dtype != HGCA_BF16)) return HGCA_ERR_UNSUPPORTED;
+    if (s->batch == 0) return HGCA_OK;
+    if (!q || !aligned16(q) || !o || !aligned16(o) || !lse) return HGCA_ERR_INVALID_ARG;
+    return HGCA_OK;
+}
+
+int rows_attention(const hgca_shape *s, const void *q, int32_t n_q, bool kv8, TreeArgs &a, void *o, int32_t o_dtype, float *lse,
+                   void *ws, size_t ws_bytes, void *stream)
+{
+    const TreeLayout t = tree_layout(s, n_q, a.kv.cap);
+    if (!ws || ws_bytes < t.total || !aligned16(ws)) return HGCA_ERR_WORKSPACE;
+    char *base = static_cast<char *>(ws);
+    a.sh = to_dev(s);
+    a.q = q;
+    a.n_q = n_q;
+    a.n_splits = t.n_splits;
+    a.row_blocks = t.row_blocks;
+    a.o_bf16 = o_dtype == HGCA_BF16;
+    a.part_o = reinterpret_cast<float *>(base + t.part_o);
+    a.part_m = reinterpret_cast<float *>(base + t.part_m);
+    a.part_l = reinterpret_cast<float *>(base + t.part_l);
+    a.o = o;
+    a.lse = lse;
+    return from_hip(launch_tree_attn(s->dtype, s->head_dim, kv8, a, s->batch, static_cast<hipStream_t>(stream)));
+}
+
+// The rows of an 8-bit tier as a view (a table of its own shape checks), and the scales' pointers.
+int check_kv8(const hgca_shape *s, const hgca_kv8_view *k8, hgca_kv_view *rows)
+{
+    int rc = check_shape(s);
+    if (rc != HGCA_OK) return rc;
+    if (!k8) return HGCA_ERR_INVALID_ARG;
+    *rows = hgca_kv_view{k8->k, k8->v, k8->seq_lens, k8->block_table, k8->cap, k8->block_size, k8->max_blocks, k8->first_block};
+    if ((rc = check_view(s, rows, true)) != HGCA_OK) return rc;
+    if (k8->cap > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
+    if (k8->cap > 0)
+        for (const void *p : {k8->k_scale, k8->v_scale})
+            if (!p || reinterpret_cast<uintptr_t>(p) % 4 != 0) return HGCA_ERR_INVALID_ARG;
+    return HGCA_OK;
+}
 
 }  // namespace
 
@@ -1392,6 +1470,189 @@ int hgca_managed_append_step(const hgca_shape *shape, const hgca_cache_state *ca
     }
     // eviction of as many whole blocks as it takes, sparsification of what leaves
     return from_hip(launch_kv_evict(c, shape->batch, shape->n_q_heads, beta, s));
+}
+
+
+int hgca_qk_norm_rope(const hgca_shape *shape, const void *q_in, int64_t q_token_stride, const void *k_in,
+                      int64_t k_token_stride, int32_t n_tokens, const void *q_weight, const void *k_weight, float eps,
+                      const float *inv_freq, int32_t rot_dim, const int32_t *positions, const int32_t *first_pos, int32_t flags,
+                      void *q_out, void *k_out, void *hip_stream)
+{
+    int rc = check_shape(shape);
+    if (rc != HGCA_OK) return rc;
+    if (n_tokens < 0 || (flags & ~HGCA_ROPE_INTERLEAVED) || !(eps >= 0.f)) return HGCA_ERR_INVALID_ARG;
+    if (rot_dim <= 0 || rot_dim > shape->head_dim) return HGCA_ERR_INVALID_ARG;
+    if (rot_dim % 16 != 0) return HGCA_ERR_UNSUPPORTED;
+    if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
+    const int64_t e = shape->dtype == HGCA_BF16 ? 2 : 4, tokens = (int64_t)shape->batch * n_tokens;
+    const int64_t q_row = (int64_t)shape->n_q_heads * shape->head_dim, k_row = (int64_t)shape->n_kv_heads * shape->head_dim;
+    const int64_t qs = q_token_stride ? q_token_stride : q_row, ks = k_token_stride ? k_token_stride : k_row;
+    if (qs < q_row || ks < k_row || qs * e % 16 != 0 || ks * e % 16 != 0) return HGCA_ERR_INVALID_ARG;
+    if (qs > (int64_t(1) << 40) / tokens || ks > (int64_t(1) << 40) / tokens) return HGCA_ERR_UNSUPPORTED;   // offsets stay far from 2^63
+    for (const void *p : {q_in, k_in, (const void *)q_out, (const void *)k_out})
+        if (!p || !aligned16(p)) return HGCA_ERR_INVALID_ARG;
+    if (!inv_freq || (q_weight && !aligned16(q_weight)) || (k_weight && !aligned16(k_weight))) return HGCA_ERR_INVALID_ARG;
+    struct Range {
+        uintptr_t at, bytes;
+        bool meets(const Range &o) const { return at < o.at + o.bytes && o.at < at + bytes; }
+    };
+    auto range = [&](const void *p, int64_t stride, int64_t row) {
+        return Range{reinterpret_cast<uintptr_t>(p), (uintptr_t)(((tokens - 1) * stride + row) * e)};
+    };
+    const Range qi = range(q_in, qs, q_row), ki = range(k_in, ks, k_row), qo = range(q_out, q_row, q_row), ko = range(k_out, k_row, k_row);
+    if (qo.meets(ko) || qo.meets(ki) || ko.meets(qi)) return HGCA_ERR_INVALID_ARG;
+    if ((qo.meets(qi) && !(q_out == q_in && qs == q_row)) || (ko.meets(ki) && !(k_out == k_in && ks == k_row)))
+        return HGCA_ERR_INVALID_ARG;
+    RopeArgs a{};
+    a.q = static_cast<const char *>(q_in);
+    a.k = static_cast<const char *>(k_in);
+    a.q_stride = qs;
+    a.k_stride = ks;
+    a.tokens = tokens;
+    a.n_tokens = n_tokens;
+    a.n_q_heads = shape->n_q_heads;
+    a.n_kv_heads = shape->n_kv_heads;
+    a.rot = rot_dim;
+    a.interleaved = flags & HGCA_ROPE_INTERLEAVED ? 1 : 0;
+    a.q_weight = static_cast<const char *>(q_weight);
+    a.k_weight = static_cast<const char *>(k_weight);
+    a.inv_freq = inv_freq;
+    a.positions = positions;
+    a.first_pos = first_pos;
+    a.eps = eps;
+    a.q_out = static_cast<char *>(q_out);
+    a.k_out = static_cast<char *>(k_out);
+    return from_hip(launch_qk_norm_rope(shape->dtype, shape->head_dim, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t hgca_tree_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens)
+{
+    if (check_shape(shape) != HGCA_OK || n_q < 1 || n_q > HGCA_MAX_DRAFTS || max_tokens < 0) return 0;
+    return tree_layout(shape, n_q, max_tokens).total;
+}
+
+int hgca_tree_attn(const hgca_shape *shape, const void *q, int32_t n_q, const hgca_kv_view *tier, const uint64_t *draft_mask,
+                   void *o_out, int32_t o_dtype, float *lse_out, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_rows_call(shape, q, n_q, HGCA_MAX_DRAFTS, tier, o_out, o_dtype, lse_out);
+    if (rc != HGCA_OK || shape->batch == 0) return rc;
+    if (reinterpret_cast<uintptr_t>(draft_mask) % 8 != 0) return HGCA_ERR_INVALID_ARG;
+    TreeArgs a{};
+    a.kv = to_dev(tier);
+    a.mask = draft_mask;
+    return rows_attention(shape, q, n_q, false, a, o_out, o_dtype, lse_out, ws, ws_bytes, hip_stream);
+}
+
+int hgca_kv_commit(const hgca_shape *shape, const hgca_kv_view *tier, const int32_t *first, const void *k_in, const void *v_in,
+                   int32_t n_tokens, const int32_t *path, const int32_t *cnt, int32_t *lens_out, int32_t *status, void *hip_stream)
+{
+    int rc = check_shape(shape);
+    if (rc != HGCA_OK) return rc;
+    if ((rc = check_view(shape, tier, true)) != HGCA_OK) return rc;
+    if (n_tokens < 0) return HGCA_ERR_INVALID_ARG;
+    if (tier->cap > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
+    if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
+    if (!k_in || !v_in || !aligned16(k_in) || !aligned16(v_in) || !lens_out || lens_out == first) return HGCA_ERR_INVALID_ARG;
+    CommitArgs a{};
+    a.tier = to_dev(tier);
+    a.first = first;
+    a.path = path;
+    a.cnt = cnt;
+    a.lens_out = lens_out;
+    a.status = status;
+    a.k_in = static_cast<const char *>(k_in);
+    a.v_in = static_cast<const char *>(v_in);
+    a.n_tokens = n_tokens;
+    a.n_kv_heads = shape->n_kv_heads;
+    a.row_bytes = shape->head_dim * (shape->dtype == HGCA_BF16 ? 2 : 4);
+    return from_hip(launch_kv_commit(a, shape->batch, static_cast<hipStream_t>(hip_stream)));
+}
+
+int hgca_kv8_write_tokens(const hgca_shape *shape, const hgca_kv8_view *kv8, const int32_t *first, const void *k_in,
+                          const void *v_in, int32_t n_tokens, int32_t *status, void *hip_stream)
+{
+    hgca_kv_view rows{};
+    int rc = check_kv8(shape, kv8, &rows);
+    if (rc != HGCA_OK) return rc;
+    if (n_tokens < 0) return HGCA_ERR_INVALID_ARG;
+    if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
+    if (!k_in || !v_in || !aligned16(k_in) || !aligned16(v_in)) return HGCA_ERR_INVALID_ARG;
+    Kv8WriteArgs a{};
+    a.src.k = static_cast<const char *>(k_in);
+    a.src.v = static_cast<const char *>(v_in);
+    a.dst = to_dev(&rows);
+    a.k_scale = static_cast<char *>(kv8->k_scale);
+    a.v_scale = static_cast<char *>(kv8->v_scale);
+    a.first = first;
+    a.status = status;
+    a.n_tokens = n_tokens;
+    a.n_kv_heads = shape->n_kv_heads;
+    return from_hip(launch_kv8_write(shape->dtype, shape->head_dim, false, a, shape->batch, static_cast<hipStream_t>(hip_stream)));
+}
+
+int hgca_kv8_write_tier(const hgca_shape *shape, const hgca_kv8_view *kv8, const int32_t *first, const hgca_kv_view *src,
+                        int32_t max_tokens, int32_t *status, void *hip_stream)
+{
+    hgca_kv_view rows{};
+    int rc = check_kv8(shape, kv8, &rows);
+    if (rc != HGCA_OK) return rc;
+    if ((rc = check_view(shape, src, true)) != HGCA_OK) return rc;
+    if (max_tokens < 0) return HGCA_ERR_INVALID_ARG;
+    if (src->cap > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
+    const int32_t n = std::min(max_tokens, src->cap);
+    if (shape->batch == 0 || n == 0) return HGCA_OK;
+    Kv8WriteArgs a{};
+    a.src = to_dev(src);
+    a.dst = to_dev(&rows);
+    a.k_scale = static_cast<char *>(kv8->k_scale);
+    a.v_scale = static_cast<char *>(kv8->v_scale);
+    a.first = first;
+    a.status = status;
+    a.n_tokens = n;
+    a.n_kv_heads = shape->n_kv_heads;
+    return from_hip(launch_kv8_write(shape->dtype, shape->head_dim, true, a, shape->batch, static_cast<hipStream_t>(hip_stream)));
+}
+
+int hgca_kv8_read(const hgca_shape *shape, const hgca_kv8_view *kv8, const int32_t *first, int32_t n_tokens, void *k_out,
+                  void *v_out, void *hip_stream)
+{
+    hgca_kv_view rows{};
+    int rc = check_kv8(shape, kv8, &rows);
+    if (rc != HGCA_OK) return rc;
+    if (n_tokens < 0) return HGCA_ERR_INVALID_ARG;
+    if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
+    if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return HGCA_ERR_INVALID_ARG;
+    Kv8ReadArgs a{};
+    a.src = to_dev(&rows);
+    a.k_scale = static_cast<const char *>(kv8->k_scale);
+    a.v_scale = static_cast<const char *>(kv8->v_scale);
+    a.first = first;
+    a.k_out = static_cast<char *>(k_out);
+    a.v_out = static_cast<char *>(v_out);
+    a.n_tokens = n_tokens;
+    a.n_kv_heads = shape->n_kv_heads;
+    return from_hip(launch_kv8_read(shape->dtype, shape->head_dim, a, shape->batch, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t hgca_kv8_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens)
+{
+    if (check_shape(shape) != HGCA_OK || n_q < 1 || n_q > kMaxKv8Queries || max_tokens < 0) return 0;
+    return tree_layout(shape, n_q, max_tokens).total;
+}
+
+int hgca_kv8_attn(const hgca_shape *shape, const void *q, int32_t n_q, const hgca_kv8_view *kv8, void *o_out, int32_t o_dtype,
+                  float *lse_out, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    hgca_kv_view rows{};
+    int rc = check_kv8(shape, kv8, &rows);
+    if (rc != HGCA_OK) return rc;
+    if ((rc = check_rows_call(shape, q, n_q, kMaxKv8Queries, &rows, o_out, o_dtype, lse_out)) != HGCA_OK || shape->batch == 0)
+        return rc;
+    TreeArgs a{};
+    a.kv = to_dev(&rows);
+    a.k_scale = static_cast<const char *>(kv8->k_scale);
+    a.v_scale = static_cast<const char *>(kv8->v_scale);
+    return rows_attention(shape, q, n_q, true, a, o_out, o_dtype, lse_out, ws, ws_bytes, hip_stream);
 }
 
 }  // extern "C"

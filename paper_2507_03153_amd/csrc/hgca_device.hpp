@@ -9,6 +9,7 @@ namespace hgca {
 constexpr int kWave = 64;
 
 struct bf16_t { uint16_t bits; };   // storage tag: upper half of an IEEE fp32
+struct kv8_t { uint8_t bits; };     // storage tag: E4M3, scales of 32 columns apart
 
 // One KV tier as the kernels see it (mirrors hgca_kv_view, pointers are device memory).
 struct KvDev {

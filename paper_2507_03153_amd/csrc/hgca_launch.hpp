@@ -255,4 +255,65 @@ struct CtxCompactArgs {
 };
 hipError_t launch_ctx_compact(const CtxCompactArgs &a, hipStream_t s);
 
+// ---- tokens on their way into a cache: norm and rotation, 8-bit rows, accepted drafts ----
+
+struct RopeArgs {
+    const char *q, *k;         // rows of d elements, heads side by side; q_stride / k_stride elements from token to token
+    int64_t q_stride, k_stride, tokens;   // tokens = B * n_tokens
+    int32_t n_tokens, n_q_heads, n_kv_heads, rot, interleaved;
+    const char *q_weight, *k_weight;      // [d] or null (no norm)
+    const float *inv_freq;     // [rot / 2]
+    const int32_t *positions;  // [B, n_tokens] or null: first_pos[b] (null: 0) + i
+    const int32_t *first_pos;
+    float eps;
+    char *q_out, *k_out;       // [B, n_tokens, heads, d]
+};
+hipError_t launch_qk_norm_rope(int dtype, int head_dim, const RopeArgs &a, hipStream_t s);
+
+struct Kv8WriteArgs {
+    KvDev src;                 // a tier, or k / v = rows [B, n_tokens, Hkv, d]
+    KvDev dst;                 // k, v: codes (written)
+    char *k_scale, *v_scale;   // [rows of dst, d / 32]
+    const int32_t *first;      // [B] or null (= 0): position of the first token
+    int32_t *status;           // optional
+    int32_t n_tokens, n_kv_heads;
+};
+hipError_t launch_kv8_write(int dtype, int head_dim, bool from_tier, const Kv8WriteArgs &a, int batch, hipStream_t s);
+
+struct Kv8ReadArgs {
+    KvDev src;
+    const char *k_scale, *v_scale;
+    const int32_t *first;
+    char *k_out, *v_out;       // [B, n_tokens, Hkv, d]
+    int32_t n_tokens, n_kv_heads;
+};
+hipError_t launch_kv8_read(int dtype, int head_dim, const Kv8ReadArgs &a, int batch, hipStream_t s);
+
+struct CommitArgs {
+    KvDev tier;                // k, v are written
+    const int32_t *first, *path, *cnt;    // [B], [B, n_tokens], [B]; each may be null
+    int32_t *lens_out, *status;           // [B], optional
+    const char *k_in, *v_in;   // [B, n_tokens, Hkv, row]
+    int32_t n_tokens, n_kv_heads, row_bytes;
+};
+hipError_t launch_kv_commit(const CommitArgs &a, int batch, hipStream_t s);
+
+// ---- a few queries per sequence over one tier: drafted tokens, 8-bit rows ----
+
+struct TreeArgs {
+    ShapeDev sh;
+    const void *q;             // [B, n_q, Hq, d]
+    KvDev kv;
+    const char *k_scale, *v_scale;        // 8-bit tiers
+    const uint64_t *mask;      // [B, n_q] or null: bit j = the query sees the j-th of the tier's last n_q tokens
+    int32_t n_q, n_splits, row_blocks, o_bf16;
+    float *part_o, *part_m, *part_l;      // [rows, n_splits, d], [rows, n_splits]; m in units of ln 2
+    void *o;                   // [B, n_q, Hq, d]
+    float *lse;                // [B, n_q, Hq]
+};
+// 16-row tiles of a wave for `rows` query rows per KV head
+int tree_row_tiles(int rows);
+// kv8: the tier is in 8 bits (dtype is that of q); row_blocks = blocks of 16 * tree_row_tiles() rows
+hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s);
+
 }  // namespace hgca

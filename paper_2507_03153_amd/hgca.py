@@ -28,7 +28,9 @@ EXPORTS = ("hgca_status_string", "hgca_workspace_bytes", "hgca_dense_window_attn
            "hgca_append_weights", "hgca_dense_window_attn_maw", "hgca_select_salient_grouped", "hgca_union_lists",
            "hgca_sparse_attn_grouped", "hgca_hybrid_decode_step", "hgca_ctx_compact",
            "hgca_managed_decode_step", "hgca_dense_window_attn_static", "hgca_hybrid_decode_step_selected", "hgca_kv_append_tokens",
-           "hgca_managed_append_workspace_bytes", "hgca_managed_append_step")
+           "hgca_managed_append_workspace_bytes", "hgca_managed_append_step",
+           "hgca_qk_norm_rope", "hgca_tree_workspace_bytes", "hgca_tree_attn", "hgca_kv_commit", "hgca_kv8_write_tokens",
+           "hgca_kv8_write_tier", "hgca_kv8_read", "hgca_kv8_workspace_bytes", "hgca_kv8_attn")
 STATIC_SCRATCH_BYTES = 16 << 20                  # HGCA_STATIC_SCRATCH_BYTES of include/hgca.h
 CACHE_WINDOW_FULL, CACHE_CONTEXT_FULL, CACHE_LIST_FULL = 1, 2, 4
 
@@ -42,6 +44,11 @@ class KvView(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
                 ("block_table", ctypes.c_void_p), ("cap", ctypes.c_int32), ("block_size", ctypes.c_int32),
                 ("max_blocks", ctypes.c_int32), ("first_block", ctypes.c_void_p)]
+
+
+class Kv8View(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "seq_lens", "block_table")] + \
+               [(n, ctypes.c_int32) for n in ("cap", "block_size", "max_blocks")] + [("first_block", ctypes.c_void_p)]
 
 
 class CacheState(ctypes.Structure):
@@ -137,6 +144,25 @@ def lib() -> ctypes.CDLL:
         L.hgca_maw_update.argtypes = [ps, vp, vp, vp, i32, i32, ctypes.c_float, vp]
         L.hgca_threshold_select.restype = ctypes.c_int
         L.hgca_threshold_select.argtypes = [ps, vp, vp, i32, vp, i32, ctypes.c_double, i32, vp, vp, vp, vp]
+        p8, i64 = ctypes.POINTER(Kv8View), ctypes.c_int64
+        L.hgca_qk_norm_rope.restype = ctypes.c_int
+        L.hgca_qk_norm_rope.argtypes = [ps, vp, i64, vp, i64, i32, vp, vp, ctypes.c_float, vp, i32, vp, vp, i32, vp, vp, vp]
+        L.hgca_tree_workspace_bytes.restype = sz
+        L.hgca_tree_workspace_bytes.argtypes = [ps, i32, i32]
+        L.hgca_tree_attn.restype = ctypes.c_int
+        L.hgca_tree_attn.argtypes = [ps, vp, i32, pk, vp, vp, i32, vp, vp, sz, vp]
+        L.hgca_kv_commit.restype = ctypes.c_int
+        L.hgca_kv_commit.argtypes = [ps, pk, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+        L.hgca_kv8_write_tokens.restype = ctypes.c_int
+        L.hgca_kv8_write_tokens.argtypes = [ps, p8, vp, vp, vp, i32, vp, vp]
+        L.hgca_kv8_write_tier.restype = ctypes.c_int
+        L.hgca_kv8_write_tier.argtypes = [ps, p8, vp, pk, i32, vp, vp]
+        L.hgca_kv8_read.restype = ctypes.c_int
+        L.hgca_kv8_read.argtypes = [ps, p8, vp, i32, vp, vp, vp]
+        L.hgca_kv8_workspace_bytes.restype = sz
+        L.hgca_kv8_workspace_bytes.argtypes = [ps, i32, i32]
+        L.hgca_kv8_attn.restype = ctypes.c_int
+        L.hgca_kv8_attn.argtypes = [ps, vp, i32, p8, vp, i32, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -548,3 +574,217 @@ def managed_decode_step(shape: Shape, state: "CacheState", q, k_in, v_in, alpha:
                                           _dtype_code(o_out), _ptr(lse_out), _ptr(ws_dense), ws_dense.numel(),
                                           _ptr(ws_sparse), ws_sparse.numel(), _stream(stream)),
            "hgca_managed_decode_step")
+
+
+# ---- what a step needs beside its attention: norm and rotation, drafted tokens, an 8-bit tier ----
+
+ROPE_INTERLEAVED = 1
+MAX_DRAFTS = 64                                  # HGCA_MAX_DRAFTS of include/hgca.h
+
+
+@dataclass
+class Kv8Tier:
+    """A tier in 8 bits: k, v uint8 [B,Hkv,cap,d] or [n_blocks,Hkv,bs,d] (E4M3), k_scale, v_scale uint8 [...,d/32] (E8M0)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    cap: int
+    seq_lens: Optional[torch.Tensor] = None      # int32 [B]
+    block_table: Optional[torch.Tensor] = None   # int32 [B,max_blocks]
+    block_size: int = 0
+    first_block: Optional[torch.Tensor] = None   # int32 [B]
+
+    @staticmethod
+    def like(tier: "Tier") -> "Kv8Tier":
+        """Zeroed 8-bit storage for the rows of `tier`, with its lengths and block table."""
+        rows, d = tier.k.shape[:-1], int(tier.k.shape[-1])
+        z = lambda n: torch.zeros(*rows, n, dtype=torch.uint8, device=tier.k.device)
+        return Kv8Tier(z(d), z(d), z(d // 32), z(d // 32), tier.cap, tier.seq_lens, tier.block_table, tier.block_size,
+                       tier.first_block)
+
+    def view(self) -> Kv8View:
+        mb = 0 if self.block_table is None else int(self.block_table.shape[1])
+        return Kv8View(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), _ptr(self.seq_lens),
+                       _ptr(self.block_table), int(self.cap), int(self.block_size), mb, _ptr(self.first_block))
+
+
+def _need(name: str, t: Optional[torch.Tensor], dtype, *size: int, strided: bool = False) -> None:
+    """A given tensor has this type and size and is dense."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.shape != size:
+        raise ValueError(f"{name} must be {dtype} of size {list(size)}, got {t.dtype} of size {list(t.shape)}")
+    if not strided and not t.is_contiguous():
+        raise ValueError(f"{name}: libhgca takes contiguous tensors")
+
+
+def _need_tier(shape: Shape, tier, dtype) -> None:
+    """A tier's tensors against the shape: rows of every sequence and KV head, lengths, table."""
+    H, d, cap = shape.n_kv_heads, shape.head_dim, int(tier.cap)
+    paged = tier.block_table is not None
+    rows = (tier.k.shape[0], H, tier.block_size, d) if paged else (shape.batch, H, cap, d)
+    if cap or paged:
+        _need("tier.k", tier.k, dtype, *rows)
+        _need("tier.v", tier.v, dtype, *rows)
+        if dtype == torch.uint8:
+            _need("tier.k_scale", tier.k_scale, dtype, *rows[:3], d // 32)
+            _need("tier.v_scale", tier.v_scale, dtype, *rows[:3], d // 32)
+    _need("tier.seq_lens", tier.seq_lens, torch.int32, shape.batch)
+    if paged:
+        _need("tier.block_table", tier.block_table, torch.int32, shape.batch, tier.block_table.shape[1])
+        _need("tier.first_block", tier.first_block, torch.int32, shape.batch)
+
+
+def _tier_tensors(tier):
+    return tuple(t for t in vars(tier).values() if isinstance(t, torch.Tensor))
+
+
+def _launch(where: str, stream, tensors, *args) -> None:
+    """Calls `where` on the tensors' device and the given or the current stream of it."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("libhgca takes GPU tensors only (no CPU path exists)")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"{where}: tensors on {dev} and {t.device}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"{where}: tensors on {dev}, stream on {stream.device}")
+    if dev.index == torch.cuda.current_device():
+        _check(getattr(lib(), where)(*args, _stream(stream)), where)
+    else:
+        with torch.cuda.device(dev):
+            _check(getattr(lib(), where)(*args, _stream(stream)), where)
+
+
+def _torch_dtype(shape: Shape):
+    return torch.float32 if shape.dtype == F32 else torch.bfloat16
+
+
+def _token_stride(name: str, t: torch.Tensor) -> int:
+    """Elements between consecutive tokens of [B,n,H,d], whose heads lie side by side."""
+    B, n, H, d = t.shape
+    step = t.stride(1) if n > 1 else t.stride(0) if B > 1 else H * d
+    if (d > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != d) or (B > 1 and n > 1 and t.stride(0) != n * step):
+        raise ValueError(f"{name}: heads have to lie side by side and tokens at one distance")
+    return step
+
+
+def qk_norm_rope(shape: Shape, q, k, q_out, k_out, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 positions=None, first_pos=None, interleaved: bool = False, stream=None) -> None:
+    """q [B,n,Hq,d] and k [B,n,Hkv,d] normed per head and rotated by position into q_out, k_out (dense; may be q, k where
+    those are).  q and k may be parts of wider rows (a fused projection's).  inv_freq fp32 [rot/2]; positions int32 [B,n], or
+    first_pos int32 [B] for consecutive ones."""
+    dt, n, d = _torch_dtype(shape), int(q.shape[1]), shape.head_dim
+    for name, t, H in (("q", q, shape.n_q_heads), ("k", k, shape.n_kv_heads)):
+        _need(name, t, dt, shape.batch, n, H, d, strided=True)
+    _need("q_out", q_out, dt, shape.batch, n, shape.n_q_heads, d)
+    _need("k_out", k_out, dt, shape.batch, n, shape.n_kv_heads, d)
+    _need("q_weight", q_weight, dt, d)
+    _need("k_weight", k_weight, dt, d)
+    _need("inv_freq", inv_freq, torch.float32, inv_freq.numel())
+    _need("positions", positions, torch.int32, shape.batch, n)
+    _need("first_pos", first_pos, torch.int32, shape.batch)
+    _launch("hgca_qk_norm_rope", stream, (q, k, q_out, k_out, inv_freq, q_weight, k_weight, positions, first_pos),
+            ctypes.byref(shape), _ptr(q), _token_stride("q", q), _ptr(k), _token_stride("k", k), n, _ptr(q_weight), _ptr(k_weight),
+            float(eps), _ptr(inv_freq), 2 * inv_freq.numel(), _ptr(positions), _ptr(first_pos),
+            ROPE_INTERLEAVED if interleaved else 0, _ptr(q_out), _ptr(k_out))
+
+
+def tree_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Tensor:
+    n = int(lib().hgca_tree_workspace_bytes(ctypes.byref(shape), int(n_q), int(max_tokens)))
+    if n == 0:
+        raise HgcaError(ERR_INVALID_ARG, "hgca_tree_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _need_result(shape: Shape, q, o_out, lse_out) -> int:
+    n = int(q.shape[1])
+    _need("q", q, _torch_dtype(shape), shape.batch, n, shape.n_q_heads, shape.head_dim)
+    _need("o_out", o_out, torch.bfloat16 if o_out.dtype == torch.bfloat16 else torch.float32, *q.shape)
+    _need("lse_out", lse_out, torch.float32, shape.batch, n, shape.n_q_heads)
+    return n
+
+
+def tree_attn(shape: Shape, q, tier: Tier, mask, o_out, lse_out, ws, stream=None) -> None:
+    """Attention of q [B,n,Hq,d], n <= MAX_DRAFTS drafted tokens that are the tier's last n, over the tier; mask int64 [B,n]: bit
+    j of mask[b,i] = query i sees draft j (None: all).  o_out [B,n,Hq,d] fp32 or bf16, lse_out [B,n,Hq] fp32."""
+    n = _need_result(shape, q, o_out, lse_out)
+    _need("mask", mask, torch.int64, shape.batch, n)
+    _need_tier(shape, tier, _torch_dtype(shape))
+    kv = tier.view()
+    _launch("hgca_tree_attn", stream, (q, mask, o_out, lse_out, ws) + _tier_tensors(tier), ctypes.byref(shape), _ptr(q), n,
+            ctypes.byref(kv), _ptr(mask), _ptr(o_out), _dtype_code(o_out), _ptr(lse_out), _ptr(ws), ws.numel())
+
+
+def kv_commit(shape: Shape, tier: Tier, first, k_in, v_in, lens_out, path=None, cnt=None, status=None, stream=None) -> None:
+    """Rows path[b,i], i < cnt[b], of k_in / v_in [B,n,Hkv,d] go to positions first[b] + i of the tier; lens_out[b] = first[b] +
+    cnt[b].  path int32 [B,n] (None: row i), cnt int32 [B] (None: n), first int32 [B] (None: 0)."""
+    dt, n = _torch_dtype(shape), int(k_in.shape[1])
+    _need("k_in", k_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
+    _need("v_in", v_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
+    _need("first", first, torch.int32, shape.batch)
+    _need("path", path, torch.int32, shape.batch, n)
+    _need("cnt", cnt, torch.int32, shape.batch)
+    _need("lens_out", lens_out, torch.int32, shape.batch)
+    _need("status", status, torch.int32, 1)
+    _need_tier(shape, tier, dt)
+    kv = tier.view()
+    _launch("hgca_kv_commit", stream, (k_in, v_in, first, path, cnt, lens_out, status) + _tier_tensors(tier), ctypes.byref(shape),
+            ctypes.byref(kv), _ptr(first), _ptr(k_in), _ptr(v_in), n, _ptr(path), _ptr(cnt), _ptr(lens_out), _ptr(status))
+
+
+def kv8_write_tokens(shape: Shape, tier: Kv8Tier, first, k_in, v_in, status=None, stream=None) -> None:
+    """k_in / v_in [B,n,Hkv,d] in 8 bits to positions first[b] .. (int32 [B], None: 0)."""
+    dt, n = _torch_dtype(shape), int(k_in.shape[1])
+    _need("k_in", k_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
+    _need("v_in", v_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
+    _need("first", first, torch.int32, shape.batch)
+    _need("status", status, torch.int32, 1)
+    _need_tier(shape, tier, torch.uint8)
+    kv8 = tier.view()
+    _launch("hgca_kv8_write_tokens", stream, (k_in, v_in, first, status) + _tier_tensors(tier), ctypes.byref(shape),
+            ctypes.byref(kv8), _ptr(first), _ptr(k_in), _ptr(v_in), n, _ptr(status))
+
+
+def kv8_write_tier(shape: Shape, tier: Kv8Tier, first, src: Tier, max_tokens: int, status=None, stream=None) -> None:
+    """Tokens first[b] .. src.seq_lens[b] - 1 of src (max_tokens per sequence at most) in 8 bits to the same positions."""
+    _need("first", first, torch.int32, shape.batch)
+    _need("status", status, torch.int32, 1)
+    _need_tier(shape, tier, torch.uint8)
+    _need_tier(shape, src, _torch_dtype(shape))
+    kv8, kv = tier.view(), src.view()
+    _launch("hgca_kv8_write_tier", stream, (first, status) + _tier_tensors(tier) + _tier_tensors(src), ctypes.byref(shape),
+            ctypes.byref(kv8), _ptr(first), ctypes.byref(kv), int(max_tokens), _ptr(status))
+
+
+def kv8_read(shape: Shape, tier: Kv8Tier, first, k_out, v_out, stream=None) -> None:
+    """Tokens first[b] .. of an 8-bit tier as rows k_out / v_out [B,n,Hkv,d]; rows of tokens beyond the length stay."""
+    dt, n = _torch_dtype(shape), int(k_out.shape[1])
+    _need("k_out", k_out, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
+    _need("v_out", v_out, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
+    _need("first", first, torch.int32, shape.batch)
+    _need_tier(shape, tier, torch.uint8)
+    kv8 = tier.view()
+    _launch("hgca_kv8_read", stream, (k_out, v_out, first) + _tier_tensors(tier), ctypes.byref(shape), ctypes.byref(kv8),
+            _ptr(first), n, _ptr(k_out), _ptr(v_out))
+
+
+def kv8_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Tensor:
+    n = int(lib().hgca_kv8_workspace_bytes(ctypes.byref(shape), int(n_q), int(max_tokens)))
+    if n == 0:
+        raise HgcaError(ERR_INVALID_ARG, "hgca_kv8_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def kv8_attn(shape: Shape, q, tier: Kv8Tier, o_out, lse_out, ws, stream=None) -> None:
+    """Attention of q [B,n,Hq,d] over every valid token of an 8-bit tier; o_out [B,n,Hq,d] fp32 or bf16, lse_out fp32."""
+    n = _need_result(shape, q, o_out, lse_out)
+    _need_tier(shape, tier, torch.uint8)
+    kv8 = tier.view()
+    _launch("hgca_kv8_attn", stream, (q, o_out, lse_out, ws) + _tier_tensors(tier), ctypes.byref(shape), _ptr(q), n,
+            ctypes.byref(kv8), _ptr(o_out), _dtype_code(o_out), _ptr(lse_out), _ptr(ws), ws.numel())
