@@ -609,52 +609,51 @@ class Kv8Tier:
                        _ptr(self.block_table), int(self.cap), int(self.block_size), mb, _ptr(self.first_block))
 
 
-def _need(name: str, t: Optional[torch.Tensor], dtype, *size: int, strided: bool = False) -> None:
-    """A given tensor has this type and size and is dense."""
-    if t is None:
-        return
-    if t.dtype != dtype or t.shape != size:
+def _need(name: str, t: torch.Tensor, dtype, size: tuple, dev: int) -> None:
+    """The tensor has this type and size, is dense and lies on GPU `dev` (one test per property: a call's checks are a third
+    of what it costs the host)."""
+    if t.dtype is not dtype or t.shape != size:
         raise ValueError(f"{name} must be {dtype} of size {list(size)}, got {t.dtype} of size {list(t.shape)}")
-    if not strided and not t.is_contiguous():
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on cuda:{dev}")
+    if not t.is_contiguous():
         raise ValueError(f"{name}: libhgca takes contiguous tensors")
 
 
-def _need_tier(shape: Shape, tier, dtype) -> None:
-    """A tier's tensors against the shape: rows of every sequence and KV head, lengths, table."""
-    H, d, cap = shape.n_kv_heads, shape.head_dim, int(tier.cap)
-    paged = tier.block_table is not None
-    rows = (tier.k.shape[0], H, tier.block_size, d) if paged else (shape.batch, H, cap, d)
-    if cap or paged:
-        _need("tier.k", tier.k, dtype, *rows)
-        _need("tier.v", tier.v, dtype, *rows)
-        if dtype == torch.uint8:
-            _need("tier.k_scale", tier.k_scale, dtype, *rows[:3], d // 32)
-            _need("tier.v_scale", tier.v_scale, dtype, *rows[:3], d // 32)
-    _need("tier.seq_lens", tier.seq_lens, torch.int32, shape.batch)
-    if paged:
-        _need("tier.block_table", tier.block_table, torch.int32, shape.batch, tier.block_table.shape[1])
-        _need("tier.first_block", tier.first_block, torch.int32, shape.batch)
+def _gpu_of(t: torch.Tensor) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("libhgca takes GPU tensors only (no CPU path exists)")
+    return dev
 
 
-def _tier_tensors(tier):
-    return tuple(t for t in vars(tier).values() if isinstance(t, torch.Tensor))
+def _tier_view(tier, B: int, H: int, d: int, dtype, dev: int):
+    """The view of a tier whose tensors have been checked: rows of every sequence and KV head, lengths, table."""
+    k, v, lens, table, first, cap, bs = tier.k, tier.v, tier.seq_lens, tier.block_table, tier.first_block, int(tier.cap), 0
+    rows, mb = (B, H, cap), 0
+    if table is not None:
+        bs = int(tier.block_size)
+        rows, mb = (k.shape[0], H, bs), int(table.shape[1])
+        _need("tier.block_table", table, torch.int32, (B, mb), dev)
+        if first is not None:
+            _need("tier.first_block", first, torch.int32, (B,), dev)
+    _need("tier.k", k, dtype, rows + (d,), dev)
+    _need("tier.v", v, dtype, rows + (d,), dev)
+    if lens is not None:
+        _need("tier.seq_lens", lens, torch.int32, (B,), dev)
+    if dtype is torch.uint8:
+        ks, vs = tier.k_scale, tier.v_scale
+        _need("tier.k_scale", ks, dtype, rows + (d // 32,), dev)
+        _need("tier.v_scale", vs, dtype, rows + (d // 32,), dev)
+        return Kv8View(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), _ptr(lens), _ptr(table), cap, bs, mb, _ptr(first))
+    return KvView(k.data_ptr(), v.data_ptr(), _ptr(lens), _ptr(table), cap, bs, mb, _ptr(first))
 
 
-def _launch(where: str, stream, tensors, *args) -> None:
-    """Calls `where` on the tensors' device and the given or the current stream of it."""
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("libhgca takes GPU tensors only (no CPU path exists)")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"{where}: tensors on {dev} and {t.device}")
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"{where}: tensors on {dev}, stream on {stream.device}")
-    if dev.index == torch.cuda.current_device():
+def _launch(where: str, stream, dev: int, *args) -> None:
+    """Calls `where` on GPU `dev`, on the given stream or the current one there."""
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"{where}: tensors on cuda:{dev}, stream on {stream.device}")
+    if dev == (torch.cuda.current_device() if _device is None else _device()):
         _check(getattr(lib(), where)(*args, _stream(stream)), where)
     else:
         with torch.cuda.device(dev):
@@ -665,11 +664,16 @@ def _torch_dtype(shape: Shape):
     return torch.float32 if shape.dtype == F32 else torch.bfloat16
 
 
+def _heads(shape: Shape):
+    return shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim
+
+
 def _token_stride(name: str, t: torch.Tensor) -> int:
     """Elements between consecutive tokens of [B,n,H,d], whose heads lie side by side."""
     B, n, H, d = t.shape
-    step = t.stride(1) if n > 1 else t.stride(0) if B > 1 else H * d
-    if (d > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != d) or (B > 1 and n > 1 and t.stride(0) != n * step):
+    s0, s1, s2, s3 = t.stride()
+    step = s1 if n > 1 else s0 if B > 1 else H * d
+    if s3 != 1 or (H > 1 and s2 != d) or (B > 1 and n > 1 and s0 != n * step):
         raise ValueError(f"{name}: heads have to lie side by side and tokens at one distance")
     return step
 
@@ -679,20 +683,26 @@ def qk_norm_rope(shape: Shape, q, k, q_out, k_out, inv_freq, q_weight=None, k_we
     """q [B,n,Hq,d] and k [B,n,Hkv,d] normed per head and rotated by position into q_out, k_out (dense; may be q, k where
     those are).  q and k may be parts of wider rows (a fused projection's).  inv_freq fp32 [rot/2]; positions int32 [B,n], or
     first_pos int32 [B] for consecutive ones."""
-    dt, n, d = _torch_dtype(shape), int(q.shape[1]), shape.head_dim
-    for name, t, H in (("q", q, shape.n_q_heads), ("k", k, shape.n_kv_heads)):
-        _need(name, t, dt, shape.batch, n, H, d, strided=True)
-    _need("q_out", q_out, dt, shape.batch, n, shape.n_q_heads, d)
-    _need("k_out", k_out, dt, shape.batch, n, shape.n_kv_heads, d)
-    _need("q_weight", q_weight, dt, d)
-    _need("k_weight", k_weight, dt, d)
-    _need("inv_freq", inv_freq, torch.float32, inv_freq.numel())
-    _need("positions", positions, torch.int32, shape.batch, n)
-    _need("first_pos", first_pos, torch.int32, shape.batch)
-    _launch("hgca_qk_norm_rope", stream, (q, k, q_out, k_out, inv_freq, q_weight, k_weight, positions, first_pos),
-            ctypes.byref(shape), _ptr(q), _token_stride("q", q), _ptr(k), _token_stride("k", k), n, _ptr(q_weight), _ptr(k_weight),
-            float(eps), _ptr(inv_freq), 2 * inv_freq.numel(), _ptr(positions), _ptr(first_pos),
-            ROPE_INTERLEAVED if interleaved else 0, _ptr(q_out), _ptr(k_out))
+    B, Hq, Hkv, d = _heads(shape)
+    dt, dev, n = _torch_dtype(shape), _gpu_of(q), int(q.shape[1])
+    if q.dtype is not dt or q.shape != (B, n, Hq, d) or k.dtype is not dt or k.shape != (B, n, Hkv, d) or k.get_device() != dev:
+        raise ValueError(f"q and k must be {dt} of sizes {[B, n, Hq, d]} and {[B, n, Hkv, d]} on one GPU, got {q.dtype} {list(q.shape)} "
+                         f"and {k.dtype} {list(k.shape)}")
+    _need("q_out", q_out, dt, (B, n, Hq, d), dev)
+    _need("k_out", k_out, dt, (B, n, Hkv, d), dev)
+    half = inv_freq.numel()
+    _need("inv_freq", inv_freq, torch.float32, (half,), dev)
+    if q_weight is not None:
+        _need("q_weight", q_weight, dt, (d,), dev)
+    if k_weight is not None:
+        _need("k_weight", k_weight, dt, (d,), dev)
+    if positions is not None:
+        _need("positions", positions, torch.int32, (B, n), dev)
+    if first_pos is not None:
+        _need("first_pos", first_pos, torch.int32, (B,), dev)
+    _launch("hgca_qk_norm_rope", stream, dev, ctypes.byref(shape), q.data_ptr(), _token_stride("q", q), k.data_ptr(),
+            _token_stride("k", k), n, _ptr(q_weight), _ptr(k_weight), eps, inv_freq.data_ptr(), 2 * half, _ptr(positions),
+            _ptr(first_pos), ROPE_INTERLEAVED if interleaved else 0, q_out.data_ptr(), k_out.data_ptr())
 
 
 def tree_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Tensor:
@@ -702,76 +712,80 @@ def tree_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Ten
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _need_result(shape: Shape, q, o_out, lse_out) -> int:
-    n = int(q.shape[1])
-    _need("q", q, _torch_dtype(shape), shape.batch, n, shape.n_q_heads, shape.head_dim)
-    _need("o_out", o_out, torch.bfloat16 if o_out.dtype == torch.bfloat16 else torch.float32, *q.shape)
-    _need("lse_out", lse_out, torch.float32, shape.batch, n, shape.n_q_heads)
-    return n
+def _rows_call(where: str, shape: Shape, q, tier, tier_dtype, mask, o_out, lse_out, ws, stream) -> None:
+    B, Hq, Hkv, d = _heads(shape)
+    dt, dev, n = _torch_dtype(shape), _gpu_of(q), int(q.shape[1])
+    _need("q", q, dt, (B, n, Hq, d), dev)
+    _need("o_out", o_out, torch.bfloat16 if o_out.dtype is torch.bfloat16 else torch.float32, (B, n, Hq, d), dev)
+    _need("lse_out", lse_out, torch.float32, (B, n, Hq), dev)
+    _need("ws", ws, torch.uint8, (ws.numel(),), dev)
+    kv = _tier_view(tier, B, Hkv, d, tier_dtype or dt, dev)
+    if tier_dtype is None:
+        if mask is not None:
+            _need("mask", mask, torch.int64, (B, n), dev)
+        _launch(where, stream, dev, ctypes.byref(shape), q.data_ptr(), n, ctypes.byref(kv), _ptr(mask), o_out.data_ptr(),
+                _dtype_code(o_out), lse_out.data_ptr(), ws.data_ptr(), ws.numel())
+    else:
+        _launch(where, stream, dev, ctypes.byref(shape), q.data_ptr(), n, ctypes.byref(kv), o_out.data_ptr(), _dtype_code(o_out),
+                lse_out.data_ptr(), ws.data_ptr(), ws.numel())
 
 
 def tree_attn(shape: Shape, q, tier: Tier, mask, o_out, lse_out, ws, stream=None) -> None:
     """Attention of q [B,n,Hq,d], n <= MAX_DRAFTS drafted tokens that are the tier's last n, over the tier; mask int64 [B,n]: bit
     j of mask[b,i] = query i sees draft j (None: all).  o_out [B,n,Hq,d] fp32 or bf16, lse_out [B,n,Hq] fp32."""
-    n = _need_result(shape, q, o_out, lse_out)
-    _need("mask", mask, torch.int64, shape.batch, n)
-    _need_tier(shape, tier, _torch_dtype(shape))
-    kv = tier.view()
-    _launch("hgca_tree_attn", stream, (q, mask, o_out, lse_out, ws) + _tier_tensors(tier), ctypes.byref(shape), _ptr(q), n,
-            ctypes.byref(kv), _ptr(mask), _ptr(o_out), _dtype_code(o_out), _ptr(lse_out), _ptr(ws), ws.numel())
+    _rows_call("hgca_tree_attn", shape, q, tier, None, mask, o_out, lse_out, ws, stream)
+
+
+def _optional(dev: int, *given) -> None:
+    for name, t, size in given:
+        if t is not None:
+            _need(name, t, torch.int32, size, dev)
 
 
 def kv_commit(shape: Shape, tier: Tier, first, k_in, v_in, lens_out, path=None, cnt=None, status=None, stream=None) -> None:
     """Rows path[b,i], i < cnt[b], of k_in / v_in [B,n,Hkv,d] go to positions first[b] + i of the tier; lens_out[b] = first[b] +
     cnt[b].  path int32 [B,n] (None: row i), cnt int32 [B] (None: n), first int32 [B] (None: 0)."""
-    dt, n = _torch_dtype(shape), int(k_in.shape[1])
-    _need("k_in", k_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
-    _need("v_in", v_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
-    _need("first", first, torch.int32, shape.batch)
-    _need("path", path, torch.int32, shape.batch, n)
-    _need("cnt", cnt, torch.int32, shape.batch)
-    _need("lens_out", lens_out, torch.int32, shape.batch)
-    _need("status", status, torch.int32, 1)
-    _need_tier(shape, tier, dt)
-    kv = tier.view()
-    _launch("hgca_kv_commit", stream, (k_in, v_in, first, path, cnt, lens_out, status) + _tier_tensors(tier), ctypes.byref(shape),
-            ctypes.byref(kv), _ptr(first), _ptr(k_in), _ptr(v_in), n, _ptr(path), _ptr(cnt), _ptr(lens_out), _ptr(status))
+    B, _, Hkv, d = _heads(shape)
+    dt, dev, n = _torch_dtype(shape), _gpu_of(k_in), int(k_in.shape[1])
+    _need("k_in", k_in, dt, (B, n, Hkv, d), dev)
+    _need("v_in", v_in, dt, (B, n, Hkv, d), dev)
+    _optional(dev, ("first", first, (B,)), ("path", path, (B, n)), ("cnt", cnt, (B,)), ("lens_out", lens_out, (B,)), ("status", status, (1,)))
+    kv = _tier_view(tier, B, Hkv, d, dt, dev)
+    _launch("hgca_kv_commit", stream, dev, ctypes.byref(shape), ctypes.byref(kv), _ptr(first), k_in.data_ptr(), v_in.data_ptr(), n,
+            _ptr(path), _ptr(cnt), _ptr(lens_out), _ptr(status))
 
 
 def kv8_write_tokens(shape: Shape, tier: Kv8Tier, first, k_in, v_in, status=None, stream=None) -> None:
     """k_in / v_in [B,n,Hkv,d] in 8 bits to positions first[b] .. (int32 [B], None: 0)."""
-    dt, n = _torch_dtype(shape), int(k_in.shape[1])
-    _need("k_in", k_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
-    _need("v_in", v_in, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
-    _need("first", first, torch.int32, shape.batch)
-    _need("status", status, torch.int32, 1)
-    _need_tier(shape, tier, torch.uint8)
-    kv8 = tier.view()
-    _launch("hgca_kv8_write_tokens", stream, (k_in, v_in, first, status) + _tier_tensors(tier), ctypes.byref(shape),
-            ctypes.byref(kv8), _ptr(first), _ptr(k_in), _ptr(v_in), n, _ptr(status))
+    B, _, Hkv, d = _heads(shape)
+    dt, dev, n = _torch_dtype(shape), _gpu_of(k_in), int(k_in.shape[1])
+    _need("k_in", k_in, dt, (B, n, Hkv, d), dev)
+    _need("v_in", v_in, dt, (B, n, Hkv, d), dev)
+    _optional(dev, ("first", first, (B,)), ("status", status, (1,)))
+    kv8 = _tier_view(tier, B, Hkv, d, torch.uint8, dev)
+    _launch("hgca_kv8_write_tokens", stream, dev, ctypes.byref(shape), ctypes.byref(kv8), _ptr(first), k_in.data_ptr(),
+            v_in.data_ptr(), n, _ptr(status))
 
 
 def kv8_write_tier(shape: Shape, tier: Kv8Tier, first, src: Tier, max_tokens: int, status=None, stream=None) -> None:
     """Tokens first[b] .. src.seq_lens[b] - 1 of src (max_tokens per sequence at most) in 8 bits to the same positions."""
-    _need("first", first, torch.int32, shape.batch)
-    _need("status", status, torch.int32, 1)
-    _need_tier(shape, tier, torch.uint8)
-    _need_tier(shape, src, _torch_dtype(shape))
-    kv8, kv = tier.view(), src.view()
-    _launch("hgca_kv8_write_tier", stream, (first, status) + _tier_tensors(tier) + _tier_tensors(src), ctypes.byref(shape),
-            ctypes.byref(kv8), _ptr(first), ctypes.byref(kv), int(max_tokens), _ptr(status))
+    B, _, Hkv, d = _heads(shape)
+    dev = _gpu_of(src.k)
+    _optional(dev, ("first", first, (B,)), ("status", status, (1,)))
+    kv8, kv = _tier_view(tier, B, Hkv, d, torch.uint8, dev), _tier_view(src, B, Hkv, d, _torch_dtype(shape), dev)
+    _launch("hgca_kv8_write_tier", stream, dev, ctypes.byref(shape), ctypes.byref(kv8), _ptr(first), ctypes.byref(kv),
+            int(max_tokens), _ptr(status))
 
 
 def kv8_read(shape: Shape, tier: Kv8Tier, first, k_out, v_out, stream=None) -> None:
     """Tokens first[b] .. of an 8-bit tier as rows k_out / v_out [B,n,Hkv,d]; rows of tokens beyond the length stay."""
-    dt, n = _torch_dtype(shape), int(k_out.shape[1])
-    _need("k_out", k_out, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
-    _need("v_out", v_out, dt, shape.batch, n, shape.n_kv_heads, shape.head_dim)
-    _need("first", first, torch.int32, shape.batch)
-    _need_tier(shape, tier, torch.uint8)
-    kv8 = tier.view()
-    _launch("hgca_kv8_read", stream, (k_out, v_out, first) + _tier_tensors(tier), ctypes.byref(shape), ctypes.byref(kv8),
-            _ptr(first), n, _ptr(k_out), _ptr(v_out))
+    B, _, Hkv, d = _heads(shape)
+    dt, dev, n = _torch_dtype(shape), _gpu_of(k_out), int(k_out.shape[1])
+    _need("k_out", k_out, dt, (B, n, Hkv, d), dev)
+    _need("v_out", v_out, dt, (B, n, Hkv, d), dev)
+    _optional(dev, ("first", first, (B,)))
+    kv8 = _tier_view(tier, B, Hkv, d, torch.uint8, dev)
+    _launch("hgca_kv8_read", stream, dev, ctypes.byref(shape), ctypes.byref(kv8), _ptr(first), n, k_out.data_ptr(), v_out.data_ptr())
 
 
 def kv8_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Tensor:
@@ -783,8 +797,4 @@ def kv8_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Tens
 
 def kv8_attn(shape: Shape, q, tier: Kv8Tier, o_out, lse_out, ws, stream=None) -> None:
     """Attention of q [B,n,Hq,d] over every valid token of an 8-bit tier; o_out [B,n,Hq,d] fp32 or bf16, lse_out fp32."""
-    n = _need_result(shape, q, o_out, lse_out)
-    _need_tier(shape, tier, torch.uint8)
-    kv8 = tier.view()
-    _launch("hgca_kv8_attn", stream, (q, o_out, lse_out, ws) + _tier_tensors(tier), ctypes.byref(shape), _ptr(q), n,
-            ctypes.byref(kv8), _ptr(o_out), _dtype_code(o_out), _ptr(lse_out), _ptr(ws), ws.numel())
+    _rows_call("hgca_kv8_attn", shape, q, tier, torch.uint8, None, o_out, lse_out, ws, stream)

@@ -148,26 +148,37 @@ def test_python_checks(hg):
     tier = hg.Tier(kv, kv.clone(), 64)
     with pytest.raises(ValueError, match="GPU"):
         hg.tree_attn(sh, q, tier, mask, o, lse, ws)
-    with pytest.raises(ValueError, match="mask"):
-        hg.tree_attn(sh, q, tier, mask.int(), o, lse, ws)
-    with pytest.raises(ValueError, match="lse_out"):
-        hg.tree_attn(sh, q, tier, mask, o, lse[:, :2], ws)
-    with pytest.raises(ValueError, match="tier.k"):
-        hg.tree_attn(sh, q, hg.Tier(kv, kv, 65), mask, o, lse, ws)
-    with pytest.raises(ValueError, match="q must be"):
-        hg.tree_attn(sh, q.float(), tier, mask, o, lse, ws)
+    with pytest.raises(ValueError, match="GPU"):
+        hg.kv8_attn(sh, q, tier, o, lse, ws)
+    with pytest.raises(ValueError, match="GPU"):
+        hg.qk_norm_rope(sh, q, q, q, q, o)
+    with pytest.raises(ValueError, match="GPU"):
+        hg.kv_commit(sh, tier, None, q, q, lse)
+    # as one GPU's tensors are checked (device -1 stands for it)
+    hg._need("mask", mask, torch.int64, (B, n), -1)
+    with pytest.raises(ValueError, match="mask must be"):
+        hg._need("mask", mask.int(), torch.int64, (B, n), -1)
+    with pytest.raises(ValueError, match="lse_out must be"):
+        hg._need("lse_out", lse[:, :2], torch.float32, (B, n, Hq), -1)
+    with pytest.raises(ValueError, match="contiguous"):
+        hg._need("lse_out", lse.transpose(0, 1), torch.float32, (n, B, Hq), -1)
+    with pytest.raises(ValueError, match="other tensors on cuda:1"):
+        hg._need("mask", mask, torch.int64, (B, n), 1)
+    with pytest.raises(ValueError, match="tier.k must be"):
+        hg._tier_view(hg.Tier(kv, kv, 65), B, Hkv, d, torch.bfloat16, -1)
+    with pytest.raises(ValueError, match="seq_lens"):
+        hg._tier_view(hg.Tier(kv, kv, 64, torch.zeros(B)), B, Hkv, d, torch.bfloat16, -1)
+    with pytest.raises(ValueError, match="block_table"):
+        hg._tier_view(hg.Tier(kv, kv, 64, None, torch.zeros(B + 1, 4, dtype=torch.int32), 64), B, Hkv, d, torch.bfloat16, -1)
     z = lambda w: torch.zeros(B, Hkv, 64, w, dtype=torch.uint8)
     with pytest.raises(ValueError, match="k_scale"):
-        hg.kv8_attn(sh, q, hg.Kv8Tier(z(d), z(d), z(2), z(4), 64), o, lse, ws)
+        hg._tier_view(hg.Kv8Tier(z(d), z(d), z(2), z(4), 64), B, Hkv, d, torch.uint8, -1)
     wide = torch.zeros(B, n, (Hq + 2 * Hkv) * d, **bf)
     qv, kv_ = wide[..., :Hq * d].unflatten(-1, (Hq, d)), wide[..., Hq * d:(Hq + Hkv) * d].unflatten(-1, (Hkv, d))
     assert hg._token_stride("q", qv) == hg._token_stride("k", kv_) == (Hq + 2 * Hkv) * d
     assert hg._token_stride("q", qv[:1, :1]) == Hq * d
     with pytest.raises(ValueError, match="side by side"):
         hg._token_stride("q", wide.unflatten(-1, (-1, d)).transpose(1, 2))
-    with pytest.raises(ValueError, match="first"):
-        hg.kv_commit(sh, tier, torch.zeros(B), kv[:, :, :n].transpose(1, 2).contiguous(), kv[:, :, :n].transpose(1, 2).contiguous(),
-                     torch.zeros(B, dtype=torch.int32))
 
 
 # ---- the oracle ----
