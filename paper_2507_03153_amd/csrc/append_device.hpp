@@ -120,6 +120,78 @@ template <int D, int NW> struct DmaStage {
     }
 };
 
+constexpr int kNonTemporal = 2;                  // cache policy of a load: streamed once
+constexpr int64_t kLastCache = int64_t(256) << 20;
+
+// s_waitcnt vmcnt(0) (expcnt and lgkmcnt fields at their maxima = no wait): an LDS-direct load has landed in LDS
+// when the wave's memory-load counter has counted it down.  Every wave does this before the barrier after which
+// other waves read what it loaded.
+__device__ __forceinline__ void wait_for_own_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// Requests the K and the V rows of a step.  A load instruction of a wave covers kGroupRows rows of one granule, so in
+// a full step its address is a scalar (the granule's row) plus an offset that is the lane's for good; only a step
+// that the pass's end cuts computes rows per lane (tokens behind the end read the last row).  The row numbers of a
+// paged tier are looked up before the first load is issued: an LDS read placed after an LDS-direct load waits for it.
+// POLICY_K and POLICY_V are the loads' cache policies: 0, or kNonTemporal where the rows are not to stay in the caches.
+template <int D, int NW, int POLICY_K, int POLICY_V>
+__device__ __forceinline__ void dma_step(const KvDev &kv, const BlockRows &rows, int step, int nsub, char *k_stage,
+                                         char *v_stage)
+{
+    using S = DmaStage<D, NW>;
+    static_assert(kGranule % S::kGroupRows == 0, "a load stays inside a granule");
+    constexpr int kQuadLanes = 4 * S::kRowBytes / 16;
+    const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    // what lands at byte 16 * lane of the wave's u-th group: the row inside the group and the byte of the row
+    const int k_row = lane / S::kPieces, v_row = 4 * (lane / kQuadLanes) + (lane % 8) / 2;
+    auto k_byte = [&](int u) { return 16 * ((lane % S::kPieces) ^ S::k_swizzle((w + NW * u) * S::kGroupRows + k_row)); };
+    const int v_byte = 16 * (2 * ((lane % kQuadLanes) / 8) + lane % 2);
+    typedef const __attribute__((address_space(1))) void *GlobalPtr;
+    typedef __attribute__((address_space(3))) void *LdsPtr;
+    if ((step + 1) * kStepTokens <= nsub) {                      // uniform over the workgroup
+        const int first = step * kStepTokens + w * S::kGroupRows;                        // of the wave's first load
+        uint32_t row[S::kLoads];                                 // uniform over the wave
+#pragma unroll
+        for (int u = 0; u < S::kLoads; ++u) row[u] = rows.base + first + NW * S::kGroupRows * u;
+        if (rows.table) {
+#pragma unroll
+            for (int u = 0; u < S::kLoads; ++u) row[u] = rows.table[(first + NW * S::kGroupRows * u) / kGranule];
+#pragma unroll
+            for (int u = 0; u < S::kLoads; ++u)
+                row[u] = __builtin_amdgcn_readfirstlane(row[u]) + (first + NW * S::kGroupRows * u) % kGranule;
+        }
+#pragma unroll
+        for (int u = 0; u < S::kLoads; ++u) {
+            const size_t at = (size_t)row[u] * S::kRowBytes;
+            const uint32_t k_off = k_row * S::kRowBytes + k_byte(u), v_off = v_row * S::kRowBytes + v_byte;
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(kv.k + at + k_off), (LdsPtr)(k_stage + (w + NW * u) * 1024), 16, 0, POLICY_K);
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(kv.v + at + v_off), (LdsPtr)(v_stage + (w + NW * u) * 1024), 16, 0, POLICY_V);
+        }
+        return;
+    }
+    uint32_t kr[S::kLoads], vr[S::kLoads];
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) {
+        const int first = step * kStepTokens + (w + NW * u) * S::kGroupRows;
+        const uint32_t kt = min(first + k_row, nsub - 1), vt = min(first + v_row, nsub - 1);
+        kr[u] = rows.table ? rows.table[kt / kGranule] + kt % kGranule : rows.base + kt;
+        vr[u] = rows.table ? rows.table[vt / kGranule] + vt % kGranule : rows.base + vt;
+    }
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) {
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(kv.k + (size_t)kr[u] * S::kRowBytes + k_byte(u)),
+                                         (LdsPtr)(k_stage + (w + NW * u) * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(kv.v + (size_t)vr[u] * S::kRowBytes + v_byte),
+                                         (LdsPtr)(v_stage + (w + NW * u) * 1024), 16, 0, 0);
+    }
+}
+
+// One 16-byte slice of the score contraction in bf16: C[32 x 32] += A . B over 16 columns.  A lane holds 16 bytes of row
+// lane % 32 of either operand, the lower half of the wave one piece and the upper half the next.
+__device__ __forceinline__ floatx16 score_mfma(const uint4 &a, const uint4 &b, floatx16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
 }  // namespace
 
 }  // namespace hgca

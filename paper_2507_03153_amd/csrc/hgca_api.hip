@@ -257,7 +257,7 @@ struct TreeLayout {
 TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, int32_t cap)
 {
     TreeLayout t{};
-    const int64_t rows = (int64_t)n_q * group_of(s), per_block = 16 * tree_row_tiles((int)rows);
+    const int64_t rows = (int64_t)n_q * group_of(s), per_block = tree_block_rows(s->dtype, (int)rows);
     t.row_blocks = (int32_t)((rows + per_block - 1) / per_block);
     const int64_t units = std::max<int64_t>(1, (int64_t)s->batch * s->n_kv_heads * t.row_blocks);
     t.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HGCA_TARGET_WGS_TREE / units, ((int64_t)cap + 127) / 128));

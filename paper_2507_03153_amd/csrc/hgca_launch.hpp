@@ -311,9 +311,12 @@ struct TreeArgs {
     void *o;                   // [B, n_q, Hq, d]
     float *lse;                // [B, n_q, Hq]
 };
-// 16-row tiles of a wave for `rows` query rows per KV head
-int tree_row_tiles(int rows);
-// kv8: the tier is in 8 bits (dtype is that of q); row_blocks = blocks of 16 * tree_row_tiles() rows
+// rows of a workgroup, for `rows` query rows per KV head
+int tree_block_rows(int dtype, int rows);
+// kv8: the tier is in 8 bits (dtype is that of q); row_blocks = blocks of tree_block_rows() rows.  The splits, and their fold
+// where there are several.
 hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s);
+// the splits with 128 rows per workgroup (bf16 queries; called by launch_tree_attn)
+hipError_t launch_tree_rows(int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s);
 
 }  // namespace hgca

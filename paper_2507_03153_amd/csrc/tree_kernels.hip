@@ -1,4 +1,4 @@
-// Attention of a few queries per sequence over one tier: drafted tokens that are verified together, each of which sees the
+// Attention of a few queries per sequence over one tier (more than 32 rows in bf16: tree_rows_kernels.hip): drafted tokens that are verified together, each of which sees the
 // conversation and its own ancestors among the drafts (the tier's last n tokens, a bit per draft), and queries over an 8-bit
 // tier.  A row is one query of one head of the group that shares a KV head; a launch reads K and V once per 16 or 32 rows.
 //
@@ -17,22 +17,16 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "append_device.hpp"
-#include "kv8_device.hpp"
+#include "tree_device.hpp"
 
 namespace hgca {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kTreeWaves = 4, kTreeBlock = kTreeWaves * kWave;
 constexpr uint32_t kLowHalves = 0x05040100u, kHighHalves = 0x07060302u;          // byte selectors: (b.lo, a.lo) and (b.hi, a.hi)
 
 __device__ __forceinline__ floatx4 mfma16(const uint4 &a, const uint4 &b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{lo, hi}), bf16x2));
 }
 // max / sum over the four rows of 16 lanes
 __device__ __forceinline__ float rows_max(float x) {
@@ -41,18 +35,6 @@ __device__ __forceinline__ float rows_max(float x) {
     return fmaxf(h.a, h.b);
 }
 __device__ __forceinline__ float rows_sum(float x) { return strided_sum<16>(x); }
-
-// A sequence's tokens of one tier that a workgroup goes through: a split, cut by the sequence's own length.
-struct Span {
-    int len, begin, end;
-    __device__ __forceinline__ Span(const TreeArgs &a, int b, int split) {
-        len = tier_len(a.kv, b);
-        const int unit = 32 * kTreeWaves;                        // the waves take 32 tokens in turn
-        const int64_t per = (((int64_t)len + a.n_splits - 1) / a.n_splits + unit - 1) / unit * unit;
-        begin = (int)min(split * per, (int64_t)len);
-        end = (int)min(begin + per, (int64_t)len);
-    }
-};
 
 // 16 tokens of K or of V: what a lane (n = lane % 16, g = lane / 16) holds of them.  `row` is the tile's first row, uniform over
 // the wave, nv the number of tokens that exist (the others repeat the last one).
@@ -141,14 +123,6 @@ template <int D> struct VTile<kv8_t, D> {
         }
     }
 };
-
-// Which of the tokens base + {0..3, 16..19} a row sees, as bits {0..3, 16..19}: below `tail` all, from there the bits of
-// `mask`, nothing from `end` on.  base may lie up to 31 tokens before the tail.
-__device__ __forceinline__ uint32_t seen_bits(uint64_t mask, int base, int tail, int end) {
-    const int j = base - tail, left = end - base;
-    const uint64_t m = j >= 64 ? 0 : j >= 0 ? mask >> j : j > -32 ? mask << -j | ((1ull << -j) - 1) : ~0ull;
-    return left <= 0 ? 0u : left >= 32 ? (uint32_t)m : (uint32_t)m & ((1u << left) - 1u);
-}
 
 // Running softmax of RT row tiles over NT 16-token tiles per step.  The maximum is kept on raw scores (the scale is positive); a
 // weight is 2^fma(score, scale2, shift) with shift = -max * scale2 as rounded, and `shift` is what a partial result is relative to, so that
@@ -318,7 +292,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
     const Place at(a, 16 * RT);
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
     const int group = a.sh.group, rows = a.n_q * group;
-    const Span span(a, at.b, at.split);
+    const Span span(a, at.b, at.split, 32 * NW);
 
     uint4 q[RT][QP][KS];
     uint64_t mask[RT];
@@ -358,7 +332,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
 
     RowState<RT, E> st;
     st.clear();
-    const float scale2 = a.sh.sm_scale * kLog2e;
+    const float scale2 = a.sh.sm_scale * kTreeLog2e;
     const int tail = kDrafts && a.mask ? span.len - a.n_q : span.len;      // first drafted token
 
     KTile<S, D> kt[2];
@@ -387,7 +361,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
         if constexpr (MASKED) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                seen[r] = seen_bits(mask[r], tok + 4 * g, tail, span.end);
+                seen[r] = (uint32_t)seen_tokens(mask[r], tok + 4 * g, tail, span.end);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -436,11 +410,10 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
                     for (int i = 0; i < W; ++i) {
                         uint32_t &x = v[t][j][i];
                         x = gone ? 0 : x;
-                        // the sum carries into the sign bit of either half where its exponent is all ones
-                        odd |= (x & 0x7fff7fffu) + 0x00800080u;
+                        odd |= odd_carry(x);
                     }
                 }
-            if (kDrafts && a.mask && __any((odd & 0x80008000u) != 0)) {
+            if (kDrafts && a.mask && __any((odd & kSigns) != 0)) {
                 // counts of +inf, -inf and NaN that a row sees in a column, as products of ones
                 uint4 ones[RT];
 #pragma unroll
@@ -455,13 +428,8 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
                 }
 #pragma unroll 1
                 for (int kind = 0; kind < 3; ++kind) {
-                    const uint32_t keep = kind == 2 ? 0x7fffu : 0xffffu, from = kind == 0 ? 0x7f80u : kind == 1 ? 0xff80u : 0x7f81u,
-                                   more = kind == 2 ? 0x7eu : 0u;
-                    auto flag = [&](int t, int j, int i) {
-                        const uint32_t lo = v[t][j][i] & keep, hi = v[t][j][i] >> 16 & keep;
-                        return (lo - from <= more ? 0x3f80u : 0u) | (hi - from <= more ? 0x3f800000u : 0u);
-                    };
-                    const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                    const OddKind k(kind);
+                    auto flag = [&](int t, int j, int i) { return k.ones(v[t][j][i]); };
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
                         const uint4 op = pairs(e, flag);
@@ -469,7 +437,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
                         for (int r = 0; r < RT; ++r) {
                             const floatx4 c = mfma16(op, ones[r], floatx4{});
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) st.o[r][e][i] += c[i] > 0.f ? add : 0.f;
+                            for (int i = 0; i < 4; ++i) st.o[r][e][i] += c[i] > 0.f ? k.add : 0.f;
                         }
                         __builtin_amdgcn_sched_barrier(0);       // one column at a time: few registers
                     }
@@ -479,10 +447,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int i = 0; i < W; ++i) {
-                            const uint32_t x = v[t][j][i], bad = ((x & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-                            v[t][j][i] = x & ~(bad | (bad - (bad >> 15)));
-                        }
+                        for (int i = 0; i < W; ++i) v[t][j][i] &= ~odd_halves(v[t][j][i]);
             }
         }
 #pragma unroll
@@ -535,7 +500,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
     const Place at(a, 16 * RT);
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
     const int group = a.sh.group, rows = a.n_q * group;
-    const Span span(a, at.b, at.split);
+    const Span span(a, at.b, at.split, 32 * NW);
 
     float q[RT][U][4];
     uint64_t mask[RT];
@@ -550,7 +515,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
     }
     RowState<RT, E> st;
     st.clear();
-    const float scale2 = a.sh.sm_scale * kLog2e;
+    const float scale2 = a.sh.sm_scale * kTreeLog2e;
     const int tail = a.mask ? span.len - a.n_q : span.len;
 
     float kr[U][4], vr[4][E];
@@ -575,7 +540,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
         if constexpr (MASKED) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                seen[r] = seen_bits(mask[r], tok + 4 * g, tail, span.end);
+                seen[r] = (uint32_t)seen_tokens(mask[r], tok + 4 * g, tail, span.end);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (!(seen[r] >> i & 1u)) s[r][0][i] = -INFINITY;
@@ -725,18 +690,21 @@ void launch_rows(const TreeArgs &a, dim3 grid, hipStream_t s)
 
 }  // namespace
 
-int tree_row_tiles(int rows) { return rows <= 16 ? 1 : 2; }
+int tree_block_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= 32 || dtype == 0 ? 32 : kRowsPerBlock; }
 
 hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s)
 {
-    const int rt = tree_row_tiles(a.n_q * a.sh.group);
+    const int block_rows = tree_block_rows(dtype, a.n_q * a.sh.group), rt = block_rows / 16;
     const dim3 grid((unsigned)(a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads, (unsigned)batch);
 #define HGCA_TREE_RT(S, TQ, D)                                  \
     do {                                                        \
         if (rt == 1) launch_rows<S, TQ, D, 1>(a, grid, s);      \
         else launch_rows<S, TQ, D, 2>(a, grid, s);              \
     } while (0)
-    if (kv8) {
+    if (block_rows == kRowsPerBlock) {
+        const hipError_t rc = launch_tree_rows(head_dim, kv8, a, batch, s);
+        if (rc != hipSuccess) return rc;
+    } else if (kv8) {
         if (dtype == 1 && head_dim == 64) HGCA_TREE_RT(kv8_t, bf16_t, 64);
         else if (dtype == 1) HGCA_TREE_RT(kv8_t, bf16_t, 128);
         else if (head_dim == 64) HGCA_TREE_RT(kv8_t, float, 64);
