@@ -244,27 +244,36 @@ int from_hip(hipError_t e) { return e == hipSuccess ? HGCA_OK : HGCA_ERR_DEVICE;
 constexpr int32_t kMaxRowsCap = 1 << 30;         // positions and step counts of these calls stay clear of 2^31
 constexpr int32_t kMaxKv8Queries = 4096;
 
-// Splits of a (sequence, KV head, block of rows) whose tier holds up to `cap` tokens: about 1024 workgroups, two rounds of the two
-// that a compute unit holds, of 128 tokens at least (a step of each of a workgroup's four waves).
+// Splits per (sequence, KV head, block of rows) whose tier holds up to `cap` tokens, on average over the sequences (Span): about
+// 512 workgroups, a round of the two that a compute unit holds, of 256 tokens at least; a tier of up to 512 tokens is not split,
+// which saves the fold's launch.
 #ifndef HGCA_TARGET_WGS_TREE
-#define HGCA_TARGET_WGS_TREE 1024
+#define HGCA_TARGET_WGS_TREE 512
+#endif
+#ifndef HGCA_TREE_MIN
+#define HGCA_TREE_MIN 256
+#endif
+#ifndef HGCA_TREE_WHOLE
+#define HGCA_TREE_WHOLE 512
 #endif
 struct TreeLayout {
     int32_t row_blocks, n_splits;
-    size_t part_o, part_m, part_l, total;
+    size_t part_o, part_m, part_l, seq_slots, total;
 };
 
-TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, int32_t cap)
+TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, bool kv8, int32_t cap)
 {
     TreeLayout t{};
-    const int64_t rows = (int64_t)n_q * group_of(s), per_block = tree_block_rows(s->dtype, (int)rows);
+    const int64_t rows = (int64_t)n_q * group_of(s), per_block = tree_block_rows(s->dtype, kv8, (int)rows);
     t.row_blocks = (int32_t)((rows + per_block - 1) / per_block);
     const int64_t units = std::max<int64_t>(1, (int64_t)s->batch * s->n_kv_heads * t.row_blocks);
-    t.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HGCA_TARGET_WGS_TREE / units, ((int64_t)cap + 127) / 128));
+    const int64_t most = cap <= HGCA_TREE_WHOLE ? 1 : ((int64_t)cap + HGCA_TREE_MIN - 1) / HGCA_TREE_MIN;
+    t.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HGCA_TARGET_WGS_TREE / units, most));
     const size_t parts = t.n_splits > 1 ? (size_t)s->batch * n_q * s->n_q_heads * t.n_splits : 0;
     t.part_m = align_up(parts * s->head_dim * sizeof(float));
     t.part_l = t.part_m + align_up(parts * sizeof(float));
-    t.total = std::max(t.part_l + align_up(parts * sizeof(float)), kAlign);
+    t.seq_slots = t.part_l + align_up(parts * sizeof(float));
+    t.total = t.seq_slots + (t.n_splits > 1 ? align_up(2 * (size_t)s->batch * sizeof(int32_t)) : kAlign);
     return t;
 }
 
@@ -284,7 +293,9 @@ int check_rows_call(const hgca_shape *s, const void *q, int32_t n_q, int32_t mos
 int rows_attention(const hgca_shape *s, const void *q, int32_t n_q, bool kv8, TreeArgs &a, void *o, int32_t o_dtype, float *lse,
                    void *ws, size_t ws_bytes, void *stream)
 {
-    const TreeLayout t = tree_layout(s, n_q, a.kv.cap);
+    const TreeLayout t = tree_layout(s, n_q, kv8, a.kv.cap);
+    // sequences and blocks of rows are one dimension of the grid, whose threads are counted in 32 bits
+    if ((int64_t)s->batch * t.n_splits * t.row_blocks > int64_t(1) << 23) return HGCA_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < t.total || !aligned16(ws)) return HGCA_ERR_WORKSPACE;
     char *base = static_cast<char *>(ws);
     a.sh = to_dev(s);
@@ -296,6 +307,7 @@ int rows_attention(const hgca_shape *s, const void *q, int32_t n_q, bool kv8, Tr
     a.part_o = reinterpret_cast<float *>(base + t.part_o);
     a.part_m = reinterpret_cast<float *>(base + t.part_m);
     a.part_l = reinterpret_cast<float *>(base + t.part_l);
+    a.seq_slots = reinterpret_cast<int32_t *>(base + t.seq_slots);
     a.o = o;
     a.lse = lse;
     return from_hip(launch_tree_attn(s->dtype, s->head_dim, kv8, a, s->batch, static_cast<hipStream_t>(stream)));
@@ -1528,7 +1540,7 @@ int hgca_qk_norm_rope(const hgca_shape *shape, const void *q_in, int64_t q_token
 size_t hgca_tree_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens)
 {
     if (check_shape(shape) != HGCA_OK || n_q < 1 || n_q > HGCA_MAX_DRAFTS || max_tokens < 0) return 0;
-    return tree_layout(shape, n_q, max_tokens).total;
+    return tree_layout(shape, n_q, false, max_tokens).total;
 }
 
 int hgca_tree_attn(const hgca_shape *shape, const void *q, int32_t n_q, const hgca_kv_view *tier, const uint64_t *draft_mask,
@@ -1637,7 +1649,7 @@ int hgca_kv8_read(const hgca_shape *shape, const hgca_kv8_view *kv8, const int32
 size_t hgca_kv8_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens)
 {
     if (check_shape(shape) != HGCA_OK || n_q < 1 || n_q > kMaxKv8Queries || max_tokens < 0) return 0;
-    return tree_layout(shape, n_q, max_tokens).total;
+    return tree_layout(shape, n_q, true, max_tokens).total;
 }
 
 int hgca_kv8_attn(const hgca_shape *shape, const void *q, int32_t n_q, const hgca_kv8_view *kv8, void *o_out, int32_t o_dtype,

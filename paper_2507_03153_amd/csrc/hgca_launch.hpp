@@ -307,12 +307,14 @@ struct TreeArgs {
     const char *k_scale, *v_scale;        // 8-bit tiers
     const uint64_t *mask;      // [B, n_q] or null: bit j = the query sees the j-th of the tier's last n_q tokens
     int32_t n_q, n_splits, row_blocks, o_bf16;
-    float *part_o, *part_m, *part_l;      // [rows, n_splits, d], [rows, n_splits]; m in units of ln 2
+    // n_splits > 1: partials of batch * n_splits slots (m in units of ln 2), and each sequence's first slot and number of slots
+    float *part_o, *part_m, *part_l;      // [slots, Hkv, rows of a KV head (, d)]
+    int32_t *seq_slots;                   // [B, 2]
     void *o;                   // [B, n_q, Hq, d]
     float *lse;                // [B, n_q, Hq]
 };
 // rows of a workgroup, for `rows` query rows per KV head
-int tree_block_rows(int dtype, int rows);
+int tree_block_rows(int dtype, bool kv8, int rows);
 // kv8: the tier is in 8 bits (dtype is that of q); row_blocks = blocks of tree_block_rows() rows.  The splits, and their fold
 // where there are several.
 hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s);

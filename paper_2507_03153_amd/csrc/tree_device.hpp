@@ -16,17 +16,75 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{lo, hi}), bf16x2));
 }
 
-// A sequence's tokens of one tier that a workgroup goes through: a split, cut by the sequence's own length in whole steps of the
-// workgroup.
+// The part of a sequence's tokens that a workgroup goes through.  With one split per sequence it is the whole; else the launch has
+// batch * n_splits slots per KV head and block of rows.  Up to 64 sequences take as many of them as their own lengths ask for:
+// slots of C whole steps, C about the least with which all sequences' slots are enough.  (With n_splits slots for every
+// sequence the longest one sets the time.)  Every wave works the cut out for itself, a lane per sequence; a
+// sequence without tokens takes a slot too.  More sequences fill the device with a few slots each: n_splits equal ones.
 struct Span {
-    int len, begin, end;
-    __device__ __forceinline__ Span(const TreeArgs &a, int b, int split, int unit) {
-        len = tier_len(a.kv, b);
-        const int64_t per = (((int64_t)len + a.n_splits - 1) / a.n_splits + unit - 1) / unit * unit;
-        begin = (int)min(split * per, (int64_t)len);
-        end = (int)min(begin + per, (int64_t)len);
+    int b, len, begin, end;
+    int slot, first_slot, n_slots;               // first_slot, n_slots: the sequence's
+    bool idle;                                   // no sequence needs the slot
+    __device__ __forceinline__ Span(const TreeArgs &a, int slot_of_launch, int unit) {
+        slot = slot_of_launch;
+        idle = false;
+        const int B = a.sh.batch;
+        int64_t per;
+        if (a.n_splits == 1 || B > kWave) {
+            b = slot / a.n_splits;
+            n_slots = a.n_splits;
+            first_slot = b * n_slots;
+            len = tier_len(a.kv, b);
+            per = (((int64_t)len + n_slots - 1) / n_slots + unit - 1) / unit * unit;
+        } else {
+            const int lane = threadIdx.x % kWave, slots = B * a.n_splits;
+            const int tokens = lane < B ? tier_len(a.kv, lane) : 0, steps = lane < B ? max((tokens + unit - 1) / unit, 1) : 0;
+            auto counts = [&](int c) {           // ceil(steps / c): the quotient in fp32 is off by one at most, downwards
+                const int n = (int)((float)steps * __builtin_amdgcn_rcpf((float)c) * 0.999999f);
+                return n + (n * c < steps ? 1 : 0);
+            };
+            auto enough = [&](int c) { return wave_sum((float)min(counts(c), slots + 1)) <= (float)slots; };     // whole numbers below 2^24
+            // total / slots steps may do; total / (slots - B), rounded up generously, always does
+            const float total = wave_sum((float)steps);
+            int c = max((int)(total / (float)slots), 1), least = c;
+            if (!enough(c)) {
+                c = (int)(total / (float)(slots - B) * 1.0001f) + 2;
+#pragma unroll 1
+                while (c - least > max(least / 32, 1)) {
+                    const int mid = least + (c - least) / 2;
+                    if (enough(mid)) c = mid; else least = mid;
+                }
+            }
+            const int n = counts(c), upto = (int)wave_inclusive_scan((uint32_t)n);
+            const uint64_t behind = __ballot(upto > slot);
+            b = 0;
+            if (behind == 0) {
+                idle = true;
+                return;
+            }
+            b = __builtin_ctzll(behind);
+            n_slots = __builtin_amdgcn_readlane(n, b);
+            first_slot = __builtin_amdgcn_readlane(upto, b) - n_slots;
+            len = __builtin_amdgcn_readlane(tokens, b);
+            per = (int64_t)__builtin_amdgcn_readfirstlane(c) * unit;
+        }
+        const int64_t at = (slot - first_slot) * per;
+        begin = (int)min(at, (int64_t)len);
+        end = (int)min(at + per, (int64_t)len);
+    }
+    // what the fold has to know of the sequence
+    __device__ __forceinline__ void tell(const TreeArgs &a) const {
+        if (a.n_splits > 1 && slot == first_slot && threadIdx.x == 0) {
+            a.seq_slots[2 * b] = first_slot;
+            a.seq_slots[2 * b + 1] = n_slots;
+        }
     }
 };
+
+// Where a row's partial of a slot lies: the rows of a KV head of a slot are consecutive.
+__device__ __forceinline__ int64_t partial_row(const TreeArgs &a, int slot, int kvh, int row) {
+    return ((int64_t)slot * a.sh.n_kv_heads + kvh) * (a.n_q * a.sh.group) + row;
+}
 
 // Which of the 64 tokens from `base` on a row sees: below `tail` all, from there the bits of `mask`, nothing from `end` on.
 __device__ __forceinline__ uint64_t seen_tokens(uint64_t mask, int base, int tail, int end) {

@@ -41,13 +41,20 @@ __device__ __forceinline__ float rows_sum(float x) { return strided_sum<16>(x); 
 template <typename S, int D> struct KTile;
 template <typename S, int D> struct VTile;
 
+// STREAM: rows that pass once and are more than the last cache holds leave the caches alone
+template <bool STREAM> __device__ __forceinline__ uint4 row16(const char *p) { return STREAM ? load16_stream(p) : load16(p); }
+template <bool STREAM> __device__ __forceinline__ uint2 row8(const char *p) {
+    const uint32_t *w = reinterpret_cast<const uint32_t *>(p);
+    return STREAM ? make_uint2(__builtin_nontemporal_load(w), __builtin_nontemporal_load(w + 1)) : *reinterpret_cast<const uint2 *>(p);
+}
+
 template <int D> struct KTile<bf16_t, D> {
     uint4 k[D / 32];
     static __device__ __forceinline__ int column(int s, int g) { return 32 * s + 8 * g; }       // of slice s of the contraction
-    __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
+    template <bool STREAM> __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
         const char *p = a.kv.k + (size_t)row * (2 * D) + (uint32_t)(min(n, nv - 1) * (2 * D) + 16 * g);
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) k[s] = load16(p + 64 * s);
+        for (int s = 0; s < D / 32; ++s) k[s] = row16<STREAM>(p + 64 * s);
     }
     __device__ __forceinline__ void prepare(int) {}
     __device__ __forceinline__ uint4 operand(int s) const { return k[s]; }
@@ -56,13 +63,13 @@ template <int D> struct KTile<bf16_t, D> {
 template <int D> struct VTile<bf16_t, D> {
     static constexpr int E = D / 16;
     uint32_t v[4][E / 2];
-    __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
+    template <bool STREAM> __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
         const char *vp = a.kv.v + (size_t)row * (2 * D);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const char *p = vp + (uint32_t)(min(4 * g + j, nv - 1) * (2 * D) + n * 2 * E);
-            if constexpr (D == 128) *reinterpret_cast<uint4 *>(v[j]) = load16(p);
-            else *reinterpret_cast<uint2 *>(v[j]) = *reinterpret_cast<const uint2 *>(p);
+            if constexpr (D == 128) *reinterpret_cast<uint4 *>(v[j]) = row16<STREAM>(p);
+            else *reinterpret_cast<uint2 *>(v[j]) = row8<STREAM>(p);
         }
     }
     __device__ __forceinline__ void words(uint32_t (&w)[4][E / 2], int) const {
@@ -78,11 +85,11 @@ template <int D> struct KTile<kv8_t, D> {
     uint32_t scales;
     float f[D / 64];
     static __device__ __forceinline__ int column(int s, int g) { return 64 * (s / 2) + 16 * g + 8 * (s % 2); }
-    __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
+    template <bool STREAM> __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
         const uint32_t r = min(n, nv - 1);
         const char *p = a.kv.k + (size_t)row * D + (r * D + 16 * g);
 #pragma unroll
-        for (int s = 0; s < D / 64; ++s) k[s] = load16(p + 64 * s);
+        for (int s = 0; s < D / 64; ++s) k[s] = row16<STREAM>(p + 64 * s);
         scales = (reinterpret_cast<const typename Kv8Scales<D>::Word *>(a.k_scale) + row)[r];
     }
     __device__ __forceinline__ void prepare(int lane) {          // a lane's 16 columns lie in one block of 32
@@ -99,14 +106,14 @@ template <int D> struct KTile<kv8_t, D> {
 template <int D> struct VTile<kv8_t, D> {
     static constexpr int E = D / 16;
     uint32_t v[4][E / 4], scales[4];
-    __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
+    template <bool STREAM> __device__ __forceinline__ void load(const TreeArgs &a, uint32_t row, int nv, int n, int g) {
         const char *vp = a.kv.v + (size_t)row * D;
         const auto *sp = reinterpret_cast<const typename Kv8Scales<D>::Word *>(a.v_scale) + row;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t r = min(4 * g + j, nv - 1);
             const char *p = vp + r * D + n * E;
-            if constexpr (D == 128) *reinterpret_cast<uint2 *>(v[j]) = *reinterpret_cast<const uint2 *>(p);
+            if constexpr (D == 128) *reinterpret_cast<uint2 *>(v[j]) = row8<STREAM>(p);
             else v[j][0] = *reinterpret_cast<const uint32_t *>(p);
             scales[j] = sp[r];
         }
@@ -201,11 +208,11 @@ template <int D, bool OUT_BF16> __device__ __forceinline__ void store_eight(void
 
 template <int D, int RT>
 __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeArgs &a, RowState<RT, D / 16> &st, int b, int kvh,
-                                            int row0, int split)
+                                            int row0, int slot)
 {
     constexpr int E = D / 16;
     const int tid = threadIdx.x, w = tid / kWave, lane = tid % kWave, n = lane % 16, g = lane / 16;
-    const int group = a.sh.group, rows = a.n_q * group;
+    const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const float l = rows_sum(st.l[r]);
@@ -249,9 +256,9 @@ __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeAr
                 x[e + 3] = fmaf(o.w, f[i], x[e + 3]);
             }
         }
-        const int64_t out_row = ((int64_t)b * a.n_q + at_row / group) * a.sh.n_q_heads + kvh * group + at_row % group;
+        const int64_t out_row = ((int64_t)b * a.n_q + (at_row >> lg)) * a.sh.n_q_heads + kvh * group + (at_row & (group - 1));
         if (a.n_splits > 1) {
-            const int64_t at = out_row * a.n_splits + split;
+            const int64_t at = partial_row(a, slot, kvh, at_row);
             store_eight<D, false>(a.part_o, at * D + c * E, x);
             if (c == 0) {
                 a.part_m[at] = M;
@@ -268,40 +275,31 @@ __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeAr
     }
 }
 
-// Block of the launch: splits of one (sequence, KV head), row blocks fastest so that those that share rows run side by side.
-struct Place {
-    int b, kvh, split, row0;
-    __device__ __forceinline__ Place(const TreeArgs &a, int rows_per_block) {
-        kvh = blockIdx.y;
-        b = blockIdx.z;
-        split = blockIdx.x / a.row_blocks;
-        row0 = (int)(blockIdx.x % a.row_blocks) * rows_per_block;
-    }
-};
-
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
 // TQ: bf16_t, or float for fp32 queries over an 8-bit tier, which enter as three bf16 parts that add up to them.  PP: parts of a weight.
-template <typename S, typename TQ, int D, int RT, int PP>
+template <typename S, typename TQ, int D, int RT, int PP, bool STREAM>
 __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
 {
     constexpr int KS = D / 32, E = D / 16, W = E / 2, QP = sizeof(TQ) == 4 ? 3 : 1, NW = kTreeWaves;
     constexpr bool kDrafts = sizeof(S) > 1;      // 8-bit tiers hold no drafted tokens
     __shared__ uint32_t s_row[kSub];
     __shared__ MergeShared<D, RT> s_merge;
-    const Place at(a, 16 * RT);
+    const int kvh = blockIdx.y, row0 = (int)(blockIdx.x % a.row_blocks) * 16 * RT;          // row blocks of a slot run side by side
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
-    const int group = a.sh.group, rows = a.n_q * group;
-    const Span span(a, at.b, at.split, 32 * NW);
+    const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
+    const Span span(a, blockIdx.x / a.row_blocks, 32 * NW);
+    if (span.idle) return;                       // uniform over the workgroup
+    if (kvh == 0 && row0 == 0) span.tell(a);
 
     uint4 q[RT][QP][KS];
     uint64_t mask[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = min(at.row0 + 16 * r + n, rows - 1);     // lanes without a row repeat the last one and store nothing
-        const int64_t qr = (int64_t)at.b * a.n_q + row / group;
+        const int row = min(row0 + 16 * r + n, rows - 1);     // lanes without a row repeat the last one and store nothing
+        const int64_t qr = (int64_t)span.b * a.n_q + (row >> lg);
         mask[r] = kDrafts && a.mask ? a.mask[qr] : ~0ull;
-        const char *p = static_cast<const char *>(a.q) + (qr * a.sh.n_q_heads + at.kvh * group + row % group) * D * (int)sizeof(TQ);
+        const char *p = static_cast<const char *>(a.q) + (qr * a.sh.n_q_heads + kvh * group + (row & (group - 1))) * D * (int)sizeof(TQ);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const char *c = p + KTile<S, D>::column(s, g) * (int)sizeof(TQ);
@@ -338,9 +336,9 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
     KTile<S, D> kt[2];
     VTile<S, D> vt[2];
     // One step: the scores of 32 tokens from kt, their weights, the outputs from vt.  next_k() and next_v() request the next step's
-    // rows into the registers as soon as these have been read.  MASKED: the step meets the end of the tokens or drafted ones.
-    auto consume = [&](auto masked, int tok, auto next_k, auto next_v) {
-        constexpr bool MASKED = decltype(masked)::value;
+    // rows into the registers as soon as these have been read.
+    auto consume = [&](int tok, auto next_k, auto next_v) {
+        const bool masked = tok + 32 > min(tail, span.end);      // the step meets the end of the tokens or drafted ones; uniform
         kt[0].prepare(lane);
         kt[1].prepare(lane);
         floatx4 s[RT][2];
@@ -358,7 +356,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
             }
         next_k();
         uint32_t seen[RT];
-        if constexpr (MASKED) {
+        if (masked) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 seen[r] = (uint32_t)seen_tokens(mask[r], tok + 4 * g, tail, span.end);
@@ -397,7 +395,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
                               __builtin_amdgcn_perm(word(1, 1, e / 2), word(1, 0, e / 2), sel),
                               __builtin_amdgcn_perm(word(1, 3, e / 2), word(1, 2, e / 2), sel));
         };
-        if constexpr (MASKED) {
+        if (masked) {
             // a weight of 0 keeps a row out of the product only if the row is finite: rows behind the end become 0, and
             // infinities and NaN of drafted rows are taken out and added for the queries that see them
             uint32_t odd = 0;
@@ -466,27 +464,24 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
     for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
         const int nsub = min(sub_len, total - sub0), first = span.begin + sub0;
         __syncthreads();                         // the table of the pass before is no longer in use
-        const BlockRows where = make_block_rows<kTreeBlock>(s_row, a.kv, a.sh.n_kv_heads, at.b, at.kvh, first, nsub);
+        const BlockRows where = make_block_rows<kTreeBlock>(s_row, a.kv, a.sh.n_kv_heads, span.b, kvh, first, nsub);
         auto fetch = [&](auto &tile, int tok) {                  // tok: in the pass; nothing behind its end
             if (tok >= nsub) return;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int gr = min(tok / 16 + t, (nsub - 1) / 16);
                 const uint32_t row = where.table ? where.table[gr] : where.base + 16 * gr;
-                tile[t].load(a, __builtin_amdgcn_readfirstlane(row), min(16, nsub - 16 * gr), n, g);
+                tile[t].template load<STREAM>(a, __builtin_amdgcn_readfirstlane(row), min(16, nsub - 16 * gr), n, g);
             }
         };
         constexpr int kStep = 32 * NW;
-        const int plain = min(tail, span.end) - first;           // steps that end at or before it need no mask
         int tok = 32 * w;
         fetch(kt, tok);
         fetch(vt, tok);
-        for (; tok < nsub && tok + 32 <= plain; tok += kStep)
-            consume(std::false_type{}, first + tok, [&] { fetch(kt, tok + kStep); }, [&] { fetch(vt, tok + kStep); });
         for (; tok < nsub; tok += kStep)
-            consume(std::true_type{}, first + tok, [&] { fetch(kt, tok + kStep); }, [&] { fetch(vt, tok + kStep); });
+            consume(first + tok, [&] { fetch(kt, tok + kStep); }, [&] { fetch(vt, tok + kStep); });
     }
-    merge_waves<D, RT>(s_merge, a, st, at.b, at.kvh, at.row0, at.split);
+    merge_waves<D, RT>(s_merge, a, st, span.b, kvh, row0, span.slot);
 }
 
 // The same over fp32 rows, on the fp32 matrix instructions (products and sums in fp32, nothing rounded in between): 16 tokens at a time.  A
@@ -497,19 +492,21 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
     constexpr int E = D / 16, U = D / 16, NW = kTreeWaves, RB = 4 * D;
     __shared__ uint32_t s_row[kSub];
     __shared__ MergeShared<D, RT> s_merge;
-    const Place at(a, 16 * RT);
+    const int kvh = blockIdx.y, row0 = (int)(blockIdx.x % a.row_blocks) * 16 * RT;          // row blocks of a slot run side by side
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
-    const int group = a.sh.group, rows = a.n_q * group;
-    const Span span(a, at.b, at.split, 32 * NW);
+    const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
+    const Span span(a, blockIdx.x / a.row_blocks, 32 * NW);
+    if (span.idle) return;                       // uniform over the workgroup
+    if (kvh == 0 && row0 == 0) span.tell(a);
 
     float q[RT][U][4];
     uint64_t mask[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = min(at.row0 + 16 * r + n, rows - 1);
-        const int64_t qr = (int64_t)at.b * a.n_q + row / group;
+        const int row = min(row0 + 16 * r + n, rows - 1);
+        const int64_t qr = (int64_t)span.b * a.n_q + (row >> lg);
         mask[r] = a.mask ? a.mask[qr] : ~0ull;
-        const char *p = static_cast<const char *>(a.q) + (qr * a.sh.n_q_heads + at.kvh * group + row % group) * RB + 16 * g;
+        const char *p = static_cast<const char *>(a.q) + (qr * a.sh.n_q_heads + kvh * group + (row & (group - 1))) * RB + 16 * g;
 #pragma unroll
         for (int u = 0; u < U; ++u) Elem<float>::expand(load16(p + 64 * u), q[r][u]);
     }
@@ -519,8 +516,8 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
     const int tail = a.mask ? span.len - a.n_q : span.len;
 
     float kr[U][4], vr[4][E];
-    auto consume = [&](auto masked, int tok, auto next_k, auto next_v) {
-        constexpr bool MASKED = decltype(masked)::value;
+    auto consume = [&](int tok, auto next_k, auto next_v) {
+        const bool masked = tok + 16 > min(tail, span.end);
         floatx4 s[RT][1], s2[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) s[r][0] = s2[r] = floatx4{};
@@ -537,7 +534,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
 #pragma unroll
         for (int r = 0; r < RT; ++r) s[r][0] += s2[r];
         uint32_t seen[RT];
-        if constexpr (MASKED) {
+        if (masked) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 seen[r] = (uint32_t)seen_tokens(mask[r], tok + 4 * g, tail, span.end);
@@ -547,7 +544,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
             }
         }
         st.weigh(s, scale2);
-        if constexpr (MASKED) {                  // as above
+        if (masked) {                            // as above
             uint32_t odd = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -600,7 +597,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
     for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
         const int nsub = min(sub_len, total - sub0), first = span.begin + sub0;
         __syncthreads();
-        const BlockRows where = make_block_rows<kTreeBlock>(s_row, a.kv, a.sh.n_kv_heads, at.b, at.kvh, first, nsub);
+        const BlockRows where = make_block_rows<kTreeBlock>(s_row, a.kv, a.sh.n_kv_heads, span.b, kvh, first, nsub);
         auto first_row = [&](int tok) {
             return (uint32_t)__builtin_amdgcn_readfirstlane(where.table ? where.table[tok / 16] : where.base + tok);
         };
@@ -621,16 +618,13 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
                     Elem<float>::expand(load16(vp + (uint32_t)(min(4 * g + j, last) * RB + n * 4 * E + 4 * e)), vr[j] + e);
         };
         constexpr int kStep = 16 * NW;
-        const int plain = min(tail, span.end) - first;
         int tok = 16 * w;
         fetch_k(tok);
         fetch_v(tok);
-        for (; tok < nsub && tok + 16 <= plain; tok += kStep)
-            consume(std::false_type{}, first + tok, [&] { fetch_k(tok + kStep); }, [&] { fetch_v(tok + kStep); });
         for (; tok < nsub; tok += kStep)
-            consume(std::true_type{}, first + tok, [&] { fetch_k(tok + kStep); }, [&] { fetch_v(tok + kStep); });
+            consume(first + tok, [&] { fetch_k(tok + kStep); }, [&] { fetch_v(tok + kStep); });
     }
-    merge_waves<D, RT>(s_merge, a, st, at.b, at.kvh, at.row0, at.split);
+    merge_waves<D, RT>(s_merge, a, st, span.b, kvh, row0, span.slot);
 }
 
 // The splits of a row: M = max m_s, O = sum o_s 2^{m_s - M} / sum l_s 2^{m_s - M}.  A wave per row; 16 or 32 lanes across the columns,
@@ -638,12 +632,16 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
 template <int D> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(TreeArgs a, int64_t rows)
 {
     constexpr int C4 = D / 4, SG = kWave / C4, PRE = 4;
-    const int lane = threadIdx.x % kWave, sg = lane / C4, c4 = lane % C4, S = a.n_splits;
-    const int64_t row = (int64_t)blockIdx.x * kTreeWaves + threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, sg = lane / C4, c4 = lane % C4;
+    const int64_t row = (int64_t)blockIdx.x * kTreeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     if (row >= rows) return;
-    const float *m = a.part_m + row * S, *l = a.part_l + row * S, *o = a.part_o + row * S * D + 4 * c4;
+    const int h = (int)(row % a.sh.n_q_heads), i = (int)(row / a.sh.n_q_heads % a.n_q), b = (int)(row / a.sh.n_q_heads / a.n_q);
+    const int first = a.seq_slots[2 * b], S = a.seq_slots[2 * b + 1];
+    const int64_t at = partial_row(a, first, h / a.sh.group, i * a.sh.group + h % a.sh.group);
+    const int64_t stride = partial_row(a, 1, 0, 0);
+    const float *m = a.part_m + at, *l = a.part_l + at, *o = a.part_o + at * D + 4 * c4;
     float M = -INFINITY;
-    for (int s = lane; s < S; s += kWave) M = fmaxf(M, m[s]);
+    for (int s = lane; s < S; s += kWave) M = fmaxf(M, m[s * stride]);
     M = wave_max(M);
     float L = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -652,10 +650,10 @@ template <int D> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(
         float4 po[PRE];
 #pragma unroll
         for (int i = 0; i < PRE; ++i) {
-            const int s = min(s0 + i * SG, S - 1);
+            const int64_t s = min(s0 + i * SG, S - 1) * stride;
             pm[i] = m[s];
             pl[i] = l[s];
-            po[i] = *reinterpret_cast<const float4 *>(o + (int64_t)s * D);
+            po[i] = *reinterpret_cast<const float4 *>(o + s * D);
         }
 #pragma unroll
         for (int i = 0; i < PRE; ++i) {
@@ -682,36 +680,49 @@ template <int D> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(
 }
 
 template <typename S, typename TQ, int D, int RT>
-void launch_rows(const TreeArgs &a, dim3 grid, hipStream_t s)
+void launch_rows(const TreeArgs &a, dim3 grid, int batch, hipStream_t s)
 {
-    if (a.o_bf16) hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 2>), grid, dim3(kTreeBlock), 0, s, a);
-    else hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 3>), grid, dim3(kTreeBlock), 0, s, a);
+    const dim3 block(kTreeBlock);
+    if constexpr (sizeof(TQ) == 2) {
+        // (fp32 queries take their rows in blocks of 16, which read K and V again)
+        if (a.row_blocks == 1 && (int64_t)batch * a.sh.n_kv_heads * a.kv.cap * D * (int)sizeof(S) * 2 >= kLastCache) {
+            if (a.o_bf16) hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 2, true>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 3, true>), grid, block, 0, s, a);
+            return;
+        }
+    }
+    if (a.o_bf16) hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 2, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 3, false>), grid, block, 0, s, a);
 }
 
 }  // namespace
 
-int tree_block_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= 32 || dtype == 0 ? 32 : kRowsPerBlock; }
+int tree_block_rows(int dtype, bool kv8, int rows)
+{
+    if (rows <= 16 || (dtype == 0 && kv8)) return 16;
+    return rows <= 32 || dtype == 0 ? 32 : kRowsPerBlock;
+}
 
 hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s)
 {
-    const int block_rows = tree_block_rows(dtype, a.n_q * a.sh.group), rt = block_rows / 16;
-    const dim3 grid((unsigned)(a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads, (unsigned)batch);
-#define HGCA_TREE_RT(S, TQ, D)                                  \
-    do {                                                        \
-        if (rt == 1) launch_rows<S, TQ, D, 1>(a, grid, s);      \
-        else launch_rows<S, TQ, D, 2>(a, grid, s);              \
+    const int block_rows = tree_block_rows(dtype, kv8, a.n_q * a.sh.group), rt = block_rows / 16;
+    const dim3 grid((unsigned)((int64_t)batch * a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads);
+#define HGCA_TREE_RT(S, D)                                               \
+    do {                                                                 \
+        if (rt == 1) launch_rows<S, bf16_t, D, 1>(a, grid, batch, s);    \
+        else launch_rows<S, bf16_t, D, 2>(a, grid, batch, s);            \
     } while (0)
     if (block_rows == kRowsPerBlock) {
         const hipError_t rc = launch_tree_rows(head_dim, kv8, a, batch, s);
         if (rc != hipSuccess) return rc;
     } else if (kv8) {
-        if (dtype == 1 && head_dim == 64) HGCA_TREE_RT(kv8_t, bf16_t, 64);
-        else if (dtype == 1) HGCA_TREE_RT(kv8_t, bf16_t, 128);
-        else if (head_dim == 64) HGCA_TREE_RT(kv8_t, float, 64);
-        else HGCA_TREE_RT(kv8_t, float, 128);
+        if (dtype == 1 && head_dim == 64) HGCA_TREE_RT(kv8_t, 64);
+        else if (dtype == 1) HGCA_TREE_RT(kv8_t, 128);
+        else if (head_dim == 64) launch_rows<kv8_t, float, 64, 1>(a, grid, batch, s);
+        else launch_rows<kv8_t, float, 128, 1>(a, grid, batch, s);
     } else if (dtype == 1) {
-        if (head_dim == 64) HGCA_TREE_RT(bf16_t, bf16_t, 64);
-        else HGCA_TREE_RT(bf16_t, bf16_t, 128);
+        if (head_dim == 64) HGCA_TREE_RT(bf16_t, 64);
+        else HGCA_TREE_RT(bf16_t, 128);
     } else if (head_dim == 64) {
         if (rt == 1) hipLaunchKernelGGL((rows_attn_f32_kernel<64, 1>), grid, dim3(kTreeBlock), 0, s, a);
         else hipLaunchKernelGGL((rows_attn_f32_kernel<64, 2>), grid, dim3(kTreeBlock), 0, s, a);

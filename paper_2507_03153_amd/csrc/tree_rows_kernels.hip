@@ -21,34 +21,34 @@ static_assert(kNW == kTreeWaves && kRowsPerBlock == 32 * kNW, "32 rows per wave"
 
 // The rows of a step of an 8-bit tier on their way through registers: thread t has a quarter of row t / 4 of K and of V.
 template <int D> struct CodesInFlight {
-    static constexpr int kBytes = D / 4, kWords = kBytes / 4;    // 32 or 16 codes: a scale's block, or half of one
-    uint32_t k[kWords], v[kWords];
-    uint8_t ks, vs;
+    static constexpr int kChunks = D / 64;       // of 16 codes, per thread and tensor: of K neighbours, of V every fourth, which
+    uint4 k[kChunks], v[kChunks];                // halves the bank conflicts of its stores
+    typename Kv8Scales<D>::Word ks, vs;
     __device__ __forceinline__ void load(const TreeArgs &a, const BlockRows &rows, int step, int nsub) {
         const int tok = min(step * kStepTokens + (int)threadIdx.x / 4, nsub - 1), part = threadIdx.x % 4;
         const size_t row = rows.table ? rows.table[tok / kGranule] + tok % kGranule : rows.base + tok;
-        const char *kp = a.kv.k + row * D + part * kBytes, *vp = a.kv.v + row * D + part * kBytes;
 #pragma unroll
-        for (int i = 0; i < kWords; i += 4) {
-            *reinterpret_cast<uint4 *>(k + i) = load16(kp + 4 * i);
-            *reinterpret_cast<uint4 *>(v + i) = load16(vp + 4 * i);
+        for (int i = 0; i < kChunks; ++i) {
+            k[i] = load16(a.kv.k + row * D + 16 * (part * kChunks + i));
+            v[i] = load16(a.kv.v + row * D + 16 * (part + 4 * i));
         }
-        ks = reinterpret_cast<const uint8_t *>(a.k_scale)[row * (D / 32) + part * kBytes / 32];
-        vs = reinterpret_cast<const uint8_t *>(a.v_scale)[row * (D / 32) + part * kBytes / 32];
+        ks = reinterpret_cast<const typename Kv8Scales<D>::Word *>(a.k_scale)[row];
+        vs = reinterpret_cast<const typename Kv8Scales<D>::Word *>(a.v_scale)[row];
     }
     __device__ __forceinline__ void store(char *k_stage, char *v_stage) const {
         using S = DmaStage<D, kNW>;
         const int row = threadIdx.x / 4, part = threadIdx.x % 4;
-        const float kf = __uint_as_float((uint32_t)ks << 23), vf = __uint_as_float((uint32_t)vs << 23);
-        auto eight = [](const uint32_t *c, float f) {
-            return make_uint4(kv8_pair_bf16<false>(c[0], f), kv8_pair_bf16<true>(c[0], f), kv8_pair_bf16<false>(c[1], f),
-                              kv8_pair_bf16<true>(c[1], f));
+        auto eight = [](uint32_t c0, uint32_t c1, float f) {
+            return make_uint4(kv8_pair_bf16<false>(c0, f), kv8_pair_bf16<true>(c0, f), kv8_pair_bf16<false>(c1, f), kv8_pair_bf16<true>(c1, f));
         };
 #pragma unroll
-        for (int i = 0; i < kWords / 2; ++i) {                   // 16-byte pieces of bf16
-            const int piece = part * (kWords / 2) + i;
-            *reinterpret_cast<uint4 *>(k_stage + S::k_offset(row, piece)) = eight(k + 2 * i, kf);
-            *reinterpret_cast<uint4 *>(v_stage + S::v_offset(row, piece / 2) + 16 * (piece % 2)) = eight(v + 2 * i, vf);
+        for (int i = 0; i < kChunks; ++i) {      // a chunk is two 16-byte pieces of bf16
+            const int kc = part * kChunks + i, vc = part + 4 * i;
+            const float kf = kv8_scale(ks, kc / 2), vf = kv8_scale(vs, vc / 2);
+            *reinterpret_cast<uint4 *>(k_stage + S::k_offset(row, 2 * kc)) = eight(k[i].x, k[i].y, kf);
+            *reinterpret_cast<uint4 *>(k_stage + S::k_offset(row, 2 * kc + 1)) = eight(k[i].z, k[i].w, kf);
+            *reinterpret_cast<uint4 *>(v_stage + S::v_offset(row, vc)) = eight(v[i].x, v[i].y, vf);
+            *reinterpret_cast<uint4 *>(v_stage + S::v_offset(row, vc) + 16) = eight(v[i].z, v[i].w, vf);
         }
     }
 };
@@ -66,23 +66,26 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     __shared__ uint32_t s_row[kSub];
 
     // Workgroups are dealt to the XCDs in turn: blocks of rows that read the same tokens take numbers that are equal modulo their number
-    int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z, rb = 0;
+    int slot = blockIdx.x, kvh = blockIdx.y, rb = 0;
     if (flat) {
         const int wg = (int)blockIdx.x, stream = wg % kXcds + kXcds * (wg / kXcds / a.row_blocks);
-        if (stream >= a.n_splits * a.sh.n_kv_heads * a.sh.batch) return;         // uniform over the workgroup
+        if (stream >= a.n_splits * a.sh.batch * a.sh.n_kv_heads) return;         // uniform over the workgroup
         rb = wg / kXcds % a.row_blocks;
-        split = stream % a.n_splits;
-        kvh = stream / a.n_splits % a.sh.n_kv_heads;
-        b = stream / a.n_splits / a.sh.n_kv_heads;
+        kvh = stream % a.sh.n_kv_heads;
+        slot = stream / a.sh.n_kv_heads;
     } else if (a.row_blocks > 1) {
-        rb = split % a.row_blocks;
-        split /= a.row_blocks;
+        rb = slot % a.row_blocks;
+        slot /= a.row_blocks;
     }
+    const Span span(a, slot, kStepTokens);
+    if (span.idle) return;                       // uniform over the workgroup
+    if (kvh == 0 && rb == 0) span.tell(a);
+    const int b = span.b;
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
-    const int group = a.sh.group, rows = a.n_q * group, row0 = rb * kRowsPerBlock + 32 * w;
+    const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group, row0 = rb * kRowsPerBlock + 32 * w;
     const bool wave_live = row0 < rows, row_exists = row0 + n < rows;
     const int row = min(row0 + n, rows - 1);     // lanes without a row repeat the last one and store nothing
-    const int64_t qr = (int64_t)b * a.n_q + row / group, out_row = qr * a.sh.n_q_heads + kvh * group + row % group;
+    const int64_t qr = (int64_t)b * a.n_q + (row >> lg), out_row = qr * a.sh.n_q_heads + kvh * group + (row & (group - 1));
     uint4 qop[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) qop[kk] = load16(static_cast<const char *>(a.q) + out_row * S::kRowBytes + 16 * (2 * kk + hw));
@@ -93,7 +96,6 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     for (int kk = 0; kk < KK; ++kk) k_lane[kk] = S::k_offset(n, 2 * kk + hw);
     const int v_lane = S::v_offset(4 * hw + lane % 16 / 4, lane / 16 % 2) + 8 * (lane % 4);
 
-    const Span span(a, b, split, kStepTokens);
     const int tail = !kCodes && a.mask ? span.len - a.n_q : span.len;            // first drafted token
     float m = -INFINITY, shift = 0.f, l = 0.f;   // l: over this lane's tokens
     floatx16 acc[DT];
@@ -265,6 +267,12 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
             if constexpr (!kCodes) wait_for_own_loads();         // the barrier alone does not wait for LDS-direct loads
             __syncthreads();
             if (s + 1 < steps) request(s + 1, k_next, v_next);
+            // the further a workgroup is in its pass, the lower its priority: of two on a unit the older would finish far ahead
+            const int left = steps - s;
+            if (2 * left > steps) __builtin_amdgcn_s_setprio(3);
+            else if (4 * left > steps) __builtin_amdgcn_s_setprio(2);
+            else if (8 * left > steps) __builtin_amdgcn_s_setprio(1);
+            else __builtin_amdgcn_s_setprio(0);
             if (wave_live) body(masked, k_cur, v_cur, first + s * kStepTokens);
             if (s + 1 < steps) arrive(k_next, v_next);
         };
@@ -282,7 +290,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     if (!row_exists) return;
     const bool whole = a.n_splits == 1;
     const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-    const int64_t at = whole ? out_row : out_row * a.n_splits + split;
+    const int64_t at = whole ? out_row : partial_row(a, slot, kvh, row);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -313,9 +321,9 @@ hipError_t launch_tree_rows(int head_dim, bool kv8, const TreeArgs &a, int batch
     const int64_t streams = (int64_t)a.n_splits * a.sh.n_kv_heads * batch;
     const int64_t blocks = (streams + kXcds - 1) / kXcds * kXcds * a.row_blocks;
     const int flat = a.row_blocks > 1 && blocks <= int64_t(1) << 23 ? 1 : 0;     // (threads of a flat grid are counted in 32 bits)
-    const dim3 grid = flat ? dim3((unsigned)blocks) : dim3((unsigned)(a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads, (unsigned)batch);
+    const dim3 grid = flat ? dim3((unsigned)blocks) : dim3((unsigned)((int64_t)batch * a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads);
     // rows that pass once and are more than the last cache holds leave the caches alone
-    const int streamed = a.row_blocks == 1 && (int64_t)batch * a.sh.n_kv_heads * a.kv.cap * head_dim * 4 >= kLastCache ? 1 : 0;
+    const int streamed = a.row_blocks == 1 && (int64_t)batch * a.sh.n_kv_heads * a.kv.cap * head_dim * (kv8 ? 2 : 4) >= kLastCache ? 1 : 0;
 #define HGCA_MANY(ST, D)                                                                                                  \
     do {                                                                                                                  \
         if (a.o_bf16) hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 2>), grid, dim3(kTreeBlock), 0, s, a, flat, streamed); \

@@ -224,6 +224,41 @@ def test_a_long_sequence_among_short_ones(gpu):
         check(o[b:b + 1], lse[b:b + 1], O, Ls, *bounds(q[b:b + 1], K, V, [L], 0.125, max(L, 1)), "f32")
 
 
+@pytest.mark.parametrize("dtype,B,n,Hq,Hkv,lens", [
+    ("bf16", 130, 2, 4, 1, "ragged"),            # a lane has several sequences
+    ("f32", 70, 3, 2, 1, "ragged"),
+    ("bf16", 40, 40, 4, 1, "one long"),          # 160 rows: two blocks of 128
+    ("bf16", 5, 20, 8, 2, "one long"),
+    ("bf16", 512, 1, 1, 1, "equal"),
+    ("bf16", 300, 1, 2, 1, "empty"),
+    ("f32", 3, 1, 8, 8, "empty"),
+])
+def test_batches_share_the_splits_by_their_lengths(gpu, dtype, B, n, Hq, Hkv, lens):
+    """Sequences of very different length, all of one length, and of none: each row is folded from its own sequence's splits."""
+    torch, hgca = gpu
+    d, bs, T = 64, 16, 2000
+    rng = np.random.default_rng(B + n)
+    L = {"ragged": lambda: (T * rng.random(B) ** 4).astype(np.int32), "one long": lambda: np.r_[np.full(B - 1, n), T].astype(np.int32),
+         "equal": lambda: np.full(B, 700, np.int32), "empty": lambda: np.zeros(B, np.int32)}[lens]()
+    print(f"\n[case] {dtype} B={B} n={n} {Hq}/{Hkv} {lens}", flush=True)
+    n_blk = [-(-int(x) // bs) for x in L]
+    table, at = np.zeros((B, T // bs), np.int32), 0
+    perm = rng.permutation(max(sum(n_blk), 1)).astype(np.int32)
+    for b, x in enumerate(n_blk):
+        table[b, :x] = perm[at:at + x]
+        at += x
+    r = (lambda *s: rng.standard_normal(s).astype(np.float32)) if dtype == "f32" else (lambda *s: do.to_bf16(rng.standard_normal(s)))
+    kb, vb, q = r(len(perm), Hkv, bs, d), r(len(perm), Hkv, bs, d), r(B, n, Hq, d)
+    m = [do.ancestors(rng, n) for _ in range(B)]
+    tier = hgca.Tier(put(torch, kb, dtype), put(torch, vb, dtype), T, i32(torch, L), i32(torch, table), bs)
+    shape = hgca.Shape(hgca.F32 if dtype == "f32" else hgca.BF16, B, Hq, Hkv, d, 0.125)
+    o, lse = call(gpu, shape, put(torch, q, dtype), tier, torch.from_numpy(do.as_int64(m)).to(DEV), "f32")
+    for b in sorted({0, 1, B // 2, B - 2, B - 1, int(np.argmax(L)), int(np.argmin(L))}):
+        K, V = (np.concatenate([x[i] for i in table[b, :n_blk[b]]] or [np.zeros((Hkv, 1, d))], 1)[None] for x in (kb, vb))
+        O, Ls = do.rows_attention(q[b:b + 1].astype(np.float64), K.astype(np.float64), V.astype(np.float64), L[b:b + 1], 0.125, m[b:b + 1])
+        check(o[b:b + 1], lse[b:b + 1], O, Ls, *bounds(q[b:b + 1], K, V, L[b:b + 1], 0.125, T), "f32")
+
+
 def test_same_result_again_and_in_a_graph(gpu):
     """Two runs agree bit for bit; a captured call follows its inputs, beside eager calls with a workspace of their own."""
     torch, hgca = gpu
