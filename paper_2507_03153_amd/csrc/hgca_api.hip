@@ -245,8 +245,8 @@ constexpr int32_t kMaxRowsCap = 1 << 30;         // positions and step counts of
 constexpr int32_t kMaxKv8Queries = 4096;
 
 // Splits per (sequence, KV head, block of rows) whose tier holds up to `cap` tokens, on average over the sequences (Span): about
-// 512 workgroups, a round of the two that a compute unit holds, of 256 tokens at least; a tier of up to 512 tokens is not split,
-// which saves the fold's launch.
+// 512 workgroups, a round of the two that a compute unit holds, of 256 tokens at least; a tier of up to 512 tokens (256, with
+// more than 32 rows per workgroup) is not split, which saves the fold's launch.
 #ifndef HGCA_TARGET_WGS_TREE
 #define HGCA_TARGET_WGS_TREE 512
 #endif
@@ -267,7 +267,7 @@ TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, bool kv8, int32_t cap)
     const int64_t rows = (int64_t)n_q * group_of(s), per_block = tree_block_rows(s->dtype, kv8, (int)rows);
     t.row_blocks = (int32_t)((rows + per_block - 1) / per_block);
     const int64_t units = std::max<int64_t>(1, (int64_t)s->batch * s->n_kv_heads * t.row_blocks);
-    const int64_t most = cap <= HGCA_TREE_WHOLE ? 1 : ((int64_t)cap + HGCA_TREE_MIN - 1) / HGCA_TREE_MIN;
+    const int64_t most = cap <= (per_block > 32 ? HGCA_TREE_MIN : HGCA_TREE_WHOLE) ? 1 : ((int64_t)cap + HGCA_TREE_MIN - 1) / HGCA_TREE_MIN;
     t.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HGCA_TARGET_WGS_TREE / units, most));
     const size_t parts = t.n_splits > 1 ? (size_t)s->batch * n_q * s->n_q_heads * t.n_splits : 0;
     t.part_m = align_up(parts * s->head_dim * sizeof(float));

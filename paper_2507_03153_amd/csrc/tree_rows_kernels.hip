@@ -53,12 +53,13 @@ template <int D> struct CodesInFlight {
     }
 };
 
-template <typename ST, int D, int PP>
+// HALVES: up to 64 rows per workgroup; two waves share 32 of them and take half of a step's tokens each, and add up at the end.
+template <typename ST, int D, int PP, bool HALVES>
 __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs a, int flat, int streamed)
 {
     using S = DmaStage<D, kNW>;
     constexpr bool kCodes = sizeof(ST) == 1;
-    constexpr int KK = D / 16, DT = D / 32, NT = kStepTokens / 32;
+    constexpr int KK = D / 16, DT = D / 32, NT = HALVES ? 1 : kStepTokens / 32, kRows = HALVES ? kRowsPerBlock / 2 : kRowsPerBlock;
     __shared__ __attribute__((aligned(1024))) char s_k0[S::kBytes];
     __shared__ __attribute__((aligned(1024))) char s_k1[S::kBytes];
     __shared__ __attribute__((aligned(1024))) char s_v0[S::kBytes];
@@ -82,7 +83,8 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     if (kvh == 0 && rb == 0) span.tell(a);
     const int b = span.b;
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
-    const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group, row0 = rb * kRowsPerBlock + 32 * w;
+    const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
+    const int row0 = rb * kRows + 32 * (HALVES ? w % 2 : w), half = HALVES ? w / 2 : 0;     // half: of every step's tokens
     const bool wave_live = row0 < rows, row_exists = row0 + n < rows;
     const int row = min(row0 + n, rows - 1);     // lanes without a row repeat the last one and store nothing
     const int64_t qr = (int64_t)b * a.n_q + (row >> lg), out_row = qr * a.sh.n_q_heads + kvh * group + (row & (group - 1));
@@ -106,6 +108,11 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     // which the lane holds eight.
     auto body = [&](auto masked, const char *k_stage, const char *v_stage, int tok) {
         constexpr bool MASKED = decltype(masked)::value;
+        if (HALVES) {                            // (half: tokens 32 half .. of the step)
+            tok += 32 * half;
+            k_stage += half * 32 * S::kRowBytes;
+            v_stage += half * S::v_offset(32, 0);
+        }
         floatx16 c[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) c[t] = floatx16{};
@@ -285,8 +292,39 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
             step(std::true_type{}, s, s % 2 ? s_k1 : s_k0, s % 2 ? s_v1 : s_v0, s % 2 ? s_k0 : s_k1, s % 2 ? s_v0 : s_v1);
     }
 
-    // the lane holds columns 32 dt + 8 q + 4 hw .. + 3 of its row
     l = halves_sum(l);
+    if constexpr (HALVES) {                      // the two waves of a row: the second one's results by way of the stages
+        __syncthreads();                         // which all waves have read
+        float *const box = reinterpret_cast<float *>(w % 2 ? s_k1 : s_k0);
+        float *const stats = reinterpret_cast<float *>(s_v0) + 3 * kWave * (w % 2);
+        if (half) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) box[(16 * dt + r) * kWave + lane] = acc[dt][r];
+            stats[lane] = m;
+            stats[kWave + lane] = shift;
+            stats[2 * kWave + lane] = l;
+        }
+        __syncthreads();
+        if (half) return;
+        const float m2 = stats[lane], shift2 = stats[kWave + lane], l2 = stats[2 * kWave + lane];
+        const float to = fminf(m == -INFINITY ? INFINITY : shift, m2 == -INFINITY ? INFINITY : shift2);          // of the larger maximum
+        const float f1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - shift);
+        const float f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - shift2);
+        l = m2 == -INFINITY ? l : fmaf(l2, f2, l * f1);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float x = box[(16 * dt + r) * kWave + lane];
+                acc[dt][r] = m2 == -INFINITY ? acc[dt][r] : m == -INFINITY ? x : fmaf(x, f2, acc[dt][r] * f1);
+            }
+        if (m == -INFINITY) l = l2;
+        m = fmaxf(m, m2);
+        shift = m == -INFINITY ? 0.f : to;
+    }
+    // the lane holds columns 32 dt + 8 q + 4 hw .. + 3 of its row
     if (!row_exists) return;
     const bool whole = a.n_splits == 1;
     const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
@@ -324,11 +362,15 @@ hipError_t launch_tree_rows(int head_dim, bool kv8, const TreeArgs &a, int batch
     const dim3 grid = flat ? dim3((unsigned)blocks) : dim3((unsigned)((int64_t)batch * a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads);
     // rows that pass once and are more than the last cache holds leave the caches alone
     const int streamed = a.row_blocks == 1 && (int64_t)batch * a.sh.n_kv_heads * a.kv.cap * head_dim * (kv8 ? 2 : 4) >= kLastCache ? 1 : 0;
-#define HGCA_MANY(ST, D)                                                                                                  \
-    do {                                                                                                                  \
-        if (a.o_bf16) hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 2>), grid, dim3(kTreeBlock), 0, s, a, flat, streamed); \
-        else hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 3>), grid, dim3(kTreeBlock), 0, s, a, flat, streamed);      \
+    const bool halves = a.n_q * a.sh.group <= kRowsPerBlock / 2;
+#define HGCA_MANY(ST, D)                                                                                                            \
+    do {                                                                                                                            \
+        if (halves && a.o_bf16) hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 2, true>), grid, block, 0, s, a, flat, streamed);  \
+        else if (halves) hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 3, true>), grid, block, 0, s, a, flat, streamed);         \
+        else if (a.o_bf16) hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 2, false>), grid, block, 0, s, a, flat, streamed);      \
+        else hipLaunchKernelGGL((many_rows_attn_kernel<ST, D, 3, false>), grid, block, 0, s, a, flat, streamed);                    \
     } while (0)
+    const dim3 block(kTreeBlock);
     if (kv8 && head_dim == 64) HGCA_MANY(kv8_t, 64);
     else if (kv8) HGCA_MANY(kv8_t, 128);
     else if (head_dim == 64) HGCA_MANY(bf16_t, 64);

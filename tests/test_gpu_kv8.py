@@ -155,6 +155,8 @@ CASES = [
     ("bf16", 128, 4, 4, 70, 48, "f32", [200, 33]),
     ("bf16", 128, 16, 2, 16, 16, "bf16", [515, 16]),
     ("bf16", 64, 8, 1, 1, 16, "f32", [1000, 31]),
+    ("bf16", 128, 16, 2, 8, 16, "f32", [515, 33, 0, 1500]),
+    ("bf16", 64, 8, 8, 50, 0, "bf16", [97, 1]),
     ("bf16", 64, 8, 4, 40, 0, "bf16", [97, 15]),
     ("f32", 128, 8, 2, 5, 0, "f32", [300, 1]),
     ("f32", 128, 8, 1, 9, 16, "bf16", [333, 47]),

@@ -100,6 +100,8 @@ CASES = [
     ("bf16", 64, 8, 4, 17, 16, "f32", [97, 128, 1000]),
     ("bf16", 64, 8, 8, 2, 0, "bf16", [2, 31, 32]),
     ("bf16", 64, 16, 2, 16, 32, "f32", [160, 161]),
+    ("bf16", 128, 16, 2, 8, 16, "f32", [700, 8, 90, 1900]),
+    ("bf16", 64, 4, 4, 64, 0, "bf16", [300, 64]),
     ("f32", 128, 8, 2, 5, 0, "f32", [200, 5, 129]),
     ("f32", 128, 8, 1, 9, 16, "f32", [9, 3, 400]),
     ("f32", 128, 4, 4, 64, 48, "bf16", [65, 260]),
