@@ -277,8 +277,9 @@ struct Kv8WriteArgs {
     const int32_t *first;      // [B] or null (= 0): position of the first token
     int32_t *status;           // optional
     int32_t n_tokens, n_kv_heads;
+    int32_t lg_tokens;         // (set by the launch function)
 };
-hipError_t launch_kv8_write(int dtype, int head_dim, bool from_tier, const Kv8WriteArgs &a, int batch, hipStream_t s);
+hipError_t launch_kv8_write(int dtype, int head_dim, bool from_tier, Kv8WriteArgs a, int batch, hipStream_t s);
 
 struct Kv8ReadArgs {
     KvDev src;
@@ -286,8 +287,9 @@ struct Kv8ReadArgs {
     const int32_t *first;
     char *k_out, *v_out;       // [B, n_tokens, Hkv, d]
     int32_t n_tokens, n_kv_heads;
+    int32_t lg_tokens;         // (set by the launch function)
 };
-hipError_t launch_kv8_read(int dtype, int head_dim, const Kv8ReadArgs &a, int batch, hipStream_t s);
+hipError_t launch_kv8_read(int dtype, int head_dim, Kv8ReadArgs a, int batch, hipStream_t s);
 
 struct CommitArgs {
     KvDev tier;                // k, v are written

@@ -81,41 +81,66 @@ __device__ __forceinline__ int room_of(const KvDev &kv, int b) {
     return (int)min((int64_t)kv.cap, max(left, (int64_t)0));
 }
 
-// D / 8 lanes per row of K and of V.  FROM_TIER: rows of the same positions of another tier; else rows [B, n, Hkv, d].
+// Which rows a workgroup goes through: D / 8 lanes per row of K and of V, so 16 or 32 rows at a time, of `tokens_at_once` tokens (a
+// power of two) of one KV head, or of few tokens of several heads; then the next ones, gridDim.x workgroups apart.  No division
+// but the one by the block size.
+template <int D> struct RowWalk {
+    static constexpr int kRows = kKv8Block / (D / 8);
+    int head, token, step;
+    __device__ __forceinline__ explicit RowWalk(int lg_tokens) {
+        const int row = threadIdx.x / (D / 8), at_once = 1 << lg_tokens;
+        head = (int)blockIdx.y * (kRows >> lg_tokens) + (row >> lg_tokens);
+        token = (int)blockIdx.x * at_once + (row & (at_once - 1));
+        step = (int)gridDim.x * at_once;
+    }
+};
+// Rows of a thread whose loads are in flight together; rows of fp32 are long enough one at a time.  8 x 4096 tokens of 8 heads of 128 written
+// and read back, 4 : 2 : 1 rows, us: bf16 90 to 97 : 94 to 96 : 94 to 97 (with a division per row 99 to 105), heads of 64 40.8 : 43.6 : 43;
+// 4 x 2000 tokens in fp32 41.6 : 36.6 : 34.9.
+template <typename T> constexpr int kTogether = sizeof(T) == 2 ? 4 : 1;
+
+// FROM_TIER: rows of the same positions of another tier; else rows [B, n, Hkv, d].
 template <typename T, int D, bool FROM_TIER>
 __global__ __launch_bounds__(kKv8Block) void kv8_write_kernel(Kv8WriteArgs a)
 {
-    constexpr int LR = D / 8, ROWS = kKv8Block / LR, RB = D * (int)sizeof(T);
-    const int b = blockIdx.y, lane = threadIdx.x % kWave, sub = threadIdx.x % LR;
+    constexpr int LR = D / 8, RB = D * (int)sizeof(T);
+    const int b = blockIdx.z, lane = threadIdx.x % kWave, sub = threadIdx.x % LR;
     const int first = max(a.first ? a.first[b] : 0, 0);
     int n = a.n_tokens;
     if (FROM_TIER) n = min(n, max(tier_len(a.src, b) - first, 0));
     const int room = max(room_of(a.dst, b) - first, 0);
     if (n > room) {
-        if (a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, kCacheContextFull);
+        if (a.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(a.status, kCacheContextFull);
         n = room;
     }
     const int32_t *to = blocks_of(a.dst, b), *from = FROM_TIER ? blocks_of(a.src, b) : nullptr;
-    const int64_t total = (int64_t)n * a.n_kv_heads;
-    for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / LR; i < total; i += (int64_t)gridDim.x * ROWS) {
-        // consecutive rows of the source are consecutive here
-        const int t = FROM_TIER ? (int)(i % n) : (int)(i / a.n_kv_heads);
-        const int h = FROM_TIER ? (int)(i / n) : (int)(i % a.n_kv_heads);
-        const size_t row = FROM_TIER ? row_of(a.src, from, a.n_kv_heads, b, h, first + t)
-                                     : ((size_t)b * a.n_tokens + t) * a.n_kv_heads + h;
-        float k[8], v[8];
-        load8<T>(a.src.k + row * RB + sub * 8 * sizeof(T), k);
-        load8<T>(a.src.v + row * RB + sub * 8 * sizeof(T), v);
-        const size_t out = row_of(a.dst, to, a.n_kv_heads, b, h, first + t);
-        uint32_t kc, vc;
-        const uint2 k8 = encode8(k, kc), v8 = encode8(v, vc);
-        *reinterpret_cast<uint2 *>(const_cast<char *>(a.dst.k) + out * D + sub * 8) = k8;
-        *reinterpret_cast<uint2 *>(const_cast<char *>(a.dst.v) + out * D + sub * 8) = v8;
-        const uint32_t ks = row_scales<D>(kc, lane), vs = row_scales<D>(vc, lane);
-        if (sub == 0) {
-            typedef typename Kv8Scales<D>::Word Word;
-            reinterpret_cast<Word *>(a.k_scale)[out] = (Word)ks;
-            reinterpret_cast<Word *>(a.v_scale)[out] = (Word)vs;
+    const RowWalk<D> walk(a.lg_tokens);
+    if (walk.head >= a.n_kv_heads) return;
+    for (int64_t t0 = walk.token; t0 < n; t0 += (int64_t)kTogether<T> * walk.step) {
+        float k[kTogether<T>][8], v[kTogether<T>][8];
+#pragma unroll
+        for (int u = 0; u < kTogether<T>; ++u) {    // (behind the last token: the last one again)
+            const int t = (int)min(t0 + (int64_t)u * walk.step, (int64_t)n - 1);
+            const size_t row = FROM_TIER ? row_of(a.src, from, a.n_kv_heads, b, walk.head, first + t)
+                                         : ((size_t)b * a.n_tokens + t) * a.n_kv_heads + walk.head;
+            load8<T>(a.src.k + row * RB + sub * 8 * sizeof(T), k[u]);
+            load8<T>(a.src.v + row * RB + sub * 8 * sizeof(T), v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether<T>; ++u) {
+            const int64_t t = t0 + (int64_t)u * walk.step;
+            if (t >= n) break;                   // (the lanes of a row agree)
+            const size_t out = row_of(a.dst, to, a.n_kv_heads, b, walk.head, first + (int)t);
+            uint32_t kc, vc;
+            const uint2 k8 = encode8(k[u], kc), v8 = encode8(v[u], vc);
+            *reinterpret_cast<uint2 *>(const_cast<char *>(a.dst.k) + out * D + sub * 8) = k8;
+            *reinterpret_cast<uint2 *>(const_cast<char *>(a.dst.v) + out * D + sub * 8) = v8;
+            const uint32_t ks = row_scales<D>(kc, lane), vs = row_scales<D>(vc, lane);
+            if (sub == 0) {
+                typedef typename Kv8Scales<D>::Word Word;
+                reinterpret_cast<Word *>(a.k_scale)[out] = (Word)ks;
+                reinterpret_cast<Word *>(a.v_scale)[out] = (Word)vs;
+            }
         }
     }
 }
@@ -123,30 +148,45 @@ __global__ __launch_bounds__(kKv8Block) void kv8_write_kernel(Kv8WriteArgs a)
 template <typename T, int D>
 __global__ __launch_bounds__(kKv8Block) void kv8_read_kernel(Kv8ReadArgs a)
 {
-    constexpr int LR = D / 8, ROWS = kKv8Block / LR, E = sizeof(T);
+    constexpr int LR = D / 8, E = sizeof(T);
     typedef typename Kv8Scales<D>::Word Word;
-    const int b = blockIdx.y, sub = threadIdx.x % LR;
+    const int b = blockIdx.z, sub = threadIdx.x % LR;
     const int first = max(a.first ? a.first[b] : 0, 0);
     const int n = min(a.n_tokens, max(min(tier_len(a.src, b), room_of(a.src, b)) - first, 0));
     const int32_t *from = blocks_of(a.src, b);
-    const int64_t total = (int64_t)n * a.n_kv_heads;
-    for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / LR; i < total; i += (int64_t)gridDim.x * ROWS) {
-        const int t = (int)(i / a.n_kv_heads), h = (int)(i % a.n_kv_heads);
-        const size_t row = row_of(a.src, from, a.n_kv_heads, b, h, first + t);
-        const size_t out = (((size_t)b * a.n_tokens + t) * a.n_kv_heads + h) * D + sub * 8;
+    const RowWalk<D> walk(a.lg_tokens);
+    if (walk.head >= a.n_kv_heads) return;
+    for (int64_t t0 = walk.token; t0 < n; t0 += (int64_t)kTogether<T> * walk.step) {
+        uint2 c[kTogether<T>][2];
+        Word scales[kTogether<T>][2];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const uint2 c = *reinterpret_cast<const uint2 *>((x ? a.src.v : a.src.k) + row * D + sub * 8);
-            const float scale = kv8_scale((uint32_t) reinterpret_cast<const Word *>(x ? a.v_scale : a.k_scale)[row], sub / 4);
-            char *dst = (x ? a.v_out : a.k_out) + out * E;
-            if constexpr (E == 4) {
-                const FloatPair p0 = kv8_pair_f32<false>(c.x, scale), p1 = kv8_pair_f32<true>(c.x, scale);
-                const FloatPair p2 = kv8_pair_f32<false>(c.y, scale), p3 = kv8_pair_f32<true>(c.y, scale);
-                *reinterpret_cast<float4 *>(dst) = make_float4(p0[0], p0[1], p1[0], p1[1]);
-                *reinterpret_cast<float4 *>(dst + 16) = make_float4(p2[0], p2[1], p3[0], p3[1]);
-            } else {
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(kv8_pair_bf16<false>(c.x, scale), kv8_pair_bf16<true>(c.x, scale),
-                                                             kv8_pair_bf16<false>(c.y, scale), kv8_pair_bf16<true>(c.y, scale));
+        for (int u = 0; u < kTogether<T>; ++u) {
+            const int t = (int)min(t0 + (int64_t)u * walk.step, (int64_t)n - 1);
+            const size_t row = row_of(a.src, from, a.n_kv_heads, b, walk.head, first + t);
+            c[u][0] = *reinterpret_cast<const uint2 *>(a.src.k + row * D + sub * 8);
+            c[u][1] = *reinterpret_cast<const uint2 *>(a.src.v + row * D + sub * 8);
+            scales[u][0] = reinterpret_cast<const Word *>(a.k_scale)[row];
+            scales[u][1] = reinterpret_cast<const Word *>(a.v_scale)[row];
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether<T>; ++u) {
+            const int64_t t = t0 + (int64_t)u * walk.step;
+            if (t >= n) break;
+            const size_t out = (((size_t)b * a.n_tokens + t) * a.n_kv_heads + walk.head) * D + sub * 8;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float scale = kv8_scale((uint32_t)scales[u][x], sub / 4);
+                char *dst = (x ? a.v_out : a.k_out) + out * E;
+                if constexpr (E == 4) {
+                    const FloatPair p0 = kv8_pair_f32<false>(c[u][x].x, scale), p1 = kv8_pair_f32<true>(c[u][x].x, scale);
+                    const FloatPair p2 = kv8_pair_f32<false>(c[u][x].y, scale), p3 = kv8_pair_f32<true>(c[u][x].y, scale);
+                    *reinterpret_cast<float4 *>(dst) = make_float4(p0[0], p0[1], p1[0], p1[1]);
+                    *reinterpret_cast<float4 *>(dst + 16) = make_float4(p2[0], p2[1], p3[0], p3[1]);
+                } else {
+                    *reinterpret_cast<uint4 *>(dst) =
+                        make_uint4(kv8_pair_bf16<false>(c[u][x].x, scale), kv8_pair_bf16<true>(c[u][x].x, scale),
+                                   kv8_pair_bf16<false>(c[u][x].y, scale), kv8_pair_bf16<true>(c[u][x].y, scale));
+                }
             }
         }
     }
@@ -183,12 +223,23 @@ unsigned share_of(int64_t units, int batch) {
     return (unsigned)std::max<int64_t>(1, std::min<int64_t>(units, std::max<int64_t>(1, 2048 / batch)));
 }
 
-}  // namespace
-
-hipError_t launch_kv8_write(int dtype, int head_dim, bool from_tier, const Kv8WriteArgs &a, int batch, hipStream_t s)
+// Rows of a workgroup by tokens and heads (RowWalk), and the grid: 2048 workgroups at most where a sequence has more tokens
+dim3 walk_grid(int head_dim, int n_tokens, int n_kv_heads, int batch, int32_t &lg_tokens)
 {
     const int rows = kKv8Block / (head_dim / 8);
-    const dim3 grid(share_of(((int64_t)a.n_tokens * a.n_kv_heads + rows - 1) / rows, batch), batch), block(kKv8Block);
+    lg_tokens = 0;
+    while ((1 << lg_tokens) < rows && (1 << lg_tokens) < n_tokens) ++lg_tokens;
+    const int heads = rows >> lg_tokens;
+    const unsigned y = (unsigned)((n_kv_heads + heads - 1) / heads);
+    const int64_t x = ((int64_t)n_tokens + (1 << lg_tokens) - 1) >> lg_tokens;
+    return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(x, 2048 / std::max<int64_t>(1, (int64_t)y * batch))), y, (unsigned)batch);
+}
+
+}  // namespace
+
+hipError_t launch_kv8_write(int dtype, int head_dim, bool from_tier, Kv8WriteArgs a, int batch, hipStream_t s)
+{
+    const dim3 grid = walk_grid(head_dim, a.n_tokens, a.n_kv_heads, batch, a.lg_tokens), block(kKv8Block);
 #define HGCA_KV8_WRITE(T, D)                                                                         \
     do {                                                                                             \
         if (from_tier) hipLaunchKernelGGL((kv8_write_kernel<T, D, true>), grid, block, 0, s, a);     \
@@ -202,10 +253,9 @@ hipError_t launch_kv8_write(int dtype, int head_dim, bool from_tier, const Kv8Wr
     return hipGetLastError();
 }
 
-hipError_t launch_kv8_read(int dtype, int head_dim, const Kv8ReadArgs &a, int batch, hipStream_t s)
+hipError_t launch_kv8_read(int dtype, int head_dim, Kv8ReadArgs a, int batch, hipStream_t s)
 {
-    const int rows = kKv8Block / (head_dim / 8);
-    const dim3 grid(share_of(((int64_t)a.n_tokens * a.n_kv_heads + rows - 1) / rows, batch), batch), block(kKv8Block);
+    const dim3 grid = walk_grid(head_dim, a.n_tokens, a.n_kv_heads, batch, a.lg_tokens), block(kKv8Block);
     if (dtype == 0 && head_dim == 64) hipLaunchKernelGGL((kv8_read_kernel<float, 64>), grid, block, 0, s, a);
     else if (dtype == 0) hipLaunchKernelGGL((kv8_read_kernel<float, 128>), grid, block, 0, s, a);
     else if (head_dim == 64) hipLaunchKernelGGL((kv8_read_kernel<bf16_t, 64>), grid, block, 0, s, a);
