@@ -17,7 +17,7 @@ class LayerCache:
 
     def __init__(self, dtype, B: int, Hq: int, Hkv: int, d: int, block_size: int, win_blocks: int, max_blocks: int,
                  k_max: int, sm_scale: float, device="cuda:0", keep_evicted_maw: bool = False,
-                 fused_tail: bool = True, win_cap_blocks: int = 0):
+                 fused_tail: bool = True, win_cap_blocks: int = 0, pool8: bool = False):
         i32 = dict(dtype=torch.int32, device=device)
         f32 = dict(dtype=torch.float32, device=device)
         self.B, self.Hq, self.Hkv, self.d = B, Hq, Hkv, d
@@ -50,6 +50,9 @@ class LayerCache:
                                 block_size, self.first_win_block)
         self.pool = hgca.Tier(self.k_blocks, self.v_blocks, self.pool_cap, self.pool_lens, self.block_table,
                               block_size, None)
+        # the pool's entries once more in 8 bits (E4M3 with scales), for draft_step: same blocks, table and lengths
+        self.pool8 = hgca.Kv8Tier.like(self.pool) if pool8 else None
+        self.pool8_lens = torch.zeros(B, **i32)          # tokens of the pool that are there already
         # per-step outputs and scratch
         self.o_w, self.lse_w = torch.empty(B, Hq, d, **f32), torch.empty(B, Hq, **f32)
         self.o_s, self.lse_s = torch.empty(B, Hq, d, **f32), torch.empty(B, Hq, **f32)
@@ -129,3 +132,47 @@ class LayerCache:
         self.append(k_in, v_in)
         self.attend(q, alpha if fused_maw else None)
         self.manage(alpha, beta, maw_done=fused_maw)
+
+    def draft_step(self, q, k_in, v_in, mask=None) -> None:
+        """Attention of n drafted tokens per sequence, which join the window for the time being: q [B,n,Hq,d], k_in / v_in
+        [B,n,Hkv,d]; bit j of mask[b,i] (int64 [B,n]) = draft i sees draft j (None: all).  They see the whole window, and the whole
+        pool, in 8 bits if the cache keeps it so.  Results in o_draft [B,n,Hq,d], lse_draft [B,n,Hq]; `commit` follows."""
+        n = int(q.shape[1])
+        if self.win_cap < (self.win_blocks * self.block_size - 1) + n:
+            raise ValueError(f"{n} drafted tokens need win_cap_blocks for l_max - 1 + {n} tokens")
+        if getattr(self, "_draft_n", None) != n:
+            f32 = dict(dtype=torch.float32, device=self.k_blocks.device)
+            self._draft_n = n
+            self.o_draft, self.o_dw, self.o_dp = (torch.empty(self.B, n, self.Hq, self.d, **f32) for _ in range(3))
+            self.lse_draft, self.lse_dw, self.lse_dp = (torch.empty(self.B, n, self.Hq, **f32) for _ in range(3))
+            self.draft_first = torch.zeros_like(self.win_lens)
+            self.ws_tree = hgca.tree_workspace(self.shape, n, self.win_cap, self.k_blocks.device)
+            make = hgca.kv8_workspace if self.pool8 is not None else hgca.append_workspace
+            self.ws_draft_pool = make(self.shape, n, self.pool_cap, self.k_blocks.device)
+        sh = self.shape
+        self.draft_first.copy_(self.win_lens)
+        self._drafts = (k_in, v_in)
+        hgca.kv_append_tokens(sh, self.state, k_in, v_in)
+        hgca.tree_attn(sh, q, self.window, mask, self.o_dw, self.lse_dw, self.ws_tree)
+        if self.pool8 is not None:
+            hgca.kv8_attn(sh, q, self.pool8, self.o_dp, self.lse_dp, self.ws_draft_pool)
+        else:
+            hgca.append_attn(sh, q, self.pool, False, self.o_dp, self.lse_dp, self.ws_draft_pool)
+        merged = hgca.Shape(sh.dtype, sh.batch * n, sh.n_q_heads, sh.n_kv_heads, sh.head_dim, sh.sm_scale)
+        hgca.lse_merge(merged, self.o_dp, self.lse_dp, self.o_dw, self.lse_dw, self.o_draft, self.lse_draft)
+
+    def commit(self, path, cnt, beta: float) -> None:
+        """Of the last draft_step's tokens those on the accepted path stay in the window: path int32 [B,n], cnt int32 [B].  Then
+        windows that have reached l_max evict (Alg. 1); what left them is stored in 8 bits if the cache keeps that.  The moving
+        averages of the tokens that stay start at 0 (attention weights under a tree mask are not averaged)."""
+        k_in, v_in = self._drafts
+        hgca.kv_commit(self.shape, self.window, self.draft_first, k_in, v_in, self.win_lens, path=path, cnt=cnt, status=self.status)
+        hgca.kv_evict(self.shape, self.state, beta)
+        self.sync_pool8()
+
+    def sync_pool8(self) -> None:
+        """Stores in 8 bits what the pool has got since the last call (after any step that may evict)."""
+        if self.pool8 is None:
+            return
+        hgca.kv8_write_tier(self.shape, self.pool8, self.pool8_lens, self.pool, self.pool_cap)
+        self.pool8_lens.copy_(self.pool_lens)
