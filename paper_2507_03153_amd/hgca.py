@@ -610,14 +610,17 @@ class Kv8Tier:
 
 
 def _need(name: str, t: torch.Tensor, dtype, size: tuple, dev: int) -> None:
-    """The tensor has this type and size, is dense and lies on GPU `dev` (one test per property: a call's checks are a third
-    of what it costs the host)."""
+    """The tensor has this type and size, is dense and lies on GPU `dev`."""
+    if t.shape != size or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        _refuse(name, t, dtype, size, dev)
+
+
+def _refuse(name: str, t: torch.Tensor, dtype, size: tuple, dev: int) -> None:
     if t.dtype is not dtype or t.shape != size:
         raise ValueError(f"{name} must be {dtype} of size {list(size)}, got {t.dtype} of size {list(t.shape)}")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, the other tensors on cuda:{dev}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: libhgca takes contiguous tensors")
+    raise ValueError(f"{name}: libhgca takes contiguous tensors")
 
 
 def _gpu_of(t: torch.Tensor) -> int:
@@ -650,30 +653,33 @@ def _tier_view(tier, B: int, H: int, d: int, dtype, dev: int):
 
 
 def _launch(where: str, stream, dev: int, *args) -> None:
-    """Calls `where` on GPU `dev`, on the given stream or the current one there."""
-    if stream is not None and stream.device.index != dev:
-        raise ValueError(f"{where}: tensors on cuda:{dev}, stream on {stream.device}")
-    if dev == (torch.cuda.current_device() if _device is None else _device()):
-        _check(getattr(lib(), where)(*args, _stream(stream)), where)
+    """Calls `where` on GPU `dev`, on the given stream or the current one there.  (A call's checks and views take the host about as
+    long as the launch: 4 of 8 us.)"""
+    call = getattr(_lib or lib(), where)
+    if stream is None and _raw_stream is not None and _device is not None and _device() == dev:
+        status = call(*args, _raw_stream(dev))
     else:
+        if stream is not None and stream.device.index != dev:
+            raise ValueError(f"{where}: tensors on cuda:{dev}, stream on {stream.device}")
         with torch.cuda.device(dev):
-            _check(getattr(lib(), where)(*args, _stream(stream)), where)
+            status = call(*args, _stream(stream))
+    if status:
+        raise HgcaError(status, where)
 
 
-def _torch_dtype(shape: Shape):
-    return torch.float32 if shape.dtype == F32 else torch.bfloat16
+_TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
 
 
 def _heads(shape: Shape):
-    return shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim
+    """Sizes and the tensors' type; another dtype code is the library's to refuse."""
+    return shape.batch, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, _TORCH_DTYPE.get(shape.dtype, torch.bfloat16)
 
 
 def _token_stride(name: str, t: torch.Tensor) -> int:
     """Elements between consecutive tokens of [B,n,H,d], whose heads lie side by side."""
-    B, n, H, d = t.shape
-    s0, s1, s2, s3 = t.stride()
+    (B, n, H, d), (s0, s1, s2, s3) = t.shape, t.stride()
     step = s1 if n > 1 else s0 if B > 1 else H * d
-    if s3 != 1 or (H > 1 and s2 != d) or (B > 1 and n > 1 and s0 != n * step):
+    if s3 != 1 or (s2 != d and H > 1) or (s0 != n * step and B > 1 and n > 1):
         raise ValueError(f"{name}: heads have to lie side by side and tokens at one distance")
     return step
 
@@ -683,8 +689,8 @@ def qk_norm_rope(shape: Shape, q, k, q_out, k_out, inv_freq, q_weight=None, k_we
     """q [B,n,Hq,d] and k [B,n,Hkv,d] normed per head and rotated by position into q_out, k_out (dense; may be q, k where
     those are).  q and k may be parts of wider rows (a fused projection's).  inv_freq fp32 [rot/2]; positions int32 [B,n], or
     first_pos int32 [B] for consecutive ones."""
-    B, Hq, Hkv, d = _heads(shape)
-    dt, dev, n = _torch_dtype(shape), _gpu_of(q), int(q.shape[1])
+    B, Hq, Hkv, d, dt = _heads(shape)
+    dev, n = _gpu_of(q), q.shape[1]
     if q.dtype is not dt or q.shape != (B, n, Hq, d) or k.dtype is not dt or k.shape != (B, n, Hkv, d) or k.get_device() != dev:
         raise ValueError(f"q and k must be {dt} of sizes {[B, n, Hq, d]} and {[B, n, Hkv, d]} on one GPU, got {q.dtype} {list(q.shape)} "
                          f"and {k.dtype} {list(k.shape)}")
@@ -713,8 +719,8 @@ def tree_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Ten
 
 
 def _rows_call(where: str, shape: Shape, q, tier, tier_dtype, mask, o_out, lse_out, ws, stream) -> None:
-    B, Hq, Hkv, d = _heads(shape)
-    dt, dev, n = _torch_dtype(shape), _gpu_of(q), int(q.shape[1])
+    B, Hq, Hkv, d, dt = _heads(shape)
+    dev, n = _gpu_of(q), q.shape[1]
     _need("q", q, dt, (B, n, Hq, d), dev)
     _need("o_out", o_out, torch.bfloat16 if o_out.dtype is torch.bfloat16 else torch.float32, (B, n, Hq, d), dev)
     _need("lse_out", lse_out, torch.float32, (B, n, Hq), dev)
@@ -736,20 +742,26 @@ def tree_attn(shape: Shape, q, tier: Tier, mask, o_out, lse_out, ws, stream=None
     _rows_call("hgca_tree_attn", shape, q, tier, None, mask, o_out, lse_out, ws, stream)
 
 
-def _optional(dev: int, *given) -> None:
-    for name, t, size in given:
-        if t is not None:
-            _need(name, t, torch.int32, size, dev)
+def _first_and_status(B: int, dev: int, first, status=None) -> None:
+    if first is not None:
+        _need("first", first, torch.int32, (B,), dev)
+    if status is not None:
+        _need("status", status, torch.int32, (1,), dev)
 
 
 def kv_commit(shape: Shape, tier: Tier, first, k_in, v_in, lens_out, path=None, cnt=None, status=None, stream=None) -> None:
     """Rows path[b,i], i < cnt[b], of k_in / v_in [B,n,Hkv,d] go to positions first[b] + i of the tier; lens_out[b] = first[b] +
     cnt[b].  path int32 [B,n] (None: row i), cnt int32 [B] (None: n), first int32 [B] (None: 0)."""
-    B, _, Hkv, d = _heads(shape)
-    dt, dev, n = _torch_dtype(shape), _gpu_of(k_in), int(k_in.shape[1])
+    B, _, Hkv, d, dt = _heads(shape)
+    dev, n = _gpu_of(k_in), k_in.shape[1]
     _need("k_in", k_in, dt, (B, n, Hkv, d), dev)
     _need("v_in", v_in, dt, (B, n, Hkv, d), dev)
-    _optional(dev, ("first", first, (B,)), ("path", path, (B, n)), ("cnt", cnt, (B,)), ("lens_out", lens_out, (B,)), ("status", status, (1,)))
+    _need("lens_out", lens_out, torch.int32, (B,), dev)
+    if path is not None:
+        _need("path", path, torch.int32, (B, n), dev)
+    if cnt is not None:
+        _need("cnt", cnt, torch.int32, (B,), dev)
+    _first_and_status(B, dev, first, status)
     kv = _tier_view(tier, B, Hkv, d, dt, dev)
     _launch("hgca_kv_commit", stream, dev, ctypes.byref(shape), ctypes.byref(kv), _ptr(first), k_in.data_ptr(), v_in.data_ptr(), n,
             _ptr(path), _ptr(cnt), _ptr(lens_out), _ptr(status))
@@ -757,11 +769,11 @@ def kv_commit(shape: Shape, tier: Tier, first, k_in, v_in, lens_out, path=None, 
 
 def kv8_write_tokens(shape: Shape, tier: Kv8Tier, first, k_in, v_in, status=None, stream=None) -> None:
     """k_in / v_in [B,n,Hkv,d] in 8 bits to positions first[b] .. (int32 [B], None: 0)."""
-    B, _, Hkv, d = _heads(shape)
-    dt, dev, n = _torch_dtype(shape), _gpu_of(k_in), int(k_in.shape[1])
+    B, _, Hkv, d, dt = _heads(shape)
+    dev, n = _gpu_of(k_in), k_in.shape[1]
     _need("k_in", k_in, dt, (B, n, Hkv, d), dev)
     _need("v_in", v_in, dt, (B, n, Hkv, d), dev)
-    _optional(dev, ("first", first, (B,)), ("status", status, (1,)))
+    _first_and_status(B, dev, first, status)
     kv8 = _tier_view(tier, B, Hkv, d, torch.uint8, dev)
     _launch("hgca_kv8_write_tokens", stream, dev, ctypes.byref(shape), ctypes.byref(kv8), _ptr(first), k_in.data_ptr(),
             v_in.data_ptr(), n, _ptr(status))
@@ -769,21 +781,21 @@ def kv8_write_tokens(shape: Shape, tier: Kv8Tier, first, k_in, v_in, status=None
 
 def kv8_write_tier(shape: Shape, tier: Kv8Tier, first, src: Tier, max_tokens: int, status=None, stream=None) -> None:
     """Tokens first[b] .. src.seq_lens[b] - 1 of src (max_tokens per sequence at most) in 8 bits to the same positions."""
-    B, _, Hkv, d = _heads(shape)
+    B, _, Hkv, d, dt = _heads(shape)
     dev = _gpu_of(src.k)
-    _optional(dev, ("first", first, (B,)), ("status", status, (1,)))
-    kv8, kv = _tier_view(tier, B, Hkv, d, torch.uint8, dev), _tier_view(src, B, Hkv, d, _torch_dtype(shape), dev)
+    _first_and_status(B, dev, first, status)
+    kv8, kv = _tier_view(tier, B, Hkv, d, torch.uint8, dev), _tier_view(src, B, Hkv, d, dt, dev)
     _launch("hgca_kv8_write_tier", stream, dev, ctypes.byref(shape), ctypes.byref(kv8), _ptr(first), ctypes.byref(kv),
             int(max_tokens), _ptr(status))
 
 
 def kv8_read(shape: Shape, tier: Kv8Tier, first, k_out, v_out, stream=None) -> None:
     """Tokens first[b] .. of an 8-bit tier as rows k_out / v_out [B,n,Hkv,d]; rows of tokens beyond the length stay."""
-    B, _, Hkv, d = _heads(shape)
-    dt, dev, n = _torch_dtype(shape), _gpu_of(k_out), int(k_out.shape[1])
+    B, _, Hkv, d, dt = _heads(shape)
+    dev, n = _gpu_of(k_out), k_out.shape[1]
     _need("k_out", k_out, dt, (B, n, Hkv, d), dev)
     _need("v_out", v_out, dt, (B, n, Hkv, d), dev)
-    _optional(dev, ("first", first, (B,)))
+    _first_and_status(B, dev, first)
     kv8 = _tier_view(tier, B, Hkv, d, torch.uint8, dev)
     _launch("hgca_kv8_read", stream, dev, ctypes.byref(shape), ctypes.byref(kv8), _ptr(first), n, k_out.data_ptr(), v_out.data_ptr())
 
