@@ -76,6 +76,15 @@ __device__ __forceinline__ uint4 load16_stream(const char *p) {
     return r;
 }
 
+// The same for a store: what is written once and is as large as the caches.
+__device__ __forceinline__ void store16_stream(char *p, const uint4 &v) {
+    uint32_t *w = reinterpret_cast<uint32_t *>(p);
+    __builtin_nontemporal_store(v.x, w + 0);
+    __builtin_nontemporal_store(v.y, w + 1);
+    __builtin_nontemporal_store(v.z, w + 2);
+    __builtin_nontemporal_store(v.w, w + 3);
+}
+
 // ---- reductions and prefix sums over lanes -----------------------------------------------------------------
 // A lane shuffle (ds_bpermute) goes through the LDS pipeline: a round trip for each of the six steps of a wave's reduction, which is
 // what short kernels consist of, and LDS issue slots, which is what bounds the score products on the vector units.  Inside a
