@@ -18,12 +18,13 @@ namespace {
 
 constexpr int kKv8Block = 256;
 
-// Rows in full precision are streamed past the caches on their way in and out (codes, which attention reads next, are not): 8 x 4096 tokens of 8
+// Rows in bf16 are streamed past the caches on their way in and out (codes, which attention reads next, are not): 8 x 4096 tokens of 8
 // heads of 128 written and read back 95.5 -> 76.8 us (407 MB, 5.3 TB/s; only in or only out 79 and 80), new tokens 89.2 -> 70.6.
+// (fp32 is not: a lane has 32 bytes, each of its two accesses meets half of a line; 4 x 2000 tokens 34.9 -> 45.4.)
 template <typename T> __device__ __forceinline__ void load8(const char *p, float *f);
 template <> __device__ __forceinline__ void load8<float>(const char *p, float *f) {
-    Elem<float>::expand(load16_stream(p), f);
-    Elem<float>::expand(load16_stream(p + 16), f + 4);
+    Elem<float>::expand(load16(p), f);
+    Elem<float>::expand(load16(p + 16), f + 4);
 }
 template <> __device__ __forceinline__ void load8<bf16_t>(const char *p, float *f) { Elem<bf16_t>::expand(load16_stream(p), f); }
 
@@ -182,8 +183,8 @@ __global__ __launch_bounds__(kKv8Block) void kv8_read_kernel(Kv8ReadArgs a)
                 if constexpr (E == 4) {
                     const FloatPair p0 = kv8_pair_f32<false>(c[u][x].x, scale), p1 = kv8_pair_f32<true>(c[u][x].x, scale);
                     const FloatPair p2 = kv8_pair_f32<false>(c[u][x].y, scale), p3 = kv8_pair_f32<true>(c[u][x].y, scale);
-                    store16_stream(dst, __builtin_bit_cast(uint4, make_float4(p0[0], p0[1], p1[0], p1[1])));
-                    store16_stream(dst + 16, __builtin_bit_cast(uint4, make_float4(p2[0], p2[1], p3[0], p3[1])));
+                    *reinterpret_cast<float4 *>(dst) = make_float4(p0[0], p0[1], p1[0], p1[1]);
+                    *reinterpret_cast<float4 *>(dst + 16) = make_float4(p2[0], p2[1], p3[0], p3[1]);
                 } else {
                     store16_stream(
                         dst, make_uint4(kv8_pair_bf16<false>(c[u][x].x, scale), kv8_pair_bf16<true>(c[u][x].x, scale),

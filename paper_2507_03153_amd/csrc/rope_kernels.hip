@@ -15,15 +15,16 @@ namespace {
 constexpr int kRopeBlock = 256, kRopeWaves = kRopeBlock / kWave;
 
 // 8 adjacent elements as floats, and back with one rounding each.  Streamed stores: 2 x 4096 tokens of 64 + 8 heads 60.0 -> 54.5 us (302 MB,
-// 5.5 TB/s), 2 x 1024 of 32 + 8 heads 10.8 -> 9.7; loads streamed as well 56.0 and 11.0.
+// 5.5 TB/s), 2 x 1024 of 32 + 8 heads 10.8 -> 9.7; loads streamed as well 56.0 and 11.0.  (fp32 is not streamed: a lane
+// has 32 bytes, and each of its two accesses would meet half of a line.)
 template <typename T> struct Eight;
 template <> struct Eight<float> {
     uint4 r[2];
     __device__ __forceinline__ void load(const char *p) { r[0] = load16(p); r[1] = load16(p + 16); }
     __device__ __forceinline__ void expand(float *f) const { Elem<float>::expand(r[0], f); Elem<float>::expand(r[1], f + 4); }
     static __device__ __forceinline__ void store(char *p, const float *f) {
-        store16_stream(p, __builtin_bit_cast(uint4, make_float4(f[0], f[1], f[2], f[3])));
-        store16_stream(p + 16, __builtin_bit_cast(uint4, make_float4(f[4], f[5], f[6], f[7])));
+        *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+        *reinterpret_cast<float4 *>(p + 16) = make_float4(f[4], f[5], f[6], f[7]);
     }
 };
 template <> struct Eight<bf16_t> {
