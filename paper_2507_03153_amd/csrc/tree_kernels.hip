@@ -224,7 +224,7 @@ __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeAr
     for (int r = 0; r < RT; ++r) {
         const float l = rows_sum(st.l[r]);
         if (g == 0) {
-            sh.m[w][16 * r + n] = st.m[r] == -INFINITY ? -INFINITY : -st.shift[r];
+            sh.m[w][16 * r + n] = l == 0.f ? -INFINITY : -st.shift[r];         // nothing seen: l is 0 (with only NaN seen it is NaN)
             sh.l[w][16 * r + n] = l;
         }
     }

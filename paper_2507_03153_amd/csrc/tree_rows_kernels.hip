@@ -296,33 +296,30 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     if constexpr (HALVES) {                      // the two waves of a row: the second one's results by way of the stages
         __syncthreads();                         // which all waves have read
         float *const box = reinterpret_cast<float *>(w % 2 ? s_k1 : s_k0);
-        float *const stats = reinterpret_cast<float *>(s_v0) + 3 * kWave * (w % 2);
+        float *const stats = reinterpret_cast<float *>(s_v0) + 2 * kWave * (w % 2);
         if (half) {
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) box[(16 * dt + r) * kWave + lane] = acc[dt][r];
-            stats[lane] = m;
-            stats[kWave + lane] = shift;
-            stats[2 * kWave + lane] = l;
+            stats[lane] = shift;
+            stats[kWave + lane] = l;
         }
         __syncthreads();
         if (half) return;
-        const float m2 = stats[lane], shift2 = stats[kWave + lane], l2 = stats[2 * kWave + lane];
-        const float to = fminf(m == -INFINITY ? INFINITY : shift, m2 == -INFINITY ? INFINITY : shift2);          // of the larger maximum
-        const float f1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - shift);
-        const float f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - shift2);
-        l = m2 == -INFINITY ? l : fmaf(l2, f2, l * f1);
+        const float shift2 = stats[lane], l2 = stats[kWave + lane];
+        const bool none = l == 0.f, none2 = l2 == 0.f;           // (with only NaN seen l is NaN)
+        const float to = none ? shift2 : none2 ? shift : fminf(shift, shift2);                   // of the larger maximum
+        const float f1 = none ? 0.f : __builtin_amdgcn_exp2f(to - shift), f2 = none2 ? 0.f : __builtin_amdgcn_exp2f(to - shift2);
+        l = none2 ? l : fmaf(l2, f2, l * f1);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float x = box[(16 * dt + r) * kWave + lane];
-                acc[dt][r] = m2 == -INFINITY ? acc[dt][r] : m == -INFINITY ? x : fmaf(x, f2, acc[dt][r] * f1);
+                acc[dt][r] = none2 ? acc[dt][r] : none ? x : fmaf(x, f2, acc[dt][r] * f1);
             }
-        if (m == -INFINITY) l = l2;
-        m = fmaxf(m, m2);
-        shift = m == -INFINITY ? 0.f : to;
+        shift = to;
     }
     // the lane holds columns 32 dt + 8 q + 4 hw .. + 3 of its row
     if (!row_exists) return;
@@ -346,7 +343,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
         if (whole) {
             a.lse[at] = l == 0.f ? -INFINITY : (__builtin_amdgcn_logf(l) - shift) * kLn2;
         } else {
-            a.part_m[at] = m == -INFINITY ? -INFINITY : -shift;
+            a.part_m[at] = l == 0.f ? -INFINITY : -shift;
             a.part_l[at] = l;
         }
     }

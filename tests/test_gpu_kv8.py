@@ -208,6 +208,31 @@ def test_fp32_queries_at_the_ends_of_the_range(gpu):
         check(o, lse, O, L, *bounds(q.astype(np.float64), Kq, Vq, [40], 1.0, 40), "f32")
 
 
+@pytest.mark.parametrize("T", [1, 129, 1217])
+@pytest.mark.parametrize("dtype,d,n,Hq", [("bf16", 128, 1, 4), ("bf16", 64, 12, 2), ("bf16", 128, 20, 2), ("bf16", 64, 70, 2), ("f32", 64, 3, 2)])
+def test_nan_scores_reach_the_result(gpu, dtype, d, n, Hq, T):
+    """A query of NaN, and a key of NaN codes behind a whole number of steps: the rows concerned are NaN, the others as without."""
+    torch, hgca = gpu
+    rng = np.random.default_rng(8)
+    K, V, q = rng.standard_normal((2, 1, T, d)), rng.standard_normal((2, 1, T, d)), rng.standard_normal((2, n, Hq, d))
+    shape = hgca.Shape(hgca.F32 if dtype == "f32" else hgca.BF16, 2, Hq, 1, d, 0.1)
+
+    def run(q, K):
+        tier, _ = tier8(gpu, rng, (K, V), [T, T])
+        o, lse = torch.empty(2, n, Hq, d, device=DEV), torch.empty(2, n, Hq, device=DEV)
+        hgca.kv8_attn(shape, put(torch, q, dtype), tier, o, lse, hgca.kv8_workspace(shape, n, T, DEV))
+        return o.cpu().numpy(), lse.cpu().numpy()
+    good, lse0 = run(q, K)
+    bad_q, bad_k = q.copy(), K.copy()
+    bad_q[0, 0, 1], bad_k[1, 0, T - 1] = np.nan, np.nan
+    with np.errstate(all="ignore"):
+        o, lse = run(bad_q, bad_k)
+    hit = np.zeros((2, n, Hq), bool)
+    hit[0, 0, 1], hit[1] = True, True
+    assert np.isfinite(good).all() and np.isnan(o[hit]).all() and np.isnan(lse[hit]).all()
+    assert np.array_equal(o[~hit], good[~hit]) and np.array_equal(lse[~hit], lse0[~hit])
+
+
 def test_captured_write_and_attention(gpu):
     """A token enters the tier and is attended to in one captured graph, replayed with new tokens and positions."""
     torch, hgca = gpu

@@ -183,6 +183,30 @@ def test_rows_that_are_not_seen_may_hold_anything(gpu, dtype, d, rows):
     assert np.array_equal(o[at][..., rest], good[at][..., rest])
 
 
+@pytest.mark.parametrize("T", [1, 33, 129, 1217])
+@pytest.mark.parametrize("dtype,d,n,Hq", [("bf16", 128, 3, 2), ("bf16", 64, 9, 2), ("bf16", 128, 20, 2), ("bf16", 64, 64, 2), ("f32", 64, 3, 2), ("f32", 128, 20, 2)])
+def test_nan_scores_reach_the_result(gpu, dtype, d, n, Hq, T):
+    """A query of NaN, and a key of NaN where it is the only token of a wave or of a split: the rows concerned are NaN, the others
+    as without it."""
+    torch, hgca = gpu
+    rng, q, K, V = inputs(5, dtype, 2, n, Hq, 1, d, T)
+    bad_q, bad_k = q.copy(), K.copy()
+    bad_q[0, 0, 1] = np.nan                      # one head of one query
+    bad_k[1, 0, T - 1] = np.nan                  # the last draft, which even queries see
+    m = [[1 << max(n - T, 0) | (1 << (n - 1) if i % 2 == 0 else 0) for i in range(n)] for _ in range(2)]
+    shape = hgca.Shape(hgca.F32 if dtype == "f32" else hgca.BF16, 2, Hq, 1, d, 0.1)
+    mask = torch.from_numpy(do.as_int64(m)).to(DEV)
+    run = lambda q, K: call(gpu, shape, put(torch, q, dtype), tier_of(gpu, rng, dtype, K, V, [T, T], 0), mask, "f32")
+    good, lse0 = (x.cpu().numpy() for x in run(q, K))
+    o, lse = (x.cpu().numpy() for x in run(bad_q, bad_k))
+    hit = np.zeros((2, n, Hq), bool)
+    hit[0, 0, 1] = True
+    hit[1, [i for i in range(n) if m[1][i] >> (n - 1) & 1]] = True
+    assert np.isfinite(good).all() and np.isfinite(lse0).all()
+    assert np.isnan(o[hit]).all() and np.isnan(lse[hit]).all()
+    assert np.array_equal(o[~hit], good[~hit]) and np.array_equal(lse[~hit], lse0[~hit])
+
+
 def test_large_scores(gpu):
     """Scores of +-2000: the maximum of a row lies anywhere, and far below it weights are 0."""
     torch, hgca = gpu
