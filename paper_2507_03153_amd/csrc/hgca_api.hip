@@ -283,7 +283,7 @@ int check_rows_call(const hgca_shape *s, const void *q, int32_t n_q, int32_t mos
     int rc = check_shape(s);
     if (rc != HGCA_OK) return rc;
     if ((rc = check_view(s, tier, true)) != HGCA_OK) return rc;
-    if (n_q < 1 || !(s->sm_scale > 0.f) || s->sm_scale > 3.0e38f) return HGCA_ERR_INVALID_ARG;
+    if (n_q < 1 || !(s->sm_scale > 0.f) || s->sm_scale > 2.0e38f) return HGCA_ERR_INVALID_ARG;
     if (n_q > most || tier->cap > kMaxRowsCap || (o_dtype != HGCA_F32 && o_dtype != HGCA_BF16)) return HGCA_ERR_UNSUPPORTED;
     if (s->batch == 0) return HGCA_OK;
     if (!q || !aligned16(q) || !o || !aligned16(o) || !lse) return HGCA_ERR_INVALID_ARG;
@@ -312,6 +312,12 @@ int rows_attention(const hgca_shape *s, const void *q, int32_t n_q, bool kv8, Tr
     a.lse = lse;
     return from_hip(launch_tree_attn(s->dtype, s->head_dim, kv8, a, s->batch, static_cast<hipStream_t>(stream)));
 }
+
+struct Range {
+    uintptr_t at, bytes;
+    Range(const void *p, int64_t n) : at(reinterpret_cast<uintptr_t>(p)), bytes((uintptr_t)n) {}
+    bool meets(const Range &o) const { return at < o.at + o.bytes && o.at < at + bytes; }
+};
 
 // The rows of an 8-bit tier as a view (a table of its own shape checks), and the scales' pointers.
 int check_kv8(const hgca_shape *s, const hgca_kv8_view *k8, hgca_kv_view *rows)
@@ -1504,12 +1510,8 @@ int hgca_qk_norm_rope(const hgca_shape *shape, const void *q_in, int64_t q_token
     for (const void *p : {q_in, k_in, (const void *)q_out, (const void *)k_out})
         if (!p || !aligned16(p)) return HGCA_ERR_INVALID_ARG;
     if (!inv_freq || (q_weight && !aligned16(q_weight)) || (k_weight && !aligned16(k_weight))) return HGCA_ERR_INVALID_ARG;
-    struct Range {
-        uintptr_t at, bytes;
-        bool meets(const Range &o) const { return at < o.at + o.bytes && o.at < at + bytes; }
-    };
     auto range = [&](const void *p, int64_t stride, int64_t row) {
-        return Range{reinterpret_cast<uintptr_t>(p), (uintptr_t)(((tokens - 1) * stride + row) * e)};
+        return Range(p, ((tokens - 1) * stride + row) * e);
     };
     const Range qi = range(q_in, qs, q_row), ki = range(k_in, ks, k_row), qo = range(q_out, q_row, q_row), ko = range(k_out, k_row, k_row);
     if (qo.meets(ko) || qo.meets(ki) || ko.meets(qi)) return HGCA_ERR_INVALID_ARG;
@@ -1565,6 +1567,12 @@ int hgca_kv_commit(const hgca_shape *shape, const hgca_kv_view *tier, const int3
     if (tier->cap > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
     if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
     if (!k_in || !v_in || !aligned16(k_in) || !aligned16(v_in) || !lens_out || lens_out == first) return HGCA_ERR_INVALID_ARG;
+    const int64_t row = shape->head_dim * (shape->dtype == HGCA_BF16 ? 2 : 4), heads = (int64_t)shape->batch * shape->n_kv_heads;
+    if (n_tokens > (int64_t(1) << 32) / heads) return HGCA_ERR_UNSUPPORTED;      // (2^32 rows are 512 GB at least)
+    if (!tier->block_table && tier->cap > 0)
+        for (const void *in : {k_in, v_in})
+            for (const void *rows : {tier->k, tier->v})
+                if (Range(in, heads * n_tokens * row).meets(Range(rows, heads * tier->cap * row))) return HGCA_ERR_INVALID_ARG;
     CommitArgs a{};
     a.tier = to_dev(tier);
     a.first = first;
@@ -1576,7 +1584,7 @@ int hgca_kv_commit(const hgca_shape *shape, const hgca_kv_view *tier, const int3
     a.v_in = static_cast<const char *>(v_in);
     a.n_tokens = n_tokens;
     a.n_kv_heads = shape->n_kv_heads;
-    a.row_bytes = shape->head_dim * (shape->dtype == HGCA_BF16 ? 2 : 4);
+    a.row_bytes = (int32_t)row;
     return from_hip(launch_kv_commit(a, shape->batch, static_cast<hipStream_t>(hip_stream)));
 }
 

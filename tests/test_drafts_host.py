@@ -118,6 +118,11 @@ def test_commit_refusals(hg):
     assert commit(k=None) == commit(v=ODD) == commit(n=-1) == commit(lens=None) == commit(lens=FAKE) == I
     assert commit(kv=view(hg, k=None)) == commit(kv=view(hg, cap=-1)) == I
     assert commit(n=0) == OK and commit(sh=shape(hg, B=0), lens=None) == OK
+    # the drafts are rows of the tier itself: 2 x 2 heads of 64 rows of 256 bytes from FAKE and from `far` on
+    far, rows = FAKE + (1 << 20), 4 * 64 * 256
+    for inside in (FAKE, FAKE + rows - 16, far, far + rows - 16, far - 16):
+        assert commit(kv=view(hg, v=far), k=inside, v=FAKE + (1 << 19)) == commit(kv=view(hg, v=far), k=FAKE + (1 << 19), v=inside) == I
+    assert commit(n=1 << 31 - 1, sh=shape(hg, B=65535), kv=view(hg, cap=0, k=None, v=None)) == hg.ERR_UNSUPPORTED
 
 
 def test_rope_refusals(hg):
