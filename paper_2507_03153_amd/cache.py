@@ -4,6 +4,8 @@ one decode step in the order of the paper's Alg. 2 (attention) and Alg. 1 (manag
 computes: every step is a libhgca call."""
 from __future__ import annotations
 
+from types import SimpleNamespace
+
 import torch
 
 from . import hgca
@@ -53,6 +55,8 @@ class LayerCache:
         # the pool's entries once more in 8 bits (E4M3 with scales), for draft_step: same blocks, table and lengths
         self.pool8 = hgca.Kv8Tier.like(self.pool) if pool8 else None
         self.pool8_lens = torch.zeros(B, **i32)          # tokens of the pool that are there already
+        self.draft_first = torch.zeros(B, **i32)         # the window's lengths before the drafts of a draft_step
+        self._drafts = {}
         # per-step outputs and scratch
         self.o_w, self.lse_w = torch.empty(B, Hq, d, **f32), torch.empty(B, Hq, **f32)
         self.o_s, self.lse_s = torch.empty(B, Hq, d, **f32), torch.empty(B, Hq, **f32)
@@ -133,45 +137,49 @@ class LayerCache:
         self.attend(q, alpha if fused_maw else None)
         self.manage(alpha, beta, maw_done=fused_maw)
 
+    def _draft_buffers(self, n: int) -> SimpleNamespace:
+        """Outputs and workspaces of draft steps of n tokens.  Kept for good: a captured graph may hold their addresses."""
+        if n not in self._drafts:
+            dev = self.k_blocks.device
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError(f"the first draft_step of {n} tokens allocates: make it before the capture")
+            f32 = dict(dtype=torch.float32, device=dev)
+            o = [torch.empty(self.B, n, self.Hq, self.d, **f32) for _ in range(3)]
+            lse = [torch.empty(self.B, n, self.Hq, **f32) for _ in range(3)]
+            make = hgca.kv8_workspace if self.pool8 is not None else hgca.append_workspace
+            self._drafts[n] = SimpleNamespace(o=o, lse=lse, ws=hgca.tree_workspace(self.shape, n, self.win_cap, dev),
+                                              ws_pool=make(self.shape, n, self.pool_cap, dev))
+        return self._drafts[n]
+
     def draft_step(self, q, k_in, v_in, mask=None) -> None:
         """Attention of n drafted tokens per sequence, which join the window for the time being: q [B,n,Hq,d], k_in / v_in
         [B,n,Hkv,d]; bit j of mask[b,i] (int64 [B,n]) = draft i sees draft j (None: all).  They see the whole window, and the whole
         pool, in 8 bits if the cache keeps it so.  Results in o_draft [B,n,Hq,d], lse_draft [B,n,Hq]; `commit` follows."""
-        n = int(q.shape[1])
+        n, sh = int(q.shape[1]), self.shape
         if self.win_cap < (self.win_blocks * self.block_size - 1) + n:
             raise ValueError(f"{n} drafted tokens need win_cap_blocks for l_max - 1 + {n} tokens")
-        if getattr(self, "_draft_n", None) != n:
-            f32 = dict(dtype=torch.float32, device=self.k_blocks.device)
-            self._draft_n = n
-            self.o_draft, self.o_dw, self.o_dp = (torch.empty(self.B, n, self.Hq, self.d, **f32) for _ in range(3))
-            self.lse_draft, self.lse_dw, self.lse_dp = (torch.empty(self.B, n, self.Hq, **f32) for _ in range(3))
-            self.draft_first = torch.zeros_like(self.win_lens)
-            self.ws_tree = hgca.tree_workspace(self.shape, n, self.win_cap, self.k_blocks.device)
-            make = hgca.kv8_workspace if self.pool8 is not None else hgca.append_workspace
-            self.ws_draft_pool = make(self.shape, n, self.pool_cap, self.k_blocks.device)
-        sh = self.shape
+        mine = self._draft_buffers(n)
+        (self.o_draft, o_w, o_p), (self.lse_draft, lse_w, lse_p) = mine.o, mine.lse
         self.draft_first.copy_(self.win_lens)
-        self._drafts = (k_in, v_in)
         hgca.kv_append_tokens(sh, self.state, k_in, v_in)
-        hgca.tree_attn(sh, q, self.window, mask, self.o_dw, self.lse_dw, self.ws_tree)
+        hgca.tree_attn(sh, q, self.window, mask, o_w, lse_w, mine.ws)
         if self.pool8 is not None:
-            hgca.kv8_attn(sh, q, self.pool8, self.o_dp, self.lse_dp, self.ws_draft_pool)
+            self.sync_pool8()
+            hgca.kv8_attn(sh, q, self.pool8, o_p, lse_p, mine.ws_pool)
         else:
-            hgca.append_attn(sh, q, self.pool, False, self.o_dp, self.lse_dp, self.ws_draft_pool)
+            hgca.append_attn(sh, q, self.pool, False, o_p, lse_p, mine.ws_pool)
         merged = hgca.Shape(sh.dtype, sh.batch * n, sh.n_q_heads, sh.n_kv_heads, sh.head_dim, sh.sm_scale)
-        hgca.lse_merge(merged, self.o_dp, self.lse_dp, self.o_dw, self.lse_dw, self.o_draft, self.lse_draft)
+        hgca.lse_merge(merged, o_p, lse_p, o_w, lse_w, self.o_draft, self.lse_draft)
 
-    def commit(self, path, cnt, beta: float) -> None:
-        """Of the last draft_step's tokens those on the accepted path stay in the window: path int32 [B,n], cnt int32 [B].  Then
-        windows that have reached l_max evict (Alg. 1); what left them is stored in 8 bits if the cache keeps that.  The moving
-        averages of the tokens that stay start at 0 (attention weights under a tree mask are not averaged)."""
-        k_in, v_in = self._drafts
+    def commit(self, k_in, v_in, path, cnt, beta: float) -> None:
+        """Of the last draft_step's tokens (its k_in, v_in) those on the accepted path stay in the window: path int32 [B,n], cnt
+        int32 [B].  Then windows that have reached l_max evict (Alg. 1).  The moving averages of the tokens that stay start at 0
+        (attention weights under a tree mask are not averaged)."""
         hgca.kv_commit(self.shape, self.window, self.draft_first, k_in, v_in, self.win_lens, path=path, cnt=cnt, status=self.status)
         hgca.kv_evict(self.shape, self.state, beta)
-        self.sync_pool8()
 
     def sync_pool8(self) -> None:
-        """Stores in 8 bits what the pool has got since the last call (after any step that may evict)."""
+        """Stores in 8 bits what the pool has got since the last call; a draft_step begins with it."""
         if self.pool8 is None:
             return
         hgca.kv8_write_tier(self.shape, self.pool8, self.pool8_lens, self.pool, self.pool_cap)

@@ -70,7 +70,7 @@ def run(gpu, dtype, pool8, rounds=10, seed=0):
             if dtype == "bf16" and not pool8:    # the append stage's weights have two parts: 2^-17 each
                 tol_o += 2.0 ** -16 * np.abs(V).max()
             assert eo <= tol_o and el <= tol_l, f"round {r} sequence {b}: dO={eo} of {tol_o}, dlse={el} of {tol_l}"
-        C.commit(i32(torch, path), i32(torch, cnt), beta=1.0)
+        C.commit(kd, v, i32(torch, path), i32(torch, cnt), beta=1.0)
         torch.cuda.synchronize()
         for b in range(B):
             rows[b] += [(kh[b, i], vh[b, i]) for i in path[b, :cnt[b]]]
@@ -122,3 +122,52 @@ def test_decode_steps_and_draft_steps_take_turns(gpu):
     for back, blocks in ((ko, C.k_blocks), (vo, C.v_blocks)):
         x = blocks[C.block_table[:, :L // 16].long()].permute(0, 1, 3, 2, 4).reshape(B, L, Hkv, d).float().cpu().numpy()
         assert np.array_equal(back.double().cpu().numpy(), do.decode(*do.encode(x)))
+
+
+def test_captured_draft_steps(gpu):
+    """Two graphs, of draft steps and commits with 3 and with 5 tokens, replayed in turn with eager steps between: each as the same
+    steps on a cache without graphs.  A first step inside a capture is refused."""
+    torch, hgca = gpu
+    from paper_2507_03153_amd.cache import LayerCache
+    B, Hq, Hkv, d = 2, 4, 2, 64
+    make = lambda: LayerCache(torch.bfloat16, B, Hq, Hkv, d, 16, 2, 16, 16, 0.125, DEV, win_cap_blocks=3, pool8=True)
+    G, E = make(), make()
+    bf = dict(dtype=torch.bfloat16, device=DEV)
+    ins = {n: [torch.zeros(B, n, h, d, **bf) for h in (Hq, Hkv, Hkv)] for n in (3, 5)}
+    mask = {n: torch.tensor([[(2 << i) - 1 for i in range(n)]] * B, dtype=torch.int64, device=DEV) for n in ins}
+    path = {n: torch.arange(n, dtype=torch.int32, device=DEV).expand(B, n).contiguous() for n in ins}
+    cnt = torch.tensor([2, 3], dtype=torch.int32, device=DEV)
+
+    def step(C, n):
+        q, k, v = ins[n]
+        C.draft_step(q, k, v, mask[n])
+        C.commit(k, v, path[n], cnt, 1.0)
+    fresh = make()
+    with pytest.raises(RuntimeError, match="before the capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            step(fresh, 3)
+    torch.cuda.synchronize()
+    graphs, outs = {}, {}
+    for n in ins:
+        step(G, n)
+        step(E, n)
+    torch.cuda.synchronize()
+    for n in ins:
+        graphs[n] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[n]):
+            step(G, n)
+        outs[n] = G.o_draft
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for r in range(24):
+        n = (3, 5)[r % 2]
+        for t in ins[n]:
+            t.copy_(torch.randn(t.shape, generator=gen, **bf))
+        if r % 5 == 4:
+            step(G, n)
+        else:
+            graphs[n].replay()
+        step(E, n)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[n], E.o_draft) and torch.equal(G.lse_draft if r % 5 == 4 else G._drafts[n].lse[0], E.lse_draft)
+        assert torch.equal(G.win_lens, E.win_lens) and torch.equal(G.pool_lens, E.pool_lens) and G.status.item() == 0
+    assert G.pool_lens.max() > 0
