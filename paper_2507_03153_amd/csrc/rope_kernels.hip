@@ -4,6 +4,9 @@
 // Everything between the load and the one rounding of the result is fp32, the angle fp64: a position of a million times a
 // frequency near 1 has no digits left in fp32 (its fraction of a turn would be off by 2^-4); the fp64 product is brought into
 // half a turn before it becomes fp32.
+//
+// Bound by memory, each row read and written once: 2 x 4096 tokens of 64 + 8 heads of 128 52.5 us, 302 MB at 5.75 TB/s (a large
+// copy: 5.16); one token x 8 sequences of 32 + 8 heads 3.5 us, the launch and a load's way.
 #include <algorithm>
 
 #include "hgca_launch.hpp"

@@ -19,7 +19,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // The part of a sequence's tokens that a workgroup goes through.  With one split per sequence it is the whole; else the launch has
 // batch * n_splits slots per KV head and block of rows.  Up to 64 sequences take as many of them as their own lengths ask for:
 // slots of C whole steps, C about the least with which all sequences' slots are enough.  (With n_splits slots for every
-// sequence the longest one sets the time.)  Every wave works the cut out for itself, a lane per sequence; a
+// sequence the longest one sets the time: 16 queries x 4 over 61 to 122 K tokens 431 : 345 to 390 us.)  Every wave works the cut out for itself, a lane per sequence; a
 // sequence without tokens takes a slot too.  More sequences fill the device with a few slots each: n_splits equal ones.
 struct Span {
     int b, len, begin, end;
