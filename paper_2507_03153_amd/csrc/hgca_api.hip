@@ -264,7 +264,8 @@ struct TreeLayout {
 TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, bool kv8, int32_t cap)
 {
     TreeLayout t{};
-    const int64_t rows = (int64_t)n_q * group_of(s), per_block = tree_block_rows(s->dtype, kv8, (int)rows);
+    const int64_t rows = (int64_t)n_q * group_of(s), tokens = (int64_t)s->batch * s->n_kv_heads * cap;
+    const int64_t per_block = tree_block_rows(s->dtype, kv8, s->head_dim, (int)rows, tokens);
     t.row_blocks = (int32_t)((rows + per_block - 1) / per_block);
     const int64_t units = std::max<int64_t>(1, (int64_t)s->batch * s->n_kv_heads * t.row_blocks);
     const int64_t most = cap <= (per_block > 32 ? HGCA_TREE_MIN : HGCA_TREE_WHOLE) ? 1 : ((int64_t)cap + HGCA_TREE_MIN - 1) / HGCA_TREE_MIN;

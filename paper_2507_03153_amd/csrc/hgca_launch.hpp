@@ -315,8 +315,8 @@ struct TreeArgs {
     void *o;                   // [B, n_q, Hq, d]
     float *lse;                // [B, n_q, Hq]
 };
-// rows of a workgroup, for `rows` query rows per KV head
-int tree_block_rows(int dtype, bool kv8, int rows);
+// rows of a workgroup, for `rows` query rows per KV head, over up to `tokens` tokens of all sequences and KV heads
+int tree_block_rows(int dtype, bool kv8, int head_dim, int rows, int64_t tokens);
 // kv8: the tier is in 8 bits (dtype is that of q); row_blocks = blocks of tree_block_rows() rows.  The splits, and their fold
 // where there are several.
 hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s);

@@ -1,4 +1,4 @@
-// What the kernels that attend with a few queries per sequence share (tree_kernels.hip: up to 32 rows per KV head and fp32,
+// What the kernels that attend with a few queries per sequence share (tree_kernels.hip: few rows per KV head and fp32,
 // tree_rows_kernels.hip: more).
 #pragma once
 

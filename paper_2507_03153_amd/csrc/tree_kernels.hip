@@ -1,4 +1,4 @@
-// Attention of a few queries per sequence over one tier (more than 32 rows in bf16: tree_rows_kernels.hip): drafted tokens that
+// Attention of a few queries per sequence over one tier (in bf16 with more than 32 rows, in part 16: tree_rows_kernels.hip): drafted tokens that
 // are verified together, each of which sees the conversation and its own ancestors among the drafts (the tier's last n tokens, a
 // bit per draft), and queries over an 8-bit tier.  A row is one query of one head of the group that shares a KV head; a launch
 // reads K and V once per 16 or 32 rows.
@@ -697,7 +697,7 @@ template <typename S, typename TQ, int D, int RT>
 void launch_rows(const TreeArgs &a, dim3 grid, int batch, hipStream_t s)
 {
     const dim3 block(kTreeBlock);
-    if constexpr (sizeof(TQ) == 2) {
+    if constexpr (sizeof(TQ) == 2 && !(sizeof(S) == 2 && D == 128 && RT == 2)) {       // (tree_block_rows takes that much elsewhere)
         // (fp32 queries take their rows in blocks of 16, which read K and V again)
         if (a.row_blocks == 1 && (int64_t)batch * a.sh.n_kv_heads * a.kv.cap * D * (int)sizeof(S) * 2 >= kLastCache) {
             if (a.o_bf16) hipLaunchKernelGGL((rows_attn_kernel<S, TQ, D, RT, 2, true>), grid, block, 0, s, a);
@@ -711,15 +711,21 @@ void launch_rows(const TreeArgs &a, dim3 grid, int batch, hipStream_t s)
 
 }  // namespace
 
-int tree_block_rows(int dtype, bool kv8, int rows)
+int tree_block_rows(int dtype, bool kv8, int head_dim, int rows, int64_t tokens)
 {
     if (rows <= 16 || (dtype == 0 && kv8)) return 16;
-    return rows <= 32 || dtype == 0 ? 32 : kRowsPerBlock;
+    if (dtype == 0) return 32;
+    // 17 to 32 rows: with steps through LDS half of the waves have no rows, but those of this file spill registers over bf16 heads
+    // of 128.  This file : LDS, 8 drafts in groups of 4, us: 8 x 16384 tokens of 8 heads 111 : 95.5, 8 x 4096 36.4 : 33.1, 64 x 300 25.1 :
+    // 21.5, 1 x 60000 68.5 : 61.6; 2 x 4096 19.2 : 19.8, 1 x 1000 14.7 : 16.8.  Heads of 64: 20.2 : 21.4 at 8 x 4096; 8 bits 67.7 : 75.9 at 8 x 16384.
+    const bool lds = rows > 32 || (!kv8 && head_dim == 128 && tokens >= int64_t(1) << 17);
+    return lds ? kRowsPerBlock : 32;
 }
 
 hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s)
 {
-    const int block_rows = tree_block_rows(dtype, kv8, a.n_q * a.sh.group), rt = block_rows / 16;
+    const int block_rows = tree_block_rows(dtype, kv8, head_dim, a.n_q * a.sh.group, (int64_t)batch * a.sh.n_kv_heads * a.kv.cap);
+    const int rt = block_rows / 16;
     const dim3 grid((unsigned)((int64_t)batch * a.n_splits * a.row_blocks), (unsigned)a.sh.n_kv_heads);
 #define HGCA_TREE_RT(S, D)                                               \
     do {                                                                 \

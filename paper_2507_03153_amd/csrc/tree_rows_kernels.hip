@@ -1,5 +1,5 @@
-// Attention of a few queries per sequence over one tier, 33 query rows and more per KV head (bf16 queries; a row is one query
-// of one head of the group): drafted tokens with a mask over a bf16 tier, and queries over an 8-bit tier.
+// Attention of a few queries per sequence over one tier, 33 query rows and more per KV head, 17 and more over many tokens with heads of
+// 128 (tree_block_rows; bf16 queries; a row is one query of one head of the group): drafted tokens with a mask over a bf16 tier, and queries over an 8-bit tier.
 //
 // Work unit: one workgroup = a split of the tokens of one (sequence, KV head) and up to 128 rows, 32 per wave.  K and V of a 64-token
 // step go through a double-buffered LDS stage that all four waves read.  bf16 rows arrive by LDS-direct loads; 8-bit rows are loaded to

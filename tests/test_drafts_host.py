@@ -69,7 +69,7 @@ def test_tree_refusals(hg):
 def test_workspace_serves_smaller_capacities(hg):
     L = hg.lib()
     for B, Hq, Hkv in ((1, 4, 4), (3, 32, 8), (64, 64, 8)):
-        for n in (1, 3, 16, 64):
+        for n in (1, 3, 5, 8, 16, 64):
             sh = shape(hg, B=B, Hq=Hq, Hkv=Hkv)
             for f in (L.hgca_tree_workspace_bytes, L.hgca_kv8_workspace_bytes):
                 sizes = [f(ctypes.byref(sh), n, c) for c in (0, 1, 127, 128, 129, 1000, 4096, 100000)]

@@ -137,6 +137,24 @@ def test_against_64_bits(gpu, dtype, d, Hq, Hkv, n, block, out, lens, masks):
     check(o, lse, O, L, *bounds(q, K, V, lens, scale, T), out)
 
 
+@pytest.mark.parametrize("B,T,n,block,out", [(64, 1024, 6, 16, "f32"), (64, 1008, 6, 0, "f32"), (64, 1024, 5, 0, "bf16"), (1, 65541, 8, 48, "f32")])
+def test_17_to_32_rows_over_many_tokens(gpu, B, T, n, block, out):
+    """Both sides of 2^17 tokens of all sequences and KV heads, where heads of 128 change kernels; lengths from none to all."""
+    torch, hgca = gpu
+    Hq, Hkv, d = 8, 2, 128
+    rng, q, K, V = inputs(B + T + n, "bf16", B, n, Hq, Hkv, d, T)
+    lens = [T] + [int(x) for x in rng.integers(0, T + 1, B - 1)]
+    lens[1:4] = [0, 1, n + 1][:B - 1]
+    m = [do.ancestors(rng, n) for _ in range(B)]
+    for b, L in enumerate(lens):
+        K[b, :, L:], V[b, :, L:] = np.nan, np.inf
+    scale = float(np.float32(d ** -0.5))
+    tier = tier_of(gpu, rng, "bf16", K, V, lens, block)
+    o, lse = call(gpu, hgca.Shape(hgca.BF16, B, Hq, Hkv, d, scale), put(torch, q, "bf16"), tier, torch.from_numpy(do.as_int64(m)).to(DEV), out)
+    O, L = do.rows_attention(q.astype(np.float64), K.astype(np.float64), V.astype(np.float64), lens, scale, m)
+    check(o, lse, O, L, *bounds(q, K, V, lens, scale, T), out)
+
+
 def test_empty_prefix_and_empty_rows(gpu):
     """Nothing but drafted tokens, a query without any bit."""
     torch, hgca = gpu
