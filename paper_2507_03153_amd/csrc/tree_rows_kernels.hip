@@ -259,8 +259,8 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     const int total = span.end - span.begin, sub_len = pass_length(a.kv, total);
     for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
         const int nsub = min(sub_len, total - sub0), first = span.begin + sub0, steps = (nsub + kStepTokens - 1) / kStepTokens;
-        // steps that end before the drafted tokens and the end need no mask
-        const int plain = max(min(tail, span.end) - first, 0) / kStepTokens;
+        // steps of the pass that end before the drafted tokens and the end need no mask
+        const int plain = max(min(min(tail, span.end) - first, nsub), 0) / kStepTokens;
         __syncthreads();                         // the previous table and stages are no longer in use
         const BlockRows where = make_block_rows<kTreeBlock>(s_row, a.kv, a.sh.n_kv_heads, b, kvh, first, nsub);
         CodesInFlight<kCodes ? D : 64> codes;

@@ -268,6 +268,44 @@ def test_a_long_sequence_among_short_ones(gpu):
         check(o[b:b + 1], lse[b:b + 1], O, Ls, *bounds(q[b:b + 1], K, V, [L], 0.125, max(L, 1)), "f32")
 
 
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("n,Hq,d", [(4, 8, 128), (5, 8, 128), (12, 8, 128), (20, 8, 64), (40, 16, 128)])
+def test_several_tables_per_workgroup(gpu, n, Hq, d, kv8):
+    """Sequences that are one workgroup's work per KV head and longer than the tables of two passes (8192 tokens each), for every number of
+    rows per workgroup."""
+    torch, hgca = gpu
+    B, T, bs = 150, 17000, 16
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 40, B).astype(np.int32)
+    lens[17], lens[3], lens[149] = T, 2 * 8192, 8193
+    n_blk = [-(-int(x) // bs) for x in lens]
+    total = sum(n_blk)
+    table = np.zeros((B, -(-T // bs)), np.int32)
+    perm, at = rng.permutation(total).astype(np.int32), 0
+    for b, x in enumerate(n_blk):
+        table[b, :x] = perm[at:at + x]
+        at += x
+    kb, vb = (do.to_bf16(rng.standard_normal((total, 2, bs, d))) for _ in range(2))
+    q = do.to_bf16(rng.standard_normal((B, n, Hq, d)))
+    shape = hgca.Shape(hgca.BF16, B, Hq, 2, d, 0.125)
+    rest = (T, i32(torch, lens), i32(torch, table), bs)
+    if kv8:
+        (kc, ks), (vc, vs) = do.encode(kb), do.encode(vb)
+        kb, vb, m = do.decode(kc, ks), do.decode(vc, vs), None
+        o, lse = torch.empty(B, n, Hq, d, device=DEV), torch.empty(B, n, Hq, device=DEV)
+        hgca.kv8_attn(shape, put(torch, q, "bf16"), hgca.Kv8Tier(*(torch.from_numpy(x).to(DEV) for x in (kc, vc, ks, vs)), *rest), o, lse,
+                      hgca.kv8_workspace(shape, n, T, DEV))
+    else:
+        m = [do.ancestors(rng, n) for _ in range(B)]
+        o, lse = call(gpu, shape, put(torch, q, "bf16"), hgca.Tier(put(torch, kb, "bf16"), put(torch, vb, "bf16"), *rest),
+                      torch.from_numpy(do.as_int64(m)).to(DEV), "f32")
+    for b in (3, 17, 18, 149):
+        L = int(lens[b])
+        K, V = (np.concatenate([x[i] for i in table[b, :n_blk[b]]] or [np.zeros((2, 0, d))], 1)[None, :, :L] for x in (kb, vb))
+        O, Ls = do.rows_attention(q[b:b + 1].astype(np.float64), K.astype(np.float64), V.astype(np.float64), [L], 0.125, None if m is None else m[b:b + 1])
+        check(o[b:b + 1], lse[b:b + 1], O, Ls, *bounds(q[b:b + 1], K, V, [L], 0.125, max(L, 1)), "f32")
+
+
 @pytest.mark.parametrize("dtype,B,n,Hq,Hkv,lens", [
     ("bf16", 130, 2, 4, 1, "ragged"),            # a lane has several sequences
     ("f32", 70, 3, 2, 1, "ragged"),
