@@ -39,8 +39,9 @@ struct Span {
         } else {
             const int lane = threadIdx.x % kWave, slots = B * a.n_splits;
             const int tokens = lane < B ? tier_len(a.kv, lane) : 0, steps = lane < B ? max((tokens + unit - 1) / unit, 1) : 0;
-            auto counts = [&](int c) {           // ceil(steps / c): the quotient in fp32 is off by one at most, downwards
-                const int n = (int)((float)steps * __builtin_amdgcn_rcpf((float)c) * 0.999999f);
+            auto counts = [&](int c) {           // ceil(steps / c): c is at least total / slots, so it is 1024 at most, and the
+                int n = (int)((float)steps * __builtin_amdgcn_rcpf((float)c) * 0.999999f);       // quotient in fp32 off by one, downwards
+                n += n * c < steps ? 1 : 0;
                 return n + (n * c < steps ? 1 : 0);
             };
             auto enough = [&](int c) { return wave_sum((float)min(counts(c), slots + 1)) <= (float)slots; };     // whole numbers below 2^24
