@@ -245,8 +245,18 @@ constexpr int32_t kMaxRowsCap = 1 << 30;         // positions and step counts of
 constexpr int32_t kMaxKv8Queries = 4096;
 
 // Splits per (sequence, KV head, block of rows) whose tier holds up to `cap` tokens, on average over the sequences (Span): about
-// 512 workgroups, a round of the two that a compute unit holds, of 256 tokens at least; a tier of up to 512 tokens (256, with
-// more than 32 rows per workgroup) is not split, which saves the fold's launch.
+// 512 workgroups, a round of the two that a compute unit holds, of 256 tokens at least.  256 : 512 : 1024 workgroups, us: one token x 8
+// over 28 K tokens in 8 bits 102.6 : 84.6 : 89.3, 64 drafts x 4 over 32 K in groups of 8 428 : 392 : 406, 32 drafts x 8 over 4 K
+// 49.8 : 50.7 : 66.4.  Kernels whose workgroup takes 64 tokens a step (fp32 tiers, more than 32 rows) get by with 128 as long
+// as there is not a workgroup per unit: 8 fp32 drafts over 1000 tokens 20.7 : 16.6, 32 in bf16 19.7 : 17.0 (with more
+// workgroups than that, 8 fp32 drafts x 4 over 2000 23.7 : 27.8).
+//
+// One split saves the partials and the fold's launch.  Split : whole, us: up to 512 tokens, 4 drafts over 500 11.7 : 9.2; up to 256 with more
+// than 32 rows per workgroup, 32 over 256 15.5 : 14.5, over 300 13.0 : 14.9; fp32 by the work of a token, 512 tokens for
+// 16 rows of 64 columns (500 12.4 : 10.3), 320 of 128 (320 12.6 : 12.2, 400 12.8 : 14.9), 160 for 32 rows (256 16.1 : 16.8, 330 16.1 : 21.1).
+// Where there is a workgroup for every other unit without splits, longer tiers too: 256 units, 32 drafts over 600 / 1000 / 2000 / 4000 tokens
+// 50.8 : 31.5, 64.1 : 49.0, 98.8 : 87.4, 155.7 : 155.7, 4 over 2000 57.2 : 52.5, 12 over 4000 108 : 112; 160 units, 32 over 1600 61.1 : 54.8,
+// 12 39.5 : 40.6; 8 bits, 256 units, 2 queries over 1000 / 2000 19.8 : 17.3, 29.6 : 31.7, 160 units, 16 over 800 / 1600 29.1 : 26.9, 37.5 : 43.4.
 #ifndef HGCA_TARGET_WGS_TREE
 #define HGCA_TARGET_WGS_TREE 512
 #endif
@@ -268,8 +278,16 @@ TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, bool kv8, int32_t cap)
     const int64_t per_block = tree_block_rows(s->dtype, kv8, s->head_dim, (int)rows, tokens);
     t.row_blocks = (int32_t)((rows + per_block - 1) / per_block);
     const int64_t units = std::max<int64_t>(1, (int64_t)s->batch * s->n_kv_heads * t.row_blocks);
-    const int64_t most = cap <= (per_block > 32 ? HGCA_TREE_MIN : HGCA_TREE_WHOLE) ? 1 : ((int64_t)cap + HGCA_TREE_MIN - 1) / HGCA_TREE_MIN;
-    t.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HGCA_TARGET_WGS_TREE / units, most));
+    auto splits = [&](int64_t workgroups, int64_t tokens) {
+        return std::max<int64_t>(1, std::min<int64_t>(workgroups / units, ((int64_t)cap + tokens - 1) / tokens));
+    };
+    const bool short_steps = (s->dtype == HGCA_F32 && !kv8) || per_block > 32;
+    int64_t whole = per_block > 32 ? HGCA_TREE_MIN : HGCA_TREE_WHOLE;
+    if (units >= HGCA_TARGET_WGS_TREE / 4) whole = (kv8 ? 5 : 8) * units;
+    else if (s->dtype == HGCA_F32 && !kv8) whole = std::min<int64_t>(whole, 640 * 16 * 64 / (per_block * s->head_dim));
+    if (cap <= whole) t.n_splits = 1;
+    else t.n_splits = (int32_t)std::max(splits(HGCA_TARGET_WGS_TREE, HGCA_TREE_MIN),
+                                        short_steps ? splits(HGCA_TARGET_WGS_TREE / 2, HGCA_TREE_MIN / 2) : 1);
     const size_t parts = t.n_splits > 1 ? (size_t)s->batch * n_q * s->n_q_heads * t.n_splits : 0;
     t.part_m = align_up(parts * s->head_dim * sizeof(float));
     t.part_l = t.part_m + align_up(parts * sizeof(float));
