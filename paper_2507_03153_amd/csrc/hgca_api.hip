@@ -249,7 +249,10 @@ constexpr int32_t kMaxKv8Queries = 4096;
 // over 28 K tokens in 8 bits 102.6 : 84.6 : 89.3, 64 drafts x 4 over 32 K in groups of 8 428 : 392 : 406, 32 drafts x 8 over 4 K
 // 49.8 : 50.7 : 66.4.  Kernels whose workgroup takes 64 tokens a step (fp32 tiers, more than 32 rows) get by with 128 as long
 // as there is not a workgroup per unit: 8 fp32 drafts over 1000 tokens 20.7 : 16.6, 32 in bf16 19.7 : 17.0 (with more
-// workgroups than that, 8 fp32 drafts x 4 over 2000 23.7 : 27.8).
+// workgroups than that, 8 fp32 drafts x 4 over 2000 23.7 : 27.8).  Splits of up to 512 tokens are not halved for a second workgroup per unit if
+// the first ones nearly fill the device and rows have 256 bytes, or a row would have more than 32 partials: 512 : 256 workgroups, 8 KV heads,
+// 4 drafts over 16000 tokens 23.1 : 20.4, in fp32 33.7 : 29.9, 32 drafts 34.8 : 31.4, x 8 over 2000 36.3 : 33.8, 2 queries over 16000 in 8 bits
+// 19.4 : 18.1 (x 8 over 2000 14.0 : 15.8; 192 workgroups, 16 queries x 12 over 2000 31.3 : 36.6; 1024 tokens, 16 x 8 over 4096 35.5 : 36.7).
 //
 // One split saves the partials and the fold's launch.  Split : whole, us: up to 512 tokens, 4 drafts over 500 11.7 : 9.2; up to 256 with more
 // than 32 rows per workgroup, 32 over 256 15.5 : 14.5, over 300 13.0 : 14.9; fp32 by the work of a token, 512 tokens for
@@ -285,9 +288,11 @@ TreeLayout tree_layout(const hgca_shape *s, int32_t n_q, bool kv8, int32_t cap)
     int64_t whole = per_block > 32 ? HGCA_TREE_MIN : HGCA_TREE_WHOLE;
     if (units >= HGCA_TARGET_WGS_TREE / 4) whole = (kv8 ? 5 : 8) * units;
     else if (s->dtype == HGCA_F32 && !kv8) whole = std::min<int64_t>(whole, 640 * 16 * 64 / (per_block * s->head_dim));
-    if (cap <= whole) t.n_splits = 1;
-    else t.n_splits = (int32_t)std::max(splits(HGCA_TARGET_WGS_TREE, HGCA_TREE_MIN),
-                                        short_steps ? splits(HGCA_TARGET_WGS_TREE / 2, HGCA_TREE_MIN / 2) : 1);
+    int64_t n = std::max(splits(HGCA_TARGET_WGS_TREE, HGCA_TREE_MIN), short_steps ? splits(HGCA_TARGET_WGS_TREE / 2, HGCA_TREE_MIN / 2) : 1);
+    const int64_t one_round = HGCA_TARGET_WGS_TREE / 2 / units;
+    const bool wide = s->head_dim * (kv8 ? 1 : s->dtype == HGCA_BF16 ? 2 : 4) >= 256;
+    if ((wide || one_round >= 32) && one_round * units >= HGCA_TARGET_WGS_TREE / 2 - 16 && cap <= 512 * one_round) n = std::min(n, one_round);
+    t.n_splits = cap <= whole ? 1 : (int32_t)n;
     const size_t parts = t.n_splits > 1 ? (size_t)s->batch * n_q * s->n_q_heads * t.n_splits : 0;
     t.part_m = align_up(parts * s->head_dim * sizeof(float));
     t.part_l = t.part_m + align_up(parts * sizeof(float));
