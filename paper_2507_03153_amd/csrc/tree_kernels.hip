@@ -642,13 +642,18 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
 
 // The splits of a row: M = max m_s, O = sum o_s 2^{m_s - M} / sum l_s 2^{m_s - M}.  A wave per row; 16 or 32 lanes across the columns,
 // the others take further splits.  Bound by two round trips to memory and the partials: 8192 rows of 128 in 8 splits 8.6 us (34 MB, 3.9
-// TB/s), 256 rows in 16 splits 4.6 us.
-template <int D> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(TreeArgs a, int64_t rows)
+// TB/s), 256 rows in 16 splits 4.6 us.  Few rows in many splits are loads one after another: they take a workgroup per row.  Wave :
+// workgroup, whole calls, us: 4 rows in 128 splits 38.1 : 30.1 (120 K tokens in 8 bits), 32 in 64 31.9 : 27.8, 128 in 32 23.9 : 22.0, 40
+// in 16 18.4 : 18.0; 2048 rows in 32 87.2 : 89.2.
+template <int D, int WAVES> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(TreeArgs a, int64_t rows)
 {
     constexpr int C4 = D / 4, SG = kWave / C4, PRE = 4;
-    const int lane = threadIdx.x % kWave, sg = lane / C4, c4 = lane % C4;
-    const int64_t row = (int64_t)blockIdx.x * kTreeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    if (row >= rows) return;
+    __shared__ float4 s_x[WAVES > 1 ? WAVES : 1][WAVES > 1 ? C4 : 1];
+    __shared__ float s_l[WAVES];
+    const int lane = threadIdx.x % kWave, sg = lane / C4, c4 = lane % C4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t row = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kTreeWaves + wave;
+    const int w = WAVES > 1 ? wave : 0;          // of the row's waves
+    if (row >= rows) return;                     // (with several waves per row there are as many workgroups as rows)
     const int h = (int)(row % a.sh.n_q_heads), i = (int)(row / a.sh.n_q_heads % a.n_q), b = (int)(row / a.sh.n_q_heads / a.n_q);
     const int first = a.seq_slots[2 * b], S = a.seq_slots[2 * b + 1];
     const int64_t at = partial_row(a, first, h / a.sh.group, i * a.sh.group + h % a.sh.group);
@@ -659,19 +664,19 @@ template <int D> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(
     M = wave_max(M);
     float L = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = sg; s0 < S; s0 += SG * PRE) {
+    for (int s0 = w * SG + sg; s0 < S; s0 += WAVES * SG * PRE) {
         float pm[PRE], pl[PRE];
         float4 po[PRE];
 #pragma unroll
         for (int i = 0; i < PRE; ++i) {
-            const int64_t s = min(s0 + i * SG, S - 1) * stride;
+            const int64_t s = min(s0 + i * WAVES * SG, S - 1) * stride;
             pm[i] = m[s];
             pl[i] = l[s];
             po[i] = *reinterpret_cast<const float4 *>(o + s * D);
         }
 #pragma unroll
         for (int i = 0; i < PRE; ++i) {
-            if (s0 + i * SG >= S || pm[i] == -INFINITY) continue;
+            if (s0 + i * WAVES * SG >= S || pm[i] == -INFINITY) continue;
             const float f = __builtin_amdgcn_exp2f(pm[i] - M);
             L = fmaf(pl[i], f, L);
             x.x = fmaf(po[i].x, f, x.x);
@@ -682,6 +687,18 @@ template <int D> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(
     }
     L = strided_sum<C4>(L);
     x = make_float4(strided_sum<C4>(x.x), strided_sum<C4>(x.y), strided_sum<C4>(x.z), strided_sum<C4>(x.w));
+    if constexpr (WAVES > 1) {
+        if (sg == 0) s_x[w][c4] = x;
+        if (lane == 0) s_l[w] = L;
+        __syncthreads();
+        if (w != 0) return;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) {
+            const float4 y = s_x[i][c4];
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+            L += s_l[i];
+        }
+    }
     if (sg != 0) return;
     const float inv = 1.f / L;
     if (L == 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -754,9 +771,12 @@ hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess || a.n_splits == 1) return rc;
     const int64_t rows = (int64_t)batch * a.n_q * a.sh.n_q_heads;
-    const dim3 fold((unsigned)((rows + kTreeWaves - 1) / kTreeWaves));
-    if (head_dim == 64) hipLaunchKernelGGL((rows_fold_kernel<64>), fold, dim3(kTreeBlock), 0, s, a, rows);
-    else hipLaunchKernelGGL((rows_fold_kernel<128>), fold, dim3(kTreeBlock), 0, s, a, rows);
+    const bool several = a.n_splits >= 16 && rows <= 1024;
+    const dim3 fold((unsigned)(several ? rows : (rows + kTreeWaves - 1) / kTreeWaves)), block(kTreeBlock);
+    if (head_dim == 64 && several) hipLaunchKernelGGL((rows_fold_kernel<64, kTreeWaves>), fold, block, 0, s, a, rows);
+    else if (head_dim == 64) hipLaunchKernelGGL((rows_fold_kernel<64, 1>), fold, block, 0, s, a, rows);
+    else if (several) hipLaunchKernelGGL((rows_fold_kernel<128, kTreeWaves>), fold, block, 0, s, a, rows);
+    else hipLaunchKernelGGL((rows_fold_kernel<128, 1>), fold, block, 0, s, a, rows);
     return hipGetLastError();
 }
 
