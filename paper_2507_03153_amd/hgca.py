@@ -679,7 +679,8 @@ def _token_stride(name: str, t: torch.Tensor) -> int:
     """Elements between consecutive tokens of [B,n,H,d], whose heads lie side by side."""
     (B, n, H, d), (s0, s1, s2, s3) = t.shape, t.stride()
     step = s1 if n > 1 else s0 if B > 1 else H * d
-    if s3 != 1 or (s2 != d and H > 1) or (s0 != n * step and B > 1 and n > 1):
+    # (an expanded tensor's distance is 0, which the library takes as rows one behind the other)
+    if s3 != 1 or (s2 != d and H > 1) or (s0 != n * step and B > 1 and n > 1) or (step < H * d and B * n > 1):
         raise ValueError(f"{name}: heads have to lie side by side and tokens at one distance")
     return step
 
