@@ -644,7 +644,8 @@ int hgca_qk_norm_rope(const hgca_shape *shape,
  * q is [B, n_q, Hq, d]; o_out [B, n_q, Hq, d] in o_dtype, lse_out fp32 [B, n_q, Hq]; a
  * query that sees nothing gives O = 0, lse = -inf.  A row that a query does not see has
  * no part in its O, whatever the row holds (with draft_mask; without it all queries see
- * all valid rows).  fp32 O is accurate to fp32: weights enter the second product
+ * all valid rows); an infinity in a V row that it sees is in its O whatever the row's
+ * weight, infinities of both signs or a NaN make NaN.  fp32 O is accurate to fp32: weights enter the second product
  * in parts that add up to them.  bf16 O is rounded once.  Results of several
  * tiers are combined with hgca_lse_merge (fp32 O, a shape whose batch is B * n_q).
  * sm_scale must be positive and finite.  tier->cap is at most 2^30, and B times the rows of a

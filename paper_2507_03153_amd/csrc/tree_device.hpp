@@ -102,15 +102,49 @@ __device__ __forceinline__ uint32_t odd_halves(uint32_t x) {
     return bad | (bad - (bad >> 15));
 }
 
-// +inf, -inf and NaN are counted one after another, as products of ones: a half of `x` is of the kind iff (half & keep) - from <= more.
-struct OddKind {
-    uint32_t keep, from, more;
-    float add;
-    __device__ __forceinline__ explicit OddKind(int kind)
-        : keep(kind == 2 ? 0x7fffu : 0xffffu), from(kind == 0 ? 0x7f80u : kind == 1 ? 0xff80u : 0x7f81u), more(kind == 2 ? 0x7eu : 0u),
-          add(kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN) {}
-    __device__ __forceinline__ uint32_t ones(uint32_t x) const {
-        return ((x & keep) - from <= more ? 0x3f80u : 0u) | ((x >> 16 & keep) - from <= more ? 0x3f800000u : 0u);
+// Infinities and NaN of the V rows that a row sees.  A weight enters a product in parts that may be negative or 0, and a weight or a
+// factor between shares may be 0 in fp32, so such a value times them says nothing: where a sum is not finite, or an odd value of a
+// drafted row has been taken out of an operand, the workgroup goes through its share of V once more and notes which kinds a column has
+// among the tokens before the drafts, and in which drafted ones.  With an infinity in every share 64 drafts x 4 over 32 K tokens take
+// 414 -> 731 us, 32 drafts x 8 over 4 K 51 -> 78.
+template <int D> struct OddSeen {
+    unsigned long long drafted[3][D];            // by kind (+inf, -inf, NaN) and column: bit j = draft j has one
+    uint32_t before[D];                          // bit k = a token before the drafts has kind k
+    // Tokens begin .. end - 1 of V; contains barriers.
+    template <typename T, int BLOCK>
+    __device__ void collect(uint32_t *s_row, const TreeArgs &a, int b, int kvh, int begin, int end, int tail) {
+        constexpr int kPer = Elem<T>::kPerLoad, kPieces = D / kPer;              // elements of 16 bytes, such pieces of a row
+        for (int i = threadIdx.x; i < D; i += BLOCK) {
+            before[i] = 0;
+            drafted[0][i] = drafted[1][i] = drafted[2][i] = 0;
+        }
+        const int total = end - begin, sub_len = pass_length(a.kv, total), piece = threadIdx.x % kPieces;
+        for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
+            const int nsub = min(sub_len, total - sub0), first = begin + sub0;
+            __syncthreads();                     // the table is no longer in use; the notes are cleared
+            const BlockRows where = make_block_rows<BLOCK>(s_row, a.kv, a.sh.n_kv_heads, b, kvh, first, nsub);
+#pragma unroll 4
+            for (int tok = threadIdx.x / kPieces; tok < nsub; tok += BLOCK / kPieces) {
+                const uint32_t row = where.table ? where.table[tok / kGranule] + tok % kGranule : where.base + tok;
+                float x[kPer];
+                Elem<T>::expand(load16(a.kv.v + (size_t)row * (D * sizeof(T)) + 16 * piece), x);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    if (fabsf(x[i]) < INFINITY) continue;
+                    const int kind = x[i] == INFINITY ? 0 : x[i] == -INFINITY ? 1 : 2, col = piece * kPer + i, j = first + tok - tail;
+                    if (j < 0) atomicOr(&before[col], 1u << kind);
+                    else atomicOr(&drafted[kind][col], 1ull << j);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    // a column's sum of a row with this mask: what the values that it sees make of it
+    __device__ __forceinline__ float result(int col, uint64_t mask, float x) const {
+        uint32_t kinds = before[col];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) kinds |= drafted[k][col] & mask ? 1u << k : 0u;
+        return kinds == 0 ? x : kinds == 1 ? INFINITY : kinds == 2 ? -INFINITY : NAN;
     }
 };
 

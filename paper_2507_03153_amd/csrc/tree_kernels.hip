@@ -198,9 +198,12 @@ template <int RT, int E> struct RowState {
 };
 
 // What the waves of a workgroup found for their own tokens becomes one result per row: the final one, or a split's partial.
-template <int D, int RT> struct MergeShared {
+struct NoOddSeen {};
+template <typename S, int D, int RT> struct MergeShared {
     float m[kTreeWaves][16 * RT], l[kTreeWaves][16 * RT];
     float o[kTreeWaves][16][D + 4];
+    uint32_t odd[kTreeWaves];                    // a wave met infinities or NaN, or sums that are not finite
+    std::conditional_t<sizeof(S) == 1, NoOddSeen, OddSeen<D>> seen;      // (codes are finite or NaN, and a NaN stays one in every product)
 };
 
 template <int D, bool OUT_BF16> __device__ __forceinline__ void store_eight(void *o, int64_t at, const float *x) {
@@ -219,11 +222,14 @@ template <int D, bool OUT_BF16> __device__ __forceinline__ void store_eight(void
     }
 }
 
-template <int D, int RT>
-__device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeArgs &a, RowState<RT, D / 16> &st, int b, int kvh,
-                                            int row0, int slot)
+// odd: the lane has taken infinities or NaN out of V.
+template <typename S, int D, int RT>
+__device__ __forceinline__ void merge_waves(MergeShared<S, D, RT> &sh, uint32_t *s_row, const TreeArgs &a, RowState<RT, D / 16> &st,
+                                            const Span &span, int tail, bool odd, int kvh, int row0)
 {
     constexpr int E = D / 16;
+    constexpr bool kOdd = sizeof(S) > 1;
+    const int b = span.b, slot = span.slot;
     const int tid = threadIdx.x, w = tid / kWave, lane = tid % kWave, n = lane % 16, g = lane / 16;
     const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
 #pragma unroll
@@ -234,6 +240,19 @@ __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeAr
             sh.l[w][16 * r + n] = l;
         }
     }
+    if constexpr (kOdd) {
+        float z[4] = {0.f, 0.f, 0.f, 0.f};       // NaN where a sum is not finite
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = fmaf(st.o[r][e][i], 0.f, z[i]);
+        const float all = (z[0] + z[1]) + (z[2] + z[3]);
+        odd = __any(all != all || odd);
+        if (lane == 0) sh.odd[w] = odd;
+    }
+    bool any_odd = false;                        // uniform over the workgroup
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (r > 0) __syncthreads();              // the tile before has been read
@@ -247,6 +266,14 @@ __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeAr
                 *reinterpret_cast<float4 *>(&sh.o[w][n][(4 * g + i) * E + e]) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
         }
         __syncthreads();
+        if constexpr (kOdd) {
+            if (r == 0) {
+#pragma unroll
+                for (int i = 0; i < kTreeWaves; ++i) any_odd = any_odd || sh.odd[i];
+                if (any_odd)
+                    sh.seen.template collect<S, kTreeBlock>(s_row, a, b, kvh, span.begin, span.end, tail);
+            }
+        }
         const int row = tid / 16, c = tid % 16, at_row = row0 + 16 * r + row;
         if (at_row >= rows) continue;            // (barriers are reached by all: the loop is unrolled and uniform)
         float M = -INFINITY, f[kTreeWaves], L = 0.f, x[E];
@@ -269,7 +296,14 @@ __device__ __forceinline__ void merge_waves(MergeShared<D, RT> &sh, const TreeAr
                 x[e + 3] = fmaf(o.w, f[i], x[e + 3]);
             }
         }
-        const int64_t out_row = ((int64_t)b * a.n_q + (at_row >> lg)) * a.sh.n_q_heads + kvh * group + (at_row & (group - 1));
+        const int64_t qr = (int64_t)b * a.n_q + (at_row >> lg), out_row = qr * a.sh.n_q_heads + kvh * group + (at_row & (group - 1));
+        if constexpr (kOdd) {
+            if (any_odd) {
+                const uint64_t mask = a.mask ? a.mask[qr] : ~0ull;
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = sh.seen.result(c * E + e, mask, x[e]);
+            }
+        }
         if (a.n_splits > 1) {
             const int64_t at = partial_row(a, slot, kvh, at_row);
             store_eight<D, false>(a.part_o, at * D + c * E, x);
@@ -297,7 +331,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
     constexpr int KS = D / 32, E = D / 16, W = E / 2, QP = sizeof(TQ) == 4 ? 3 : 1, NW = kTreeWaves;
     constexpr bool kDrafts = sizeof(S) > 1;      // 8-bit tiers hold no drafted tokens
     __shared__ uint32_t s_row[kSub];
-    __shared__ MergeShared<D, RT> s_merge;
+    __shared__ MergeShared<S, D, RT> s_merge;
     const int kvh = blockIdx.y, row0 = (int)(blockIdx.x % a.row_blocks) * 16 * RT;          // row blocks of a slot run side by side
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
     const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
@@ -346,6 +380,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
     const float scale2 = a.sh.sm_scale * kTreeLog2e;
     const int tail = kDrafts && a.mask ? span.len - a.n_q : span.len;      // first drafted token
 
+    bool met_odd = false;                        // of the lane
     KTile<S, D> kt[2];
     VTile<S, D> vt[2];
     // One step: the scores of 32 tokens from kt, their weights, the outputs from vt.  next_k() and next_v() request the next step's
@@ -410,7 +445,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
         };
         if (masked) {
             // a weight of 0 keeps a row out of the product only if the row is finite: rows behind the end become 0, and
-            // infinities and NaN of drafted rows are taken out and added for the queries that see them
+            // infinities and NaN of drafted rows are taken out (OddSeen brings them to the queries that see them)
             uint32_t odd = 0;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -424,35 +459,8 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
                         odd |= odd_carry(x);
                     }
                 }
-            if (kDrafts && a.mask && __any((odd & kSigns) != 0)) {
-                // counts of +inf, -inf and NaN that a row sees in a column, as products of ones
-                uint4 ones[RT];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    uint32_t x[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t two = seen[r] >> (16 * (c / 2) + 2 * (c % 2));
-                        x[c] = (two & 1u) * 0x3f80u | (two >> 1 & 1u) * 0x3f800000u;
-                    }
-                    ones[r] = make_uint4(x[0], x[1], x[2], x[3]);
-                }
-#pragma unroll 1
-                for (int kind = 0; kind < 3; ++kind) {
-                    const OddKind k(kind);
-                    auto flag = [&](int t, int j, int i) { return k.ones(v[t][j][i]); };
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const uint4 op = pairs(e, flag);
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            const floatx4 c = mfma16(op, ones[r], floatx4{});
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) st.o[r][e][i] += c[i] > 0.f ? k.add : 0.f;
-                        }
-                        __builtin_amdgcn_sched_barrier(0);       // one column at a time: few registers
-                    }
-                }
+            if (kDrafts && a.mask && (odd & kSigns)) {
+                met_odd = true;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -494,7 +502,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_kernel(TreeArgs a)
         for (; tok < nsub; tok += kStep)
             consume(first + tok, [&] { fetch(kt, tok + kStep); }, [&] { fetch(vt, tok + kStep); });
     }
-    merge_waves<D, RT>(s_merge, a, st, span.b, kvh, row0, span.slot);
+    merge_waves<S, D, RT>(s_merge, s_row, a, st, span, tail, met_odd, kvh, row0);
 }
 
 // The same over fp32 rows, on the fp32 matrix instructions (products and sums in fp32, nothing rounded in between): 16 tokens at a time.  A
@@ -504,7 +512,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
 {
     constexpr int E = D / 16, U = D / 16, NW = kTreeWaves, RB = 4 * D;
     __shared__ uint32_t s_row[kSub];
-    __shared__ MergeShared<D, RT> s_merge;
+    __shared__ MergeShared<float, D, RT> s_merge;
     const int kvh = blockIdx.y, row0 = (int)(blockIdx.x % a.row_blocks) * 16 * RT;          // row blocks of a slot run side by side
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
     const int lg = __builtin_ctz(a.sh.group), group = a.sh.group, rows = a.n_q * group;
@@ -528,6 +536,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
     const float scale2 = a.sh.sm_scale * kTreeLog2e;
     const int tail = a.mask ? span.len - a.n_q : span.len;
 
+    bool met_odd = false;                        // of the lane
     float kr[U][4], vr[4][E];
     auto consume = [&](int tok, auto next_k, auto next_v) {
         const bool masked = tok + 16 > min(tail, span.end);
@@ -558,38 +567,18 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
         }
         st.weigh(s, scale2);
         if (masked) {                            // as above
-            uint32_t odd = 0;
+            float odd[4] = {0.f, 0.f, 0.f, 0.f}; // NaN where a value is not finite
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bool gone = tok + 4 * g + j >= span.end;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     vr[j][e] = gone ? 0.f : vr[j][e];
-                    odd |= (__float_as_uint(vr[j][e]) & 0x7fffffffu) + 0x00800000u;
+                    odd[j] = fmaf(vr[j][e], 0.f, odd[j]);
                 }
             }
-            if (a.mask && __any((odd & 0x80000000u) != 0)) {
-#pragma unroll 1
-                for (int kind = 0; kind < 3; ++kind) {
-                    const uint32_t keep = kind == 2 ? 0x7fffffffu : ~0u, more = kind == 2 ? 0x7ffffeu : 0u,
-                                   from = kind == 0 ? 0x7f800000u : kind == 1 ? 0xff800000u : 0x7f800001u;
-                    const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            floatx4 c = floatx4{};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float is = (__float_as_uint(vr[j][e]) & keep) - from <= more ? 1.f : 0.f;
-                                c = __builtin_amdgcn_mfma_f32_16x16x4f32(is, (float)(seen[r] >> j & 1u), c, 0, 0, 0);
-                            }
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) st.o[r][e][i] += c[i] > 0.f ? add : 0.f;
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
+            if (a.mask && __builtin_isnan((odd[0] + odd[1]) + (odd[2] + odd[3]))) {
+                met_odd = true;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -637,7 +626,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
         for (; tok < nsub; tok += kStep)
             consume(first + tok, [&] { fetch_k(tok + kStep); }, [&] { fetch_v(tok + kStep); });
     }
-    merge_waves<D, RT>(s_merge, a, st, span.b, kvh, row0, span.slot);
+    merge_waves<float, D, RT>(s_merge, s_row, a, st, span, tail, met_odd, kvh, row0);
 }
 
 // The splits of a row: M = max m_s, O = sum o_s 2^{m_s - M} / sum l_s 2^{m_s - M}.  A wave per row; 16 or 32 lanes across the columns,
@@ -700,6 +689,17 @@ template <int D, int WAVES> __global__ __launch_bounds__(kTreeBlock) void rows_f
         }
     }
     if (sg != 0) return;
+    if (not_finite(x.x) || not_finite(x.y) || not_finite(x.z) || not_finite(x.w)) {
+        // a split's infinity is one whatever the split's factor, which may be 0
+        float4 odd = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [](float &sum, float y) { sum += not_finite(y) ? y : 0.f; };
+        for (int s = 0; s < S; ++s) {
+            const float4 y = *reinterpret_cast<const float4 *>(o + s * stride * D);
+            add(odd.x, y.x), add(odd.y, y.y), add(odd.z, y.z), add(odd.w, y.w);
+        }
+        x = make_float4(not_finite(odd.x) ? odd.x : x.x, not_finite(odd.y) ? odd.y : x.y, not_finite(odd.z) ? odd.z : x.z,
+                        not_finite(odd.w) ? odd.w : x.w);
+    }
     const float inv = 1.f / L;
     if (L == 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
     else x = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);

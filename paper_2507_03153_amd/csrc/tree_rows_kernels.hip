@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     __shared__ __attribute__((aligned(1024))) char s_k1[S::kBytes];
     __shared__ __attribute__((aligned(1024))) char s_v0[S::kBytes];
     __shared__ __attribute__((aligned(1024))) char s_v1[S::kBytes];
-    __shared__ uint32_t s_row[kSub];
+    __shared__ uint32_t s_row[kSub], s_odd[kNW];
 
     // Workgroups are dealt to the XCDs in turn: blocks of rows that read the same tokens take numbers that are equal modulo their number
     int slot = blockIdx.x, kvh = blockIdx.y, rb = 0;
@@ -105,6 +105,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     const int v_lane = S::v_offset(4 * hw + lane % 16 / 4, lane / 16 % 2) + 8 * (lane % 4);
 
     const int tail = !kCodes && a.mask ? span.len - a.n_q : span.len;            // first drafted token
+    bool met_odd = false;                        // uniform over the wave
     float m = -INFINITY, shift = 0.f, l = 0.f;   // l: over this lane's tokens
     floatx16 acc[DT];
 #pragma unroll
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
             if (g + 1 < 2 * NT) read_v(g + 1, vop[(g + 1) % 2]);
             if constexpr (MASKED && !kCodes) {
                 // rows behind the end become 0 (a weight of 0 does not keep an infinity out); infinities and NaN of drafted rows are taken
-                // out and added for the rows that see them
+                // out (OddSeen brings them to the rows that see them)
                 const int left = span.end - (tok + 16 * g + 4 * hw);            // the lane's tokens: 0..3 and 8..11 of them
                 uint32_t odd = 0;
 #pragma unroll
@@ -218,23 +219,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
                     v[dt] = make_uint4(x[0], x[1], x[2], x[3]);
                 }
                 if (a.mask && __any((odd & kSigns) != 0)) {
-                    uint32_t one[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t two = (uint32_t)(seen >> (16 * g + 8 * (i / 2) + 2 * (i % 2)));
-                        one[i] = (two & 1u) * 0x3f80u | (two >> 1 & 1u) * 0x3f800000u;
-                    }
-#pragma unroll 1
-                    for (int kind = 0; kind < 3; ++kind) {
-                        const OddKind k(kind);
-#pragma unroll
-                        for (int dt = 0; dt < DT; ++dt) {
-                            const floatx16 count = product(make_uint4(k.ones(v[dt].x), k.ones(v[dt].y), k.ones(v[dt].z), k.ones(v[dt].w)), one, floatx16{});
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[dt][r] += count[r] > 0.f ? k.add : 0.f;
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-                    }
+                    met_odd = true;
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
                         uint4 &x = v[dt];
@@ -299,8 +284,26 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     }
 
     l = halves_sum(l);
+    if constexpr (!kCodes) {                     // (codes are finite or NaN, and a NaN stays one in every product)
+        float z[4] = {0.f, 0.f, 0.f, 0.f};       // NaN where a sum is not finite
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[r % 4] = fmaf(acc[dt][r], 0.f, z[r % 4]);
+        const float all = (z[0] + z[1]) + (z[2] + z[3]);
+        met_odd = __any(all != all) || met_odd;
+        if (lane == 0) s_odd[w] = met_odd;
+    }
+    if constexpr (HALVES || !kCodes) __syncthreads();            // all waves have read the stages
+    OddSeen<D> &seen_odd = *reinterpret_cast<OddSeen<D> *>(s_v1);
+    static_assert(sizeof(OddSeen<D>) <= sizeof(s_v1), "the notes lie in a stage");
+    bool any_odd = false;                        // uniform over the workgroup
+    if constexpr (!kCodes) {
+#pragma unroll
+        for (int i = 0; i < kNW; ++i) any_odd = any_odd || s_odd[i];
+        if (any_odd) seen_odd.template collect<ST, kTreeBlock>(s_row, a, b, kvh, span.begin, span.end, tail);
+    }
     if constexpr (HALVES) {                      // the two waves of a row: the second one's results by way of the stages
-        __syncthreads();                         // which all waves have read
         float *const box = reinterpret_cast<float *>(w % 2 ? s_k1 : s_k0);
         float *const stats = reinterpret_cast<float *>(s_v0) + 2 * kWave * (w % 2);
         if (half) {
@@ -329,6 +332,14 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     }
     // the lane holds columns 32 dt + 8 q + 4 hw .. + 3 of its row
     if (!row_exists) return;
+    if constexpr (!kCodes) {
+        if (any_odd) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[dt][r] = seen_odd.result(32 * dt + 8 * (r / 4) + 4 * hw + r % 4, mask, acc[dt][r]);
+        }
+    }
     const bool whole = a.n_splits == 1;
     const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
     const int64_t at = whole ? out_row : partial_row(a, slot, kvh, row);
