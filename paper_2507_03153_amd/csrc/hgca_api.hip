@@ -1590,9 +1590,16 @@ int hgca_kv_commit(const hgca_shape *shape, const hgca_kv_view *tier, const int3
     if (n_tokens < 0) return HGCA_ERR_INVALID_ARG;
     if (tier->cap > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
     if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
-    if (!k_in || !v_in || !aligned16(k_in) || !aligned16(v_in) || !lens_out || lens_out == first) return HGCA_ERR_INVALID_ARG;
+    if (!k_in || !v_in || !aligned16(k_in) || !aligned16(v_in) || !lens_out) return HGCA_ERR_INVALID_ARG;
     const int64_t row = shape->head_dim * (shape->dtype == HGCA_BF16 ? 2 : 4), heads = (int64_t)shape->batch * shape->n_kv_heads;
     if (n_tokens > (int64_t(1) << 32) / heads) return HGCA_ERR_UNSUPPORTED;      // (2^32 rows are 512 GB at least)
+    // one workgroup of a sequence writes its new length while others still read what the rows go by
+    const int64_t per_seq = 4 * (int64_t)shape->batch;
+    const Range lens(lens_out, per_seq);
+    auto read_beside = [&](const int32_t *p, int64_t each) { return p && lens.meets(Range(p, per_seq * each)); };
+    if (read_beside(first, 1) || read_beside(cnt, 1) || read_beside(path, n_tokens) ||
+        (tier->block_table && (read_beside(tier->first_block, 1) || read_beside(tier->block_table, tier->max_blocks))))
+        return HGCA_ERR_INVALID_ARG;
     if (!tier->block_table && tier->cap > 0)
         for (const void *in : {k_in, v_in})
             for (const void *rows : {tier->k, tier->v})
