@@ -667,7 +667,8 @@ int hgca_tree_attn(const hgca_shape *shape, const void *q, int32_t n_q,
  * them stay as they are.  Tokens beyond the tier's capacity or table row are left out (bit
  * HGCA_CACHE_CONTEXT_FULL of *status, optional).  tier->k / v are written and tier->seq_lens
  * is not read; lens_out (device int32 [B]) may be the array behind it, but must not overlap
- * `first`, cnt, path or the tier's table (refused).
+ * `first`, cnt, path or the tier's table (refused).  n_tokens = 0 is a no-op as batch = 0
+ * is: lens_out stays as it is (cnt[b] = 0 gives first[b]).
  * k_in / v_in must not overlap the tier's rows (refused where the tier is contiguous). */
 int hgca_kv_commit(const hgca_shape *shape, const hgca_kv_view *tier,
                    const int32_t *first, const void *k_in, const void *v_in,

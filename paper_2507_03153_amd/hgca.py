@@ -752,7 +752,8 @@ def _first_and_status(B: int, dev: int, first, status=None) -> None:
 
 def kv_commit(shape: Shape, tier: Tier, first, k_in, v_in, lens_out, path=None, cnt=None, status=None, stream=None) -> None:
     """Rows path[b,i], i < cnt[b], of k_in / v_in [B,n,Hkv,d] go to positions first[b] + i of the tier; lens_out[b] = first[b] +
-    cnt[b].  path int32 [B,n] (None: row i), cnt int32 [B] (None: n), first int32 [B] (None: 0)."""
+    cnt[b].  path int32 [B,n] (None: row i), cnt int32 [B] (None: n), first int32 [B] (None: 0).  With n = 0 nothing is written,
+    lens_out neither."""
     B, _, Hkv, d, dt = _heads(shape)
     dev, n = _gpu_of(k_in), k_in.shape[1]
     _need("k_in", k_in, dt, (B, n, Hkv, d), dev)
