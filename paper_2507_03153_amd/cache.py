@@ -155,7 +155,13 @@ class LayerCache:
         """Attention of n drafted tokens per sequence, which join the window for the time being: q [B,n,Hq,d], k_in / v_in
         [B,n,Hkv,d]; bit j of mask[b,i] (int64 [B,n]) = draft i sees draft j (None: all).  They see the whole window, and the whole
         pool, in 8 bits if the cache keeps it so.  Results in o_draft [B,n,Hq,d], lse_draft [B,n,Hq]; `commit` follows."""
-        n, sh = int(q.shape[1]), self.shape
+        n, sh, dev = int(q.shape[1]), self.shape, self.k_blocks.get_device()
+        # the append is not taken back: what the later calls would refuse is refused before it
+        hgca._need("q", q, self.k_blocks.dtype, (self.B, n, self.Hq, self.d), dev)
+        for name, t in (("k_in", k_in), ("v_in", v_in)):
+            hgca._need(name, t, self.k_blocks.dtype, (self.B, n, self.Hkv, self.d), dev)
+        if mask is not None:
+            hgca._need("mask", mask, torch.int64, (self.B, n), dev)
         if self.win_cap < (self.win_blocks * self.block_size - 1) + n:
             raise ValueError(f"{n} drafted tokens need win_cap_blocks for l_max - 1 + {n} tokens")
         mine = self._draft_buffers(n)
