@@ -1,9 +1,10 @@
 """Plumbing for the KV manager calls: owns the device buffers of one layer's cache state (block pool,
 block table, window / pool lengths, moving averages, per-head salient lists) and enqueues the calls of
 one decode step in the order of the paper's Alg. 2 (attention) and Alg. 1 (management).  Nothing here
-computes: every step is a libhgca call."""
+computes: every step is a libhgca call, but for the few lengths that a draft step keeps apart."""
 from __future__ import annotations
 
+from dataclasses import replace
 from types import SimpleNamespace
 
 import torch
@@ -33,8 +34,8 @@ class LayerCache:
         self.v_blocks = torch.zeros_like(self.k_blocks)
         self.block_table = torch.arange(B * max_blocks, **i32).reshape(B, max_blocks).contiguous()
         self.first_win_block = torch.zeros(B, **i32)
-        self.win_lens = torch.zeros(B, **i32)
-        self.pool_lens = torch.zeros(B, **i32)
+        self._lens = torch.zeros(2, B, **i32)
+        self.win_lens, self.pool_lens = self._lens[0], self._lens[1]
         self.a_maw = torch.zeros(B, Hq, self.win_cap, **f32)
         self.ctx_idx = torch.full((B, Hq, max(k_max, 1)), -1, **i32)
         self.ctx_cnt = torch.zeros(B, Hq, **i32)
@@ -56,6 +57,12 @@ class LayerCache:
         self.pool8 = hgca.Kv8Tier.like(self.pool) if pool8 else None
         self.pool8_lens = torch.zeros(B, **i32)          # tokens of the pool that are there already
         self.draft_first = torch.zeros(B, **i32)         # the window's lengths before the drafts of a draft_step
+        self.draft_ok = torch.zeros(B, **i32)            # 1: the drafts are in the window, 0: it had no room for them
+        self._draft_cnt = torch.zeros(B, **i32)          # what `commit` takes of them
+        # the tiers of a draft_step: a sequence without its drafts has no tokens
+        self._draft_lens = torch.zeros(2, B, **i32)
+        self._draft_window = replace(self.window, seq_lens=self._draft_lens[0])
+        self._draft_pool = replace(self.pool8 if pool8 else self.pool, seq_lens=self._draft_lens[1])
         self._drafts = {}
         # per-step outputs and scratch
         self.o_w, self.lse_w = torch.empty(B, Hq, d, **f32), torch.empty(B, Hq, **f32)
@@ -154,7 +161,10 @@ class LayerCache:
     def draft_step(self, q, k_in, v_in, mask=None) -> None:
         """Attention of n drafted tokens per sequence, which join the window for the time being: q [B,n,Hq,d], k_in / v_in
         [B,n,Hkv,d]; bit j of mask[b,i] (int64 [B,n]) = draft i sees draft j (None: all).  They see the whole window, and the whole
-        pool, in 8 bits if the cache keeps it so.  Results in o_draft [B,n,Hq,d], lse_draft [B,n,Hq]; `commit` follows."""
+        pool, in 8 bits if the cache keeps it so.  Results in o_draft [B,n,Hq,d], lse_draft [B,n,Hq]; one `commit` follows.
+
+        A sequence whose table row has no room for n more tokens takes none (status bit CACHE_CONTEXT_FULL, draft_ok[b] = 0): its
+        queries see nothing, O = 0 and lse = -inf, and `commit` leaves it as it is."""
         n, sh, dev = int(q.shape[1]), self.shape, self.k_blocks.get_device()
         # the append is not taken back: what the later calls would refuse is refused before it
         hgca._need("q", q, self.k_blocks.dtype, (self.B, n, self.Hq, self.d), dev)
@@ -168,20 +178,29 @@ class LayerCache:
         (self.o_draft, o_w, o_p), (self.lse_draft, lse_w, lse_p) = mine.o, mine.lse
         self.draft_first.copy_(self.win_lens)
         hgca.kv_append_tokens(sh, self.state, k_in, v_in)
-        hgca.tree_attn(sh, q, self.window, mask, o_w, lse_w, mine.ws)
+        torch.gt(self.win_lens, self.draft_first, out=self.draft_ok)
+        torch.mul(self._lens, self.draft_ok, out=self._draft_lens)
+        hgca.tree_attn(sh, q, self._draft_window, mask, o_w, lse_w, mine.ws)
         if self.pool8 is not None:
             self.sync_pool8()
-            hgca.kv8_attn(sh, q, self.pool8, o_p, lse_p, mine.ws_pool)
+            hgca.kv8_attn(sh, q, self._draft_pool, o_p, lse_p, mine.ws_pool)
         else:
-            hgca.append_attn(sh, q, self.pool, False, o_p, lse_p, mine.ws_pool)
+            hgca.append_attn(sh, q, self._draft_pool, False, o_p, lse_p, mine.ws_pool)
         merged = hgca.Shape(sh.dtype, sh.batch * n, sh.n_q_heads, sh.n_kv_heads, sh.head_dim, sh.sm_scale)
         hgca.lse_merge(merged, o_p, lse_p, o_w, lse_w, self.o_draft, self.lse_draft)
 
     def commit(self, k_in, v_in, path, cnt, beta: float) -> None:
         """Of the last draft_step's tokens (its k_in, v_in) those on the accepted path stay in the window: path int32 [B,n], cnt
-        int32 [B].  Then windows that have reached l_max evict (Alg. 1).  The moving averages of the tokens that stay start at 0
-        (attention weights under a tree mask are not averaged)."""
-        hgca.kv_commit(self.shape, self.window, self.draft_first, k_in, v_in, self.win_lens, path=path, cnt=cnt, status=self.status)
+        int32 [B] (None: all n).  Then windows that have reached l_max evict (Alg. 1).  The moving averages of the tokens that stay
+        start at 0 (attention weights under a tree mask are not averaged): tokens that are evicted before a decode step has seen
+        them pass no threshold, so that decode steps attend to them again only from an append_step on, which draws up the lists
+        anew.  Draft steps, which attend to the whole pool, lose nothing by that."""
+        n = int(k_in.shape[1])
+        if cnt is not None:
+            hgca._need("cnt", cnt, torch.int32, (self.B,), self.k_blocks.get_device())
+        torch.mul(self.draft_ok, n if cnt is None else cnt, out=self._draft_cnt)
+        hgca.kv_commit(self.shape, self.window, self.draft_first, k_in, v_in, self.win_lens, path=path, cnt=self._draft_cnt,
+                       status=self.status)
         hgca.kv_evict(self.shape, self.state, beta)
 
     def sync_pool8(self) -> None:
