@@ -648,8 +648,8 @@ int hgca_qk_norm_rope(const hgca_shape *shape,
  * weight, infinities of both signs or a NaN make NaN.  fp32 O is accurate to fp32: weights enter the second product
  * in parts that add up to them.  bf16 O is rounded once.  Results of several
  * tiers are combined with hgca_lse_merge (fp32 O, a shape whose batch is B * n_q).
- * sm_scale must be positive and finite.  tier->cap is at most 2^30, and B times the rows of a
- * group (n_q * Hq / Hkv), in blocks of 16 to 128, at most 2^23.  ws needs
+ * sm_scale must be positive and finite; scaled scores may be of any size up to 2^127.
+ * tier->cap is at most 2^30, and B times the rows of a group (n_q * Hq / Hkv), in blocks of 16 to 128, at most 2^23.  ws needs
  * hgca_tree_workspace_bytes(shape, n_q, tier->cap), which also serves smaller capacities. */
 #define HGCA_MAX_DRAFTS 64
 size_t hgca_tree_workspace_bytes(const hgca_shape *shape, int32_t n_q, int32_t max_tokens);

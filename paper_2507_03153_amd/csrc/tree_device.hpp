@@ -82,6 +82,20 @@ struct Span {
     }
 };
 
+// What a row's weights are relative to, for a maximum m of its raw scores: 2^-shift_of, as rounded, so that a weight 2^fma(score, scale2,
+// shift) has none of the rounding in it.  From 2^30 on the rounding is tens of powers of two and a weight would leave fp32: there scores
+// have their maximum subtracted first, which is exact, and then the scale alone.  (Two such scores are 2^64 apart in weight or equal.)
+constexpr float kFarShift = 1073741824.f, kLargest = 3.40282347e38f;
+__device__ __forceinline__ float shift_of(float m, float scale2) {
+    return m == -INFINITY ? 0.f : __builtin_amdgcn_fmed3f(-m * scale2, -kLargest, kLargest);
+}
+__device__ __forceinline__ bool is_far(float shift) { return fabsf(shift) >= kFarShift; }
+// the factor that takes sums relative to one maximum to another, at least as large; 1 where they are equal
+__device__ __forceinline__ float rescale_factor(float m, float m_new, float scale2) {
+    const float from = shift_of(m, scale2), to = shift_of(m_new, scale2);
+    return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(is_far(from) || is_far(to) ? (m - m_new) * scale2 : to - from);
+}
+
 // Where a row's partial of a slot lies: the rows of a KV head of a slot are consecutive.
 __device__ __forceinline__ int64_t partial_row(const TreeArgs &a, int slot, int kvh, int row) {
     return ((int64_t)slot * a.sh.n_kv_heads + kvh) * (a.n_q * a.sh.group) + row;

@@ -145,12 +145,13 @@ template <int D> struct VTile<kv8_t, D> {
 };
 
 // Running softmax of RT row tiles over NT 16-token tiles per step.  The maximum is kept on raw scores (the scale is positive); a
-// weight is 2^fma(score, scale2, shift) with shift = -max * scale2 as rounded, and `shift` is what a partial result is relative to, so that
-// the rounding of the shift is in no result.
+// weight is 2^fma(score, scale2, shift) with the shift of the maximum (shift_of), which partial results are relative to.
 template <int RT, int E> struct RowState {
-    float m[RT], shift[RT], l[RT];               // l: over the lane's own tokens
+    float m[RT], shift[RT], l[RT];               // shift: 0 for far rows; l: over the lane's own tokens
+    bool far;                                    // a row of the wave is far (uniform over the wave)
     floatx4 o[RT][E];
     __device__ __forceinline__ void clear() {
+        far = false;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             m[r] = -INFINITY;
@@ -173,16 +174,27 @@ template <int RT, int E> struct RowState {
             more = more || mx[r] > m[r];
         }
         if (__any(more)) {                       // uniform over the wave
+            bool any_far = false;
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const float m_new = fmaxf(m[r], rows_max(mx[r]));
-                const float to = m_new == -INFINITY ? 0.f : -m_new * scale2;
-                const float corr = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - shift[r]);     // 1 where the maximum stands
+                const float m_new = fmaxf(m[r], rows_max(mx[r])), to = shift_of(m_new, scale2), corr = rescale_factor(m[r], m_new, scale2);
                 m[r] = m_new;
-                shift[r] = to;
+                shift[r] = is_far(to) ? 0.f : to;
+                any_far = any_far || is_far(to);
                 l[r] *= corr;
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[r][e] *= corr;
+            }
+            far = __any(any_far);
+        }
+        if (far) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float less = is_far(shift_of(m[r], scale2)) ? m[r] : 0.f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[r][t][i] -= less;
             }
         }
 #pragma unroll
@@ -236,7 +248,8 @@ __device__ __forceinline__ void merge_waves(MergeShared<S, D, RT> &sh, uint32_t 
     for (int r = 0; r < RT; ++r) {
         const float l = rows_sum(st.l[r]);
         if (g == 0) {
-            sh.m[w][16 * r + n] = l == 0.f ? -INFINITY : -st.shift[r];         // nothing seen: l is 0 (with only NaN seen it is NaN)
+            // nothing seen: l is 0 (with only NaN seen it is NaN)
+            sh.m[w][16 * r + n] = l == 0.f ? -INFINITY : -shift_of(st.m[r], a.sh.sm_scale * kTreeLog2e);
             sh.l[w][16 * r + n] = l;
         }
     }

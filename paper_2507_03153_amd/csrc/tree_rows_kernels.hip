@@ -105,8 +105,8 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     const int v_lane = S::v_offset(4 * hw + lane % 16 / 4, lane / 16 % 2) + 8 * (lane % 4);
 
     const int tail = !kCodes && a.mask ? span.len - a.n_q : span.len;            // first drafted token
-    bool met_odd = false;                        // uniform over the wave
-    float m = -INFINITY, shift = 0.f, l = 0.f;   // l: over this lane's tokens
+    bool met_odd = false, far = false;           // uniform over the wave; far: a row of it is (shift_of)
+    float m = -INFINITY, shift = 0.f, l = 0.f;   // shift: 0 for far rows; l: over this lane's tokens
     floatx16 acc[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = floatx16{};
@@ -165,14 +165,18 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, c[t][r]);
         if (__any(mx > m)) {                     // uniform over the wave
-            const float m_new = fmaxf(m, halves_max(mx));
-            const float to = m_new == -INFINITY ? 0.f : -m_new * scale2;
-            const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - shift);       // 1 where the maximum stands
+            const float m_new = fmaxf(m, halves_max(mx)), to = shift_of(m_new, scale2), corr = rescale_factor(m, m_new, scale2);
             m = m_new;
-            shift = to;
+            shift = is_far(to) ? 0.f : to;
+            far = __any(is_far(to));
             l *= corr;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) acc[dt] *= corr;
+        }
+        if (far) {
+            const float less = is_far(shift_of(m, scale2)) ? m : 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c[t] -= less;
         }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         uint32_t part[PP][4];
@@ -284,6 +288,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void many_rows_attn_kernel(TreeArgs 
     }
 
     l = halves_sum(l);
+    shift = shift_of(m, scale2);
     if constexpr (!kCodes) {                     // (codes are finite or NaN, and a NaN stays one in every product)
         float z[4] = {0.f, 0.f, 0.f, 0.f};       // NaN where a sum is not finite
 #pragma unroll
