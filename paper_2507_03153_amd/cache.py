@@ -158,6 +158,13 @@ class LayerCache:
                                               ws_pool=make(self.shape, n, self.pool_cap, dev))
         return self._drafts[n]
 
+    def _device(self) -> int:
+        """The cache's GPU, which has to be the current one: some of the calls of a step take that one's stream."""
+        dev = self.k_blocks.get_device()
+        if torch.cuda.current_device() != dev:
+            raise ValueError(f"the cache is on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+        return dev
+
     def draft_step(self, q, k_in, v_in, mask=None) -> None:
         """Attention of n drafted tokens per sequence, which join the window for the time being: q [B,n,Hq,d], k_in / v_in
         [B,n,Hkv,d]; bit j of mask[b,i] (int64 [B,n]) = draft i sees draft j (None: all).  They see the whole window, and the whole
@@ -165,7 +172,7 @@ class LayerCache:
 
         A sequence whose table row has no room for n more tokens takes none (status bit CACHE_CONTEXT_FULL, draft_ok[b] = 0): its
         queries see nothing, O = 0 and lse = -inf, and `commit` leaves it as it is."""
-        n, sh, dev = int(q.shape[1]), self.shape, self.k_blocks.get_device()
+        n, sh, dev = int(q.shape[1]), self.shape, self._device()
         # the append is not taken back: what the later calls would refuse is refused before it
         hgca._need("q", q, self.k_blocks.dtype, (self.B, n, self.Hq, self.d), dev)
         for name, t in (("k_in", k_in), ("v_in", v_in)):
@@ -195,9 +202,9 @@ class LayerCache:
         start at 0 (attention weights under a tree mask are not averaged): tokens that are evicted before a decode step has seen
         them pass no threshold, so that decode steps attend to them again only from an append_step on, which draws up the lists
         anew.  Draft steps, which attend to the whole pool, lose nothing by that."""
-        n = int(k_in.shape[1])
+        n, dev = int(k_in.shape[1]), self._device()
         if cnt is not None:
-            hgca._need("cnt", cnt, torch.int32, (self.B,), self.k_blocks.get_device())
+            hgca._need("cnt", cnt, torch.int32, (self.B,), dev)
         torch.mul(self.draft_ok, n if cnt is None else cnt, out=self._draft_cnt)
         hgca.kv_commit(self.shape, self.window, self.draft_first, k_in, v_in, self.win_lens, path=path, cnt=self._draft_cnt,
                        status=self.status)
