@@ -646,7 +646,8 @@ int hgca_qk_norm_rope(const hgca_shape *shape,
  * no part in its O, whatever the row holds (with draft_mask; without it all queries see
  * all valid rows); an infinity in a V row that it sees is in its O whatever the row's
  * weight, infinities of both signs or a NaN make NaN.  fp32 O is accurate to fp32: weights enter the second product
- * in parts that add up to them.  bf16 O is rounded once.  Results of several
+ * in parts that add up to them.  For bf16 O they enter with 16 bits (2e-6 of O, below
+ * its one rounding of 2^-9).  Results of several
  * tiers are combined with hgca_lse_merge (fp32 O, a shape whose batch is B * n_q).
  * sm_scale must be positive and finite; scaled scores may be of any size up to 2^127.
  * tier->cap is at most 2^30, and B times the rows of a group (n_q * Hq / Hkv), in blocks of 16 to 128, at most 2^23.  ws needs

@@ -258,8 +258,11 @@ constexpr int32_t kMaxKv8Queries = 4096;
 // than 32 rows per workgroup, 32 over 256 15.5 : 14.5, over 300 13.0 : 14.9; fp32 by the work of a token, 512 tokens for
 // 16 rows of 64 columns (500 12.4 : 10.3), 320 of 128 (320 12.6 : 12.2, 400 12.8 : 14.9), 160 for 32 rows (256 16.1 : 16.8, 330 16.1 : 21.1).
 // Where there is a workgroup for every other unit without splits, longer tiers too: 256 units, 32 drafts over 600 / 1000 / 2000 / 4000 tokens
-// 50.8 : 31.5, 64.1 : 49.0, 98.8 : 87.4, 155.7 : 155.7, 4 over 2000 57.2 : 52.5, 12 over 4000 108 : 112; 160 units, 32 over 1600 61.1 : 54.8,
-// 12 39.5 : 40.6; 8 bits, 256 units, 2 queries over 1000 / 2000 19.8 : 17.3, 29.6 : 31.7, 160 units, 16 over 800 / 1600 29.1 : 26.9, 37.5 : 43.4.
+// 50.8 : 31.5, 64.1 : 49.0, 98.8 : 87.4, 155.7 : 155.7, 4 over 2000 57.2 : 52.5, 12 over 4000 108 : 112; 160 units, 32 over 1600 61.1 : 54.8
+// (the rule, eight tokens per unit, splits there all the same: it is the rule for fewer rows too), 12 39.5 : 40.6; 8 bits, 256 units, 2 queries over 1000 / 2000 19.8 : 17.3, 29.6 : 31.7, 160 units, 16 over 800 / 1600 29.1 : 26.9, 37.5 : 43.4.
+//
+// More than 256 units are not split at all, and lengths are then not dealt either (Span): one token x 32 / 33 / 40 / 64 / 65 sequences of 8 KV heads
+// over 28 K in 8 bits 315 / 496 / 527 / 626 / 882, one of 120 K among 31 / 39 of 2 K 94 / 1475, 64 drafts x 8 / 9 over 16 K in groups of 8 535 / 752.
 #ifndef HGCA_TARGET_WGS_TREE
 #define HGCA_TARGET_WGS_TREE 512
 #endif

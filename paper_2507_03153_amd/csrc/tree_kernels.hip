@@ -13,8 +13,9 @@
 // tokens that it holds the scores of, and pairs of tokens are put together by one byte permutation each; output column m * E + e is row
 // m of the e-th product.
 //
-// fp32 outputs ask for weights as exact as fp32 (O within 5e-7 of 64 bits): they enter the second product as three bf16 parts that add
-// up to them.  Outputs in bf16, whose own rounding is 2^-9, take two parts (2e-6).
+// fp32 outputs ask for weights as exact as fp32: they enter the second product as three bf16 parts that add up to them (O is then 2e-7 to
+// 1.1e-6 off 64 bits).  Outputs in bf16, whose own rounding is 2^-9, take two parts, 16 bits of a weight, 2e-6 of O: of 65536 outputs of 64 drafts
+// over 32 K tokens 164 are not the nearest bf16 number, 73 with three parts and 134 of sums in fp32; three parts take 390 -> 478 us.
 //
 // What bounds it: the stream of K and V (16 rows meet a K row in one product, so a workgroup's arithmetic is short), and with few
 // tokens a workgroup's chain of loads.  One token x 8 sequences over 28 K tokens of 8 heads of 128 in 8 bits, groups of 4: 79.5 us, 485 MB
@@ -644,7 +645,7 @@ __global__ __launch_bounds__(kTreeBlock, 2) void rows_attn_f32_kernel(TreeArgs a
 
 // The splits of a row: M = max m_s, O = sum o_s 2^{m_s - M} / sum l_s 2^{m_s - M}.  A wave per row; 16 or 32 lanes across the columns,
 // the others take further splits.  Bound by two round trips to memory and the partials: 8192 rows of 128 in 8 splits 8.6 us (34 MB, 3.9
-// TB/s), 256 rows in 16 splits 4.6 us.  Few rows in many splits are loads one after another: they take a workgroup per row.  Wave :
+// TB/s), 256 rows in 8 splits 4.6 us.  Few rows in many splits are loads one after another: they take a workgroup per row.  Wave :
 // workgroup, whole calls, us: 4 rows in 128 splits 38.1 : 30.1 (120 K tokens in 8 bits), 32 in 64 31.9 : 27.8, 128 in 32 23.9 : 22.0, 40
 // in 16 18.4 : 18.0; 2048 rows in 32 87.2 : 89.2.
 template <int D, int WAVES> __global__ __launch_bounds__(kTreeBlock) void rows_fold_kernel(TreeArgs a, int64_t rows)

@@ -9,7 +9,7 @@
 // fp32 results take the weights in three bf16 parts (4 units of matrix work per useful 2), bf16 results in two (3 per 2).
 //
 // What bounds it: matrix and vector instructions of a SIMD's two waves, which overlap in part, and the power they take.  64 drafts x 4 sequences
-// over 32 K tokens, 64 / 8 heads of 128, bf16 result: 375 to 434 us, 275 GFLOP, 412 with the parts, matrix units busy 57 % of the cycles at 1.7
+// over 32 K tokens, 64 / 8 heads of 128, bf16 result: 375 to 448 us, 275 GFLOP, 412 with the parts, matrix units busy 56 % of the cycles at 1.7
 // GHz; with K and V of zeros 274 us.  16 queries x 4, 61 to 122 K tokens in 8 bits, fp32 result: 345 to 412 us for 204 (409)
 // GFLOP.  32 drafts x 8 over 4 K tokens, 32 / 8 heads: 40 us, 102 MB read and 34 MB of partials written, about half of it a workgroup's start
 // and end (eight steps each), and 8.6 us of fold.
