@@ -613,7 +613,8 @@ int hgca_append_weights_tiers(const hgca_shape *shape, const void *q, int32_t n_
  * eps), and its first rot_dim columns are rotated in pairs by the token's position,
  * (a, b) -> (a cos t - b sin t, a sin t + b cos t) with t = position *
  * inv_freq[j] for pair j; the other columns are left as normed.  The angle is formed in
- * fp64 (far positions keep their digits), all else in fp32, rounded once.
+ * fp64 (far positions keep their digits), all else in fp32, rounded once; a row whose sum
+ * of squares is no fp32 number (values from about 1e18 on) gives 0.
  * q_in is [B, n_tokens, Hq, d], k_in [B, n_tokens, Hkv, d] in shape.dtype;
  * q_token_stride / k_token_stride are elements from one token's row to the next (0:
  * Hq * d and Hkv * d), a multiple of 16 bytes, so that both may be parts of one

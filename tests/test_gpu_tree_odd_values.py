@@ -123,3 +123,39 @@ def test_nan_codes_of_an_8_bit_tier(gpu, d, Hq, n):
     want = outs[0][0].copy()
     want[..., 3] = want[..., 4] = np.nan
     assert np.array_equal(outs[1][0], want, equal_nan=True) and np.array_equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("dtype,d,Hq,n", [("bf16", 128, 4, 3), ("bf16", 128, 4, 6), ("bf16", 64, 4, 12), ("bf16", 64, 8, 20), ("f32", 64, 4, 3)])
+def test_behind_the_first_table_of_block_rows(gpu, dtype, d, Hq, n):
+    """A sequence that is one workgroup's work and longer than two tables (8192 tokens each), among 299 short ones: values in each of its
+    three passes, the drafts in the last."""
+    torch, hgca = gpu
+    B, T, bs, at = 300, 17000, 16, 211
+    rng = np.random.default_rng(n)
+    lens = rng.integers(1, 40, B).astype(np.int32)
+    lens[at] = T - 5
+    n_blk = [-(-int(x) // bs) for x in lens]
+    table, perm, start = np.zeros((B, -(-T // bs)), np.int32), rng.permutation(sum(n_blk)).astype(np.int32), 0
+    for b, x in enumerate(n_blk):
+        table[b, :x] = perm[start:start + x]
+        start += x
+    r = (lambda *s: rng.standard_normal(s).astype(np.float32)) if dtype == "f32" else (lambda *s: do.to_bf16(rng.standard_normal(s)))
+    kb, vb, q = r(len(perm), 1, bs, d), r(len(perm), 1, bs, d), r(B, n, Hq, d)
+    m = [do.ancestors(rng, n) for _ in range(B)]
+    bad, L = vb.copy(), T - 5
+    put_at = lambda tok, col, x: bad.__setitem__((table[at, tok // bs], 0, tok % bs, col), x)
+    for tok, col, x in ((3, 0, np.inf), (8191, 1, -np.inf), (8192, 2, np.inf), (9000, 3, np.nan), (16384, 4, np.inf), (L - n - 1, 5, -np.inf),
+                        (2, 6, np.inf), (12000, 6, -np.inf), (L - n, 7, np.inf), (L - 1, 8, -np.inf)):
+        put_at(tok, col, x)
+    shape = hgca.Shape(hgca.F32 if dtype == "f32" else hgca.BF16, B, Hq, 1, d, 0.125)
+    sent, outs = torch.from_numpy(do.as_int64(m)).to(DEV), []
+    for v in (vb, bad):
+        tier = hgca.Tier(put(torch, kb, dtype), put(torch, v, dtype), T, i32(torch, lens), i32(torch, table), bs)
+        outs.append([x.cpu().numpy() for x in call(gpu, shape, put(torch, q, dtype), tier, sent, "f32")])
+    (good, lse0), (o, lse) = outs
+    V = np.concatenate([bad[i, 0] for i in table[at, :n_blk[at]]])[:L]
+    sees = np.ones((n, L), bool)
+    sees[:, L - n:] = [[m[at][i] >> j & 1 for j in range(n)] for i in range(n)]
+    want = good.copy()
+    want[at] = expected(good[at], V, sees)
+    assert np.isfinite(good).all() and np.array_equal(o, want, equal_nan=True) and np.array_equal(lse, lse0)
