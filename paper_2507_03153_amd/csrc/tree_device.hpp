@@ -84,7 +84,7 @@ struct Span {
 
 // What a row's weights are relative to, for a maximum m of its raw scores: 2^-shift_of, as rounded, so that a weight 2^fma(score, scale2,
 // shift) has none of the rounding in it.  From 2^30 on the rounding is tens of powers of two and a weight would leave fp32: there scores
-// have their maximum subtracted first, which is exact, and then the scale alone.  (Two such scores are 2^64 apart in weight or equal.)
+// have their maximum subtracted first, and a weight is 2^((score - m) scale2).  (Two such scores are 2^64 apart in weight or equal.)
 constexpr float kFarShift = 1073741824.f, kLargest = 3.40282347e38f;
 __device__ __forceinline__ float shift_of(float m, float scale2) {
     return m == -INFINITY ? 0.f : __builtin_amdgcn_fmed3f(-m * scale2, -kLargest, kLargest);
