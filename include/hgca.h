@@ -724,6 +724,121 @@ int hgca_kv8_attn(const hgca_shape *shape, const void *q, int32_t n_q,
                   const hgca_kv8_view *kv8, void *o_out, int32_t o_dtype, float *lse_out,
                   void *ws, size_t ws_bytes, void *hip_stream);
 
+/* ---- A server's step: requests of different size packed one behind the other. ---- */
+
+/* Blocks of a paged tier dealt out on the device.  Row b of block_table names the blocks of
+ * sequence b, its first held[b] entries are in use and hold lens[b] tokens (held[b] >=
+ * ceil(lens[b] / block_size)); free_blocks[0 .. *free_count) are the numbers of the blocks
+ * that nobody holds, a stack whose top is the last.  All arrays are device memory; a tier
+ * over them is { k, v, lens, block_table, cap, block_size, max_blocks }.  n_blocks *
+ * block_size is at most 2^31 - 1.  Calls on one state go one after the other. */
+typedef struct {
+    int32_t *block_table;         /* [batch, max_blocks] (rw)                              */
+    int32_t *held;                /* [batch] (rw)                                          */
+    int32_t *lens;                /* [batch] (rw)                                          */
+    int32_t *free_blocks;         /* [n_blocks] (rw)                                       */
+    int32_t *free_count;          /* [1] (rw)                                              */
+    int32_t *status;              /* [1] (rw) sticky HGCA_CACHE_* bits, or NULL            */
+    int32_t *scratch;             /* [3 * batch + 1], contents undefined between calls     */
+    int32_t batch, block_size, max_blocks, n_blocks;
+} hgca_block_state;
+
+enum {
+    HGCA_CACHE_BLOCKS_OUT = 8,    /* free blocks did not suffice: a sequence got no tokens          */
+    HGCA_CACHE_TOKENS_FULL = 16   /* more tokens than max_tokens: a sequence got none               */
+};
+
+/* n_new[b] more tokens (device int32 [batch], negative counts as 0) for every sequence: its
+ * table row gets the blocks that they need, lens[b] and held[b] grow, and the step's tokens
+ * are laid out one sequence behind the other: cu_out ([batch + 1]) receives where each
+ * sequence's tokens begin, positions_out and slots_out ([max_tokens]) each token's
+ * position in its sequence and its slot, block * block_size + position % block_size; from
+ * cu_out[batch] on 0 and -1.  A sequence takes all of its tokens or none: none where its
+ * table row is too short (HGCA_CACHE_CONTEXT_FULL), where the blocks that it and the
+ * sequences before it ask for are more than there are (HGCA_CACHE_BLOCKS_OUT; one that
+ * asks for none is not meant) or their tokens more than max_tokens
+ * (HGCA_CACHE_TOKENS_FULL); what a sequence without room for it in its row asks for does
+ * not count.  The k-th granted block, in order of the sequences, is
+ * free_blocks[*free_count - 1 - k].  Entries of a row behind those in use stay as they
+ * are.  block_size of 1 and more. */
+int hgca_kv_plan(const hgca_block_state *state, const int32_t *n_new, int32_t max_tokens,
+                 int32_t *cu_out, int32_t *positions_out, int32_t *slots_out, void *hip_stream);
+
+/* Sequences are cut down to new_lens[b] tokens (device int32 [batch]; no longer than they
+ * are, 0 for one that has ended): the blocks behind go back on the stack, the last
+ * sequence's last one first, so that giving back what the last hgca_kv_plan granted makes
+ * the stack what it was.  new_lens may be lens itself. */
+int hgca_kv_release(const hgca_block_state *state, const int32_t *new_lens, void *hip_stream);
+
+/* Rows of packed tokens enter a tier: k_in, v_in are n_tokens rows of [Hkv, d] in
+ * shape.dtype, k_token_stride / v_token_stride elements apart (0: Hkv * d; a multiple of 16
+ * bytes), so that both may be parts of one projection's rows; token t goes to slot slots[t]
+ * (device int32 [n_tokens]) as hgca_kv_plan gives it, of a contiguous tier b * cap +
+ * position.  Tokens whose slot is not in [0, n_slots) are left out (n_slots: slots of the
+ * tier, its blocks times block_size or B * cap); slots differ from each other.  tier->k, v
+ * are written, its lengths and table not read (a contiguous tier has none).  k_in / v_in
+ * must not overlap the tier's rows (refused). */
+int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_slots,
+                  const int32_t *slots, const void *k_in, int64_t k_token_stride,
+                  const void *v_in, int64_t v_token_stride, int32_t n_tokens, void *hip_stream);
+
+/* Attention of packed new tokens over one tier that holds them already: the tokens of
+ * sequence b are rows cu[b] .. cu[b + 1] - 1 of q (device int32 [B + 1], ascending from 0; at
+ * most n_tokens; any number of them, 0 included), and the last ones of the tier, so that row cu[b] + i
+ * has position p = seq_lens[b] - (cu[b + 1] - cu[b]) + i.  Row t sees token j of the tier's
+ * valid ones where
+ *     j < prefix_lens[b], or
+ *     j >= first[t], j <= p (with HGCA_CHUNK_CAUSAL), and p - j < window (window > 0).
+ * prefix_lens (device int32 [B]), first (device int32 [n_tokens]) may be NULL, window 0: no
+ * such condition.  Its score is s = sm_scale <q, k_j>, capped, if softcap > 0, to softcap *
+ * tanh(s / softcap), and then, if slopes (device fp32 [Hq]) is given, less slopes[h] * |p - j|.
+ * q has q_token_stride elements from row to row (0: Hq * d; a multiple of 16 bytes).
+ * o_out is [n_tokens, Hq, d] in o_dtype, lse_out fp32 [n_tokens, Hq]; rows from cu[B] on are
+ * left as they are, a row that sees nothing gives O = 0, lse = -inf.  A row of the tier
+ * that a query does not see has no part in its O, whatever it holds; an infinity in a V row that
+ * it sees is in its O, infinities of both signs or a NaN make NaN.  fp32 O is accurate to
+ * fp32.  For bf16 O of bf16 inputs the weights enter the second product rounded once to
+ * bf16 (2^-9 of a weight, at random: as much again as O's own rounding), the sum that divides them does not.
+ * sm_scale must be positive and finite, scaled scores at most 2^126 in magnitude, softcap
+ * finite; tier->cap is at most 2^30.  Results do not depend on other calls and repeat bit for
+ * bit; where a sequence is cut into shares does depend on the batch.  ws needs
+ * hgca_chunk_workspace_bytes(shape, n_tokens, tier->cap), which also serves fewer tokens and
+ * smaller capacities. */
+enum { HGCA_CHUNK_CAUSAL = 1 };
+size_t hgca_chunk_workspace_bytes(const hgca_shape *shape, int32_t n_tokens, int32_t max_tokens);
+int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stride, const int32_t *cu,
+                    int32_t n_tokens, const hgca_kv_view *tier, int32_t flags, int32_t window,
+                    float softcap, const float *slopes, const int32_t *prefix_lens, const int32_t *first,
+                    void *o_out, int32_t o_dtype, float *lse_out,
+                    void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Which of n_drafts drafted tokens per sequence stay, by the target's probabilities, and the
+ * token that follows them (speculative sampling: what comes out is distributed as the
+ * target's own samples).  tokens is device int32 [B, n_drafts]; drafted token 0, the root, is taken
+ * as accepted (the token sampled last).  parents (device int32 [B, n_drafts], NULL: i - 1) names
+ * the token that each one follows; a token whose parent is not an earlier one, or which
+ * is not in [0, vocab), is in no tree.  target[b, i] and draft[b, i] are the distributions
+ * after token i, rows of vocab elements in p_dtype (fp32 or bf16), *_row_stride elements from
+ * token to token (0: vocab) and *_seq_stride from sequence to sequence (0: n_drafts rows);
+ * elements that are negative or not finite count as 0.  At token i, from the root on, the
+ * tokens that follow it are tried in order: x is accepted if u[b, j] * draft[b, i, x] <
+ * p(x), p = target[b, i] at first; after a refusal p is max(p - draft[b, i], 0) divided by its sum.  draft NULL
+ * (tokens chosen without chance): x is accepted if u[b, j] < p(x), and a refused one leaves
+ * p, which is divided by the sum of the rest.  Where no token is accepted any more one is
+ * drawn from p (from target[b, i] if nothing is left): the lowest x at which the running sum exceeds u_next[b] times the
+ * whole.  u (device fp32 [B, n_drafts], u[b, 0] is not used) and u_next ([B]) are uniform in [0, 1).
+ * Sums are fp64.  path_out ([B, n_drafts]) receives the accepted tokens' indices, root first, then -1,
+ * cnt_out ([B]) their number, the path and cnt of hgca_kv_commit; next_out ([B]) the drawn
+ * token, -1 where the row has no positive element.  1 <= n_drafts <= HGCA_MAX_DRAFTS, vocab at most 2^30.
+ * ws (8-byte aligned) needs hgca_verify_workspace_bytes(batch, vocab). */
+size_t hgca_verify_workspace_bytes(int32_t batch, int32_t vocab);
+int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p_dtype,
+                       const void *target, int64_t target_row_stride, int64_t target_seq_stride,
+                       const void *draft, int64_t draft_row_stride, int64_t draft_seq_stride,
+                       const int32_t *tokens, const int32_t *parents, const float *u, const float *u_next,
+                       int32_t *path_out, int32_t *cnt_out, int32_t *next_out,
+                       void *ws, size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

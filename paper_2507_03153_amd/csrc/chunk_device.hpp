@@ -1,0 +1,418 @@
+// What the kernels of packed chunks share (chunk_kernels.hip: bf16, chunk_f32_kernels.hip: fp32): how the work is cut, which
+// tokens a row sees, how a score becomes what the softmax runs over.
+#pragma once
+
+#include "tree_device.hpp"
+
+namespace hgca {
+
+namespace {
+
+constexpr int kChunkStep = kStepTokens;          // tokens of a step
+constexpr int kChunkWaves = kTreeWaves, kChunkBlock = kTreeBlock;
+static_assert(kChunkRows == 32 * kChunkWaves, "32 rows per wave");
+
+// ---- the cut ----
+// A sequence of n tokens has u = ceil(n * group / kChunkRows) units, each over at most `steps` steps of its tokens.  Units are cut into shares
+// of at most C steps, C = the steps of all units over the number of shares aimed at (and kChunkLeast at least): s = ceil(steps / C)
+// shares each, so that there are at most target + (number of units) shares, and at most 2 target in units that have several.
+// One long sequence among many short ones, a prompt among single tokens: a share is as long as any other.  Up to 64 sequences every wave works it
+// out for itself, a lane per sequence, from the lengths on the device; more are worked out by a launch before.
+constexpr int kChunkLeast = 4;
+
+struct SeqWork {
+    int n0, nq, len, pre;                        // first row of q, rows, tokens, tokens that all rows see
+    int units, steps;
+    __device__ __forceinline__ SeqWork(const ChunkArgs &a, int b) {
+        n0 = min(max(a.cu[b], 0), a.n_tokens);
+        nq = min(max(a.cu[b + 1], n0), a.n_tokens) - n0;
+        len = tier_len(a.kv, b);
+        pre = a.prefix ? min(max(a.prefix[b], 0), len) : 0;
+        units = (int)(((int64_t)nq * a.sh.group + kChunkRows - 1) / kChunkRows);
+        int64_t tokens = len;                    // that a unit's rows may see
+        if (a.causal) tokens = min(tokens, (int64_t)a.window + kChunkRows / a.sh.group + pre + 3 * kChunkStep);
+        steps = max((int)((tokens + kChunkStep - 1) / kChunkStep), 1);
+    }
+};
+
+__device__ __forceinline__ int share_steps(const ChunkArgs &a, float all) {
+    return max((int)(all / (float)a.target * 1.0001f) + 1, kChunkLeast);
+}
+// 0 for a sequence without new tokens
+__device__ __forceinline__ int shares_of(const SeqWork &q, int c) { return q.units > 0 ? (q.steps + c - 1) / c : 0; }
+
+// The entry of an ascending list at[0 .. n] with at[i] <= x < at[i + 1], by the lanes of a wave; -1: x >= at[n].
+__device__ __forceinline__ int wave_search(const int32_t *at, int n, int x) {
+    if (x >= at[n]) return -1;
+    const int lane = threadIdx.x % kWave;
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + kWave - 1) / kWave, i = lo + lane * step;
+        const int up = __popcll(__ballot(i < hi && at[min(i, n)] <= x));         // lane 0 is one of them
+        lo += (up - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+// A share of a unit, or (fold) a unit that has several.
+struct Place {
+    int b, unit, share, n_shares, part;          // part: where the unit's partials begin
+    bool idle;
+    // by slot of the launch, or, with FOLD, by number among the units with several shares
+    template <bool FOLD> __device__ __forceinline__ void find(const ChunkArgs &a, int x) {
+        const int B = a.sh.batch, lane = threadIdx.x % kWave;
+        int inside, units;
+        idle = true;
+        if (B <= kWave) {
+            units = n_shares = 0;
+            float work = 0.f;
+            int steps = 1;
+            if (lane < B) {
+                const SeqWork q(a, lane);
+                units = q.units;
+                steps = q.steps;
+                work = (float)units * (float)steps;
+            }
+            const int c = share_steps(a, wave_sum(work));
+            const int shares = units > 0 ? (steps + c - 1) / c : 0, slots = units * shares, several = shares > 1 ? slots : 0;
+            const int parts = (int)wave_inclusive_scan((uint32_t)several) - several;
+            const int mine = FOLD ? (shares > 1 ? units : 0) : slots, upto = (int)wave_inclusive_scan((uint32_t)mine);
+            const uint64_t behind = __ballot(upto > x);
+            if (behind == 0) return;
+            b = __builtin_ctzll(behind);
+            inside = x - (__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(mine, b));
+            units = __builtin_amdgcn_readlane(units, b);
+            n_shares = __builtin_amdgcn_readlane(shares, b);
+            part = __builtin_amdgcn_readlane(parts, b);
+        } else {
+            const int32_t *const slots = a.cut + 1, *const parts = slots + B + 1, *const several = parts + B + 1;
+            const int32_t *const list = FOLD ? several : slots;
+            b = wave_search(list, B, x);
+            if (b < 0) return;
+            inside = x - list[b];
+            const SeqWork q(a, b);
+            units = q.units;
+            n_shares = shares_of(q, a.cut[0]);
+            part = parts[b];
+        }
+        // the units of a share run side by side (they read the same tokens), those that see most first
+        share = FOLD ? 0 : inside / units;
+        unit = FOLD ? inside : units - 1 - inside % units;
+        part += unit * n_shares;
+        // (a list of beginnings that does not ascend can ask for more than there is)
+        idle = n_shares > 1 && (int64_t)part + n_shares > a.parts;
+    }
+};
+
+// ---- what a row sees ----
+struct RowSees {
+    int lo, hi, pre;                             // tokens [0, pre) and [lo, hi)
+    __device__ __forceinline__ RowSees(const ChunkArgs &a, const SeqWork &q, int query) {
+        const int p = q.len - q.nq + query;
+        pre = q.pre;
+        hi = a.causal ? min(p + 1, q.len) : q.len;
+        lo = a.window == INT32_MAX ? 0 : max(p - a.window + 1, 0);
+        if (a.first) lo = max(lo, a.first[q.n0 + query]);
+    }
+    // of the 64 tokens from `base` on
+    __device__ __forceinline__ uint64_t mask(int base) const {
+        auto below = [&](int x) {
+            const int n = x - base;
+            return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+        };
+        return below(pre) | (below(hi) & ~below(lo));
+    }
+};
+
+__device__ __forceinline__ int wave_min_int(int v) {
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) v = min(v, __shfl_xor(v, step));
+    return v;
+}
+__device__ __forceinline__ int wave_max_int(int v) {
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) v = max(v, __shfl_xor(v, step));
+    return v;
+}
+
+// What the rows of a wave see together: everything in [0, pre) and [all_lo, all_hi), nothing outside [0, pre) and [any_lo, any_hi).
+struct WaveSees {
+    int pre, all_lo, all_hi, any_lo, any_hi;
+    __device__ __forceinline__ WaveSees(const RowSees &r) {
+        pre = r.pre;
+        const bool some = r.hi > r.lo;
+        all_lo = __builtin_amdgcn_readfirstlane(wave_max_int(r.lo));
+        all_hi = __builtin_amdgcn_readfirstlane(wave_min_int(r.hi));
+        any_lo = __builtin_amdgcn_readfirstlane(wave_min_int(some ? r.lo : INT32_MAX));
+        any_hi = __builtin_amdgcn_readfirstlane(wave_max_int(some ? r.hi : 0));
+    }
+    __device__ __forceinline__ bool all(int t, int n) const { return t + n <= pre || (t >= all_lo && t + n <= all_hi); }
+    __device__ __forceinline__ bool none(int t, int n) const { return t >= pre && (t >= any_hi || t + n <= any_lo); }
+};
+
+// The steps of a share: those of the prefix and those from the first token that a row of the unit sees to the last.
+struct Steps {
+    int begin[2], end[2];
+    __device__ __forceinline__ Steps(int pre, int lo, int hi, int share, int n_shares) {
+        int head = (pre + kChunkStep - 1) / kChunkStep, from = 0, to = 0;
+        if (hi > lo) {
+            from = lo / kChunkStep;
+            to = (hi + kChunkStep - 1) / kChunkStep;
+        }
+        if (from <= head) {                      // one run
+            head = max(head, to);
+            from = to = head;
+        }
+        const int total = head + (to - from), per = (total + n_shares - 1) / n_shares;
+        const int i0 = min(share * per, total), i1 = min(i0 + per, total);
+        begin[0] = min(i0, head);
+        end[0] = min(i1, head);
+        begin[1] = from + max(i0 - head, 0);
+        end[1] = from + max(i1 - head, 0);
+    }
+};
+
+// ---- scores ----
+// kPlainScores: what the softmax runs over is the product, times sm_scale log2 e in the exponent of 2.  kCapped: tanh(product * sm_scale / cap), times
+// cap log2 e.  kBiased: the score itself in units of ln 2, capped or not, less slope * distance.
+enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
+
+// tanh x.  Up to kTanhNear it is x + x^3 P(x^2), P fitted to the least largest relative error (3.5e-7 with four terms, 1.5e-8 with
+// five); beyond, 1 - 2 / (1 + e^2x), whose rounding is then small against the result.
+constexpr float kTanhNear = 0.7f;
+template <bool FINE> __device__ __forceinline__ float tanh_near(float x) {
+    const float z = x * x;
+    const float p = FINE ? fmaf(z, fmaf(z, fmaf(z, fmaf(z, -0.00513866264f, 0.0200919714f), -0.0535588600f), 0.133291110f), -0.333331913f)
+                         : fmaf(z, fmaf(z, fmaf(z, 0.0139381709f, -0.0510163754f), 0.132876605f), -0.333310843f);
+    return fmaf(x * z, p, x);
+}
+template <bool FINE> __device__ __forceinline__ float tanh_any(float x) {
+    const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kTreeLog2e * fabsf(x))), 1.f);
+    return fabsf(x) <= kTanhNear ? tanh_near<FINE>(x) : copysignf(far, x);
+}
+
+template <int MODE, bool FINE> struct ScoreMap {
+    float k2;                                    // a weight is 2^(k2 * (what apply leaves) - its maximum's)
+    float kx, scale2, cap2, slope2;
+    __device__ __forceinline__ ScoreMap(const ChunkArgs &a, int head) {
+        scale2 = a.sh.sm_scale * kTreeLog2e;
+        kx = MODE == kPlainScores || a.cap <= 0.f ? 0.f : a.sh.sm_scale / a.cap;
+        cap2 = a.cap * kTreeLog2e;
+        slope2 = MODE == kBiased ? a.slopes[head] * kTreeLog2e : 0.f;
+        k2 = MODE == kPlainScores ? scale2 : MODE == kCapped ? cap2 : 1.f;
+    }
+    // c[t][r] is the product with token first + 32 t + 8 (r / 4) + r % 4 of a row at position pos
+    template <int NT> __device__ __forceinline__ void apply(floatx16 (&c)[NT], int pos, int first) const {
+        if constexpr (MODE == kPlainScores) return;
+        const float d = (float)(pos - first);
+        auto biased = [&](float x, float factor, int t, int r) {
+            return fmaf(-slope2, fabsf(d - (float)(32 * t + 8 * (r / 4) + r % 4)), x * factor);
+        };
+        if (MODE == kBiased && kx == 0.f) {      // uniform over the launch
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) c[t][r] = biased(c[t][r], scale2, t, r);
+            return;
+        }
+        float most = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(c[t][r]));
+        const bool near = !__any(!(most * kx <= kTanhNear));
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) c[t][r] = near ? tanh_near<FINE>(c[t][r] * kx) : tanh_any<FINE>(c[t][r] * kx);
+        if constexpr (MODE == kBiased) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) c[t][r] = biased(c[t][r], cap2, t, r);
+        }
+    }
+};
+
+// ---- infinities and NaN of V ----
+// A weight of 0 does not keep such a value out of a matrix product, and a weight, or a factor between shares, may be 0 for a row that does
+// see it.  Steps that some row of a wave does not see all of have them taken out of the operand; a workgroup that has taken some out, or whose
+// sums are not finite, goes through its steps of V once more, 64 tokens at a time, and notes which columns of which tokens hold which kind.
+template <int D> struct OddTokens {
+    unsigned long long bits[3][D];               // by kind (+inf, -inf, NaN) and column: bit j = the step's token j holds one
+    template <typename T>
+    __device__ void note(const ChunkArgs &a, int b, int kvh, int first, int end) {
+        constexpr int kPer = Elem<T>::kPerLoad, kPieces = D / kPer;
+        __syncthreads();                         // the last step's notes have been read
+        for (int i = threadIdx.x; i < 3 * D; i += kChunkBlock) (&bits[0][0])[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kChunkStep * kPieces; i += kChunkBlock) {
+            const int j = i / kPieces, piece = i % kPieces, tok = first + j;
+            if (tok >= end) continue;
+            int64_t row;
+            if (a.kv.block_table) {
+                const int32_t *const blocks = a.kv.block_table + (int64_t)b * a.kv.max_blocks + (a.kv.first_block ? a.kv.first_block[b] : 0);
+                row = ((int64_t)blocks[tok / a.kv.block_size] * a.sh.n_kv_heads + kvh) * a.kv.block_size + tok % a.kv.block_size;
+            } else {
+                row = ((int64_t)b * a.sh.n_kv_heads + kvh) * a.kv.cap + tok;
+            }
+            float x[kPer];
+            Elem<T>::expand(load16(a.kv.v + row * (int64_t)(D * sizeof(T)) + 16 * piece), x);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                if (fabsf(x[e]) < INFINITY) continue;
+                const int kind = x[e] == INFINITY ? 0 : x[e] == -INFINITY ? 1 : 2;
+                atomicOr(&bits[kind][piece * kPer + e], 1ull << j);
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// A row's sums after the loop: acc[dt][r] is column 32 dt + 8 (r / 4) + 4 hw + r % 4 of the lane's row.  Brings in what the values that the row
+// sees make of them, if any wave of the workgroup has met one.  All threads of the workgroup take part; s_odd and notes are LDS of its
+// own.
+template <typename T, int D>
+__device__ void settle_odd(const ChunkArgs &a, int b, int kvh, const RowSees &sees, const Steps &steps, int len, bool met, int (&s_odd)[kChunkWaves],
+                           OddTokens<D> &notes, floatx16 (&acc)[D / 32]) {
+    constexpr int DT = D / 32;
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, hw = lane / 32;
+    float z[4] = {0.f, 0.f, 0.f, 0.f};           // NaN where a sum is not finite
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[r % 4] = fmaf(acc[dt][r], 0.f, z[r % 4]);
+    const float all = (z[0] + z[1]) + (z[2] + z[3]);
+    met = __any(all != all) || met;
+    if (lane == 0) s_odd[w] = met;
+    __syncthreads();
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kChunkWaves; ++i) any = any || s_odd[i];
+    if (!any) return;                            // uniform over the workgroup
+    uint64_t kinds[3] = {0, 0, 0};               // a bit per element of acc
+    for (int part = 0; part < 2; ++part)
+        for (int s = steps.begin[part]; s < steps.end[part]; ++s) {
+            const int first = s * kChunkStep;
+            notes.template note<T>(a, b, kvh, first, len);
+            const uint64_t seen = sees.mask(first);
+#pragma unroll 1
+            for (int k = 0; k < 3; ++k) {
+                uint64_t got = 0;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (notes.bits[k][32 * dt + 8 * (r / 4) + 4 * hw + r % 4] & seen) got |= 1ull << (16 * dt + r);
+                kinds[0] |= k == 0 ? got : 0;
+                kinds[1] |= k == 1 ? got : 0;
+                kinds[2] |= k == 2 ? got : 0;
+            }
+        }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int i = 16 * dt + r;
+            const bool up = kinds[0] >> i & 1, down = kinds[1] >> i & 1, none = kinds[2] >> i & 1;
+            acc[dt][r] = none || (up && down) ? NAN : up ? INFINITY : down ? -INFINITY : acc[dt][r];
+        }
+}
+
+// Where a lane's row of a unit lies.
+struct RowPlace {
+    bool live;                                   // else the lane repeats the unit's last row and stores nothing
+    int query, head, row;                        // query of the sequence, head of the tensors, row of the unit
+    int64_t out;                                 // row of q, o and lse
+    __device__ __forceinline__ RowPlace(const ChunkArgs &a, const SeqWork &q, int unit, int kvh, int r) {
+        const int lg = __builtin_ctz(a.sh.group);
+        const int64_t i = (int64_t)unit * kChunkRows + r, rows = (int64_t)q.nq << lg;
+        live = i < rows;
+        const int64_t mine = live ? i : rows - 1;
+        row = r;
+        query = (int)(mine >> lg);
+        head = kvh * a.sh.group + (int)(mine & (a.sh.group - 1));
+        out = (int64_t)(q.n0 + query) * a.sh.n_q_heads + head;
+    }
+};
+
+// The unit's first and last seen token outside the prefix, over all its rows: s_range is LDS, cleared here.  lo and hi ascend with the row
+// but for `first`.
+__device__ __forceinline__ void unit_range(const WaveSees &w, int (&s_range)[2], int &lo, int &hi) {
+    if (threadIdx.x == 0) {
+        s_range[0] = INT32_MAX;
+        s_range[1] = 0;
+    }
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) {
+        atomicMin(&s_range[0], w.any_lo);
+        atomicMax(&s_range[1], w.any_hi);
+    }
+    __syncthreads();
+    lo = s_range[0];
+    hi = s_range[1];
+}
+
+// A row's result, or its share's partial: l over all tokens of the share, sums relative to 2^-shift.
+template <int D>
+__device__ __forceinline__ void store_row(const ChunkArgs &a, const Place &at, int kvh, const RowPlace &rp, float l, float shift,
+                                          const floatx16 (&acc)[D / 32]) {
+    if (!rp.live) return;
+    const int hw = threadIdx.x % kWave / 32;
+    const bool whole = at.n_shares == 1;
+    const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+    const int64_t to = whole ? rp.out : ((int64_t)(at.part + at.share) * a.sh.n_kv_heads + kvh) * kChunkRows + rp.row;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int64_t e = to * D + 32 * dt + 8 * q4 + 4 * hw;
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = whole && l == 0.f ? 0.f : acc[dt][4 * q4 + i] * inv;
+            if (whole && a.o_bf16)
+                *reinterpret_cast<uint2 *>(static_cast<char *>(a.o) + 2 * e) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+            else
+                *reinterpret_cast<float4 *>((whole ? static_cast<float *>(a.o) : a.part_o) + e) = make_float4(x[0], x[1], x[2], x[3]);
+        }
+    if (hw == 0) {
+        if (whole) {
+            a.lse[to] = l == 0.f ? -INFINITY : (__builtin_amdgcn_logf(l) - shift) * kLn2;
+        } else {
+            a.part_m[to] = l == 0.f ? -INFINITY : -shift;
+            a.part_l[to] = l;
+        }
+    }
+}
+
+// The running maximum, sum and rescaling of a row over a step's scores (as left by ScoreMap): returns the shift of a weight 2^(k2 c + shift).
+template <int DT> struct Running {
+    float m = -INFINITY, shift = 0.f, l = 0.f;   // shift: 0 for far rows (shift_of); l: over this lane's tokens
+    bool far = false;                            // uniform over the wave: a row of it is
+    template <int NT> __device__ __forceinline__ void update(floatx16 (&c)[NT], float k2, floatx16 (&acc)[DT]) {
+        float mx = c[0][0];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, c[t][r]);
+        if (__any(mx > m)) {                     // uniform over the wave
+            const float m_new = fmaxf(m, halves_max(mx)), to = shift_of(m_new, k2), corr = rescale_factor(m, m_new, k2);
+            m = m_new;
+            shift = is_far(to) ? 0.f : to;
+            far = __any(is_far(to));
+            l *= corr;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) acc[dt] *= corr;
+        }
+        if (far) {
+            const float less = is_far(shift_of(m, k2)) ? m : 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c[t] -= less;
+        }
+    }
+};
+
+}  // namespace
+
+}  // namespace hgca

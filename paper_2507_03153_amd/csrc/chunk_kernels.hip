@@ -1,0 +1,351 @@
+// Attention of packed new tokens, any number per sequence, over one tier, in bf16: causal or not, with a window, a prefix that all see, a
+// first token per row (documents), scores capped by a tanh, a bias by distance; and the fold of the shares that several workgroups went
+// through.
+//
+// Work unit: 128 rows (a row is one query of one head of the group), 32 per wave, and a share of the tokens that they see
+// (chunk_device.hpp).  K and V of a 64-token step go through a double-buffered LDS stage that all four waves read, brought in by LDS-direct
+// loads while the step before is worked on.  Products are 32 x 32 tiles of the matrix cores with the rows in the columns,
+//   S^T[token, row] = K . Q^T,  O^T[col, row] += V^T . P^T,
+// so that a lane's column is its row in both, a row's maximum and sum need one exchange between the wave's halves, and the scores as they come
+// out of the first product are the operand of the second.
+// A wave tells by its rows' ranges which steps all of them see (no mask), and which none (left out).
+#include <algorithm>
+#include <type_traits>
+
+#include "chunk_device.hpp"
+
+namespace hgca {
+
+namespace {
+
+template <int D, int PP, int MODE>
+__global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
+{
+    using S = DmaStage<D, kChunkWaves>;
+    constexpr int KK = D / 16, DT = D / 32, NT = kChunkStep / 32;
+    __shared__ __attribute__((aligned(1024))) char s_k0[S::kBytes];
+    __shared__ __attribute__((aligned(1024))) char s_k1[S::kBytes];
+    __shared__ __attribute__((aligned(1024))) char s_v0[S::kBytes];
+    __shared__ __attribute__((aligned(1024))) char s_v1[S::kBytes];
+    __shared__ uint32_t s_row[kSub];
+    __shared__ int s_odd[kChunkWaves], s_range[2];
+
+    const int kvh = blockIdx.x % a.sh.n_kv_heads;
+    Place at;
+    at.find<false>(a, blockIdx.x / a.sh.n_kv_heads);
+    if (at.idle) return;                         // uniform over the workgroup
+    const SeqWork seq(a, at.b);
+    const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
+    const RowPlace rp(a, seq, at.unit, kvh, 32 * w + n);
+    const bool wave_live = __any(rp.live);       // uniform over the wave
+    uint4 qop[KK];
+    {
+        const char *const q = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * S::kRowBytes;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) qop[kk] = load16(q + 16 * (2 * kk + hw));
+    }
+    const RowSees sees(a, seq, rp.query);
+    const WaveSees wave(sees);
+    int lo, hi;
+    unit_range(wave, s_range, lo, hi);
+    const Steps steps(seq.pre, lo, hi, at.share, at.n_shares);
+    const int pos = seq.len - seq.nq + rp.query;
+    const ScoreMap<MODE, PP != 1> map(a, rp.head);
+    int k_lane[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) k_lane[kk] = S::k_offset(n, 2 * kk + hw);
+    const int v_lane = S::v_offset(4 * hw + lane % 16 / 4, lane / 16 % 2) + 8 * (lane % 4);
+
+    bool met_odd = false;                        // uniform over the wave
+    Running<DT> run;
+    floatx16 acc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = floatx16{};
+
+    // One step.  c[t][r] is the score of step token 32 t + 8 (r / 4) + 4 hw + r % 4; group g of the second product is 16 tokens, of
+    // which the lane holds eight.
+    auto body = [&](auto masked, const char *k_stage, const char *v_stage, int tok) {
+        constexpr bool MASKED = decltype(masked)::value;
+        floatx16 c[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) c[t] = floatx16{};
+        uint4 kf[KK][NT];
+        auto read_slice = [&](int kk) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) kf[kk][t] = *reinterpret_cast<const uint4 *>(k_stage + t * 32 * S::kRowBytes + k_lane[kk]);
+        };
+        read_slice(0);
+        read_slice(1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {        // operands are read two slices ahead
+            if (kk + 2 < KK) read_slice(kk + 2);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c[t] = score_mfma(kf[kk][t], qop[kk], c[t]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        uint4 vop[2][DT];
+        auto read_v = [&](int g, uint4 (&x)[DT]) {
+            const char *v = v_stage + S::v_offset(16 * g, 0) + v_lane;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const short4v x0 = lds_read_tr16(v + 256 * dt), x1 = lds_read_tr16(v + S::v_offset(8, 0) + 256 * dt);
+                const short8v both = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+                x[dt] = __builtin_bit_cast(uint4, both);
+            }
+        };
+        read_v(0, vop[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        map.apply(c, pos, tok + 4 * hw);
+        if constexpr (MASKED) {
+            const uint64_t seen = sees.mask(tok + 4 * hw);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!(seen >> (32 * t + 8 * (r / 4) + r % 4) & 1)) c[t][r] = -INFINITY;
+        }
+        run.update(c, map.k2, acc);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint32_t part[PP][4];
+        auto weigh = [&](int g) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float p[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    p[x] = __builtin_amdgcn_exp2f(fmaf(c[g / 2][8 * (g % 2) + 2 * e + x], map.k2, run.shift));   // masked scores give 0
+                    sum[(2 * e + x) % 4] += p[x];
+                }
+#pragma unroll
+                for (int t = 0; t < PP; ++t) {
+                    part[t][e] = pack_bf16(p[0], p[1]);
+                    if (t + 1 < PP) {
+                        p[0] -= __uint_as_float(part[t][e] << 16);
+                        p[1] -= __uint_as_float(part[t][e] & 0xffff0000u);
+                    }
+                }
+            }
+        };
+        weigh(0);
+#pragma unroll
+        for (int g = 0; g < 2 * NT; ++g) {
+            __builtin_amdgcn_sched_barrier(0);
+            uint4(&v)[DT] = vop[g % 2];
+            if (g + 1 < 2 * NT) read_v(g + 1, vop[(g + 1) % 2]);
+            if constexpr (MASKED) {              // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
+                uint32_t odd = 0;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) odd |= odd_carry(v[dt].x) | odd_carry(v[dt].y) | odd_carry(v[dt].z) | odd_carry(v[dt].w);
+                if (__any((odd & kSigns) != 0)) {
+                    met_odd = true;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        uint4 &x = v[dt];
+                        x = make_uint4(x.x & ~odd_halves(x.x), x.y & ~odd_halves(x.y), x.z & ~odd_halves(x.z), x.w & ~odd_halves(x.w));
+                    }
+                }
+            }
+            uint32_t now[PP][4];
+#pragma unroll
+            for (int t = 0; t < PP; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) now[t][e] = part[t][e];
+#pragma unroll
+            for (int t = 0; t < PP; ++t)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+                    acc[dt] = score_mfma(v[dt], make_uint4(now[t][0], now[t][1], now[t][2], now[t][3]), acc[dt]);
+            if (g + 1 < 2 * NT) weigh(g + 1);
+        }
+        run.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+
+#pragma unroll 1
+    for (int range = 0; range < 2; ++range) {
+        const int from = steps.begin[range] * kChunkStep, total = min(steps.end[range] * kChunkStep, seq.len) - from;
+        const int sub_len = pass_length(a.kv, total);
+#pragma unroll 1
+        for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
+            const int nsub = min(sub_len, total - sub0), first = from + sub0, count = (nsub + kChunkStep - 1) / kChunkStep;
+            __syncthreads();                     // the previous table and stages are no longer in use
+            const BlockRows where = make_block_rows<kChunkBlock>(s_row, a.kv, a.sh.n_kv_heads, at.b, kvh, first, nsub);
+            dma_step<D, kChunkWaves, 0, 0>(a.kv, where, 0, nsub, s_k0, s_v0);
+            // Step s reads the stages of its parity, and the rows of step s + 1 go to those of the other parity, which were last read in
+            // step s - 1: the barrier at its top orders both.
+            auto step = [&](int s, const char *k_cur, const char *v_cur, char *k_next, char *v_next) {
+                wait_for_own_loads();            // the barrier alone does not wait for LDS-direct loads
+                __syncthreads();
+                if (s + 1 < count) dma_step<D, kChunkWaves, 0, 0>(a.kv, where, s + 1, nsub, k_next, v_next);
+                const int tok = first + s * kChunkStep;
+                if (!wave_live || wave.none(tok, kChunkStep)) return;
+                if (wave.all(tok, kChunkStep)) body(std::false_type{}, k_cur, v_cur, tok);
+                else body(std::true_type{}, k_cur, v_cur, tok);
+            };
+            for (int s = 0; s < count; s += 2) {
+                step(s, s_k0, s_v0, s_k1, s_v1);
+                if (s + 1 < count) step(s + 1, s_k1, s_v1, s_k0, s_v0);
+            }
+        }
+    }
+
+    __syncthreads();                             // all waves have read the stages
+    OddTokens<D> &notes = *reinterpret_cast<OddTokens<D> *>(s_v1);
+    static_assert(sizeof(OddTokens<D>) <= sizeof(s_v1), "the notes lie in a stage");
+    settle_odd<bf16_t, D>(a, at.b, kvh, sees, steps, seq.len, met_odd, s_odd, notes, acc);
+    store_row<D>(a, at, kvh, rp, halves_sum(run.l), shift_of(run.m, map.k2), acc);
+}
+
+// ---- more than 64 sequences: the cut by a launch of its own ----
+
+constexpr int kCutBlock = 1024, kCutWaves = kCutBlock / kWave;
+
+__global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
+{
+    __shared__ float s_work[kCutWaves];
+    __shared__ uint32_t s_sum[3][kCutWaves];
+    const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, B = a.sh.batch;
+    float work = 0.f;
+    for (int b = tid; b < B; b += kCutBlock) {
+        const SeqWork q(a, b);
+        work += (float)q.units * (float)q.steps;
+    }
+    work = wave_sum(work);
+    if (lane == 0) s_work[w] = work;
+    __syncthreads();
+    work = s_work[0];
+#pragma unroll
+    for (int i = 1; i < kCutWaves; ++i) work += s_work[i];
+    const int c = share_steps(a, work);
+    int32_t *const lists = a.cut + 1;            // three lists of B + 1 beginnings: slots, partials, units with several shares
+    if (tid == 0) a.cut[0] = c;
+    if (tid < 3) lists[tid * (B + 1)] = 0;
+    uint32_t base[3] = {0, 0, 0};
+    for (int b0 = 0; b0 < B; b0 += kCutBlock) {
+        const int b = b0 + tid;
+        uint32_t v[3] = {0, 0, 0};
+        if (b < B) {
+            const SeqWork q(a, b);
+            const int n = shares_of(q, c);
+            v[0] = (uint32_t)q.units * n;
+            v[1] = n > 1 ? v[0] : 0;
+            v[2] = n > 1 ? q.units : 0;
+        }
+        __syncthreads();
+        for (int k = 0; k < 3; ++k) {
+            v[k] = wave_inclusive_scan(v[k]);
+            if (lane == kWave - 1) s_sum[k][w] = v[k];
+        }
+        __syncthreads();
+        for (int k = 0; k < 3; ++k) {
+            uint32_t before = base[k];
+            for (int i = 0; i < kCutWaves; ++i) {
+                before += i < w ? s_sum[k][i] : 0;
+                base[k] += s_sum[k][i];
+            }
+            if (b < B) lists[k * (B + 1) + b + 1] = (int32_t)min(before + v[k], 0x7fffffffu);
+        }
+    }
+}
+
+// ---- the fold ----
+
+constexpr int kChunkFoldRows = 8;                // rows of a workgroup
+
+// Rows of a unit that has several shares: O = sum o_s 2^(m_s - M) / L, L = sum l_s 2^(m_s - M), m_s in powers of 2.  A row's columns are held by D / 4
+// lanes, four each; where a unit has fewer rows than a workgroup takes, several sets of lanes share a row's partials.
+template <int D>
+__global__ __launch_bounds__(kChunkFoldRows * D / 4) void chunk_fold_kernel(ChunkArgs a)
+{
+    constexpr int C4 = D / 4;
+    __shared__ float4 s_acc[kChunkFoldRows][C4];
+    __shared__ float s_m[kChunkFoldRows], s_l[kChunkFoldRows];
+    const int kvh = blockIdx.y, set = threadIdx.x / C4, c4 = threadIdx.x % C4;
+    Place at;
+    at.find<true>(a, blockIdx.x);
+    if (at.idle) return;                         // uniform over the workgroup
+    const SeqWork seq(a, at.b);
+    const int64_t left = ((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows;
+    const int rows = (int)min(left, (int64_t)kChunkRows) - (int)blockIdx.z * kChunkFoldRows;         // from this workgroup's first on
+    if (rows <= 0) return;
+    int per_row = 1;                             // sets of lanes that share a row
+    while (per_row * 2 * rows <= kChunkFoldRows) per_row *= 2;
+    const int mine = set / per_row, r = blockIdx.z * kChunkFoldRows + min(mine, rows - 1);
+    float m = -INFINITY, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto join = [](float &m0, float &l0, float4 &a0, float m1, float l1, const float4 &a1) {
+        const float top = fmaxf(m0, m1), to = top == -INFINITY ? 0.f : top;
+        const float f0 = __builtin_amdgcn_exp2f(m0 - to), f1 = __builtin_amdgcn_exp2f(m1 - to);
+        // an infinity or NaN stays what it is, whatever its share weighs
+        auto one = [&](float x, float y) {
+            const float p = fabsf(x) < INFINITY ? x * f0 : x, q = fabsf(y) < INFINITY ? y * f1 : y;
+            return p + q;
+        };
+        l0 = one(l0, l1);
+        a0 = make_float4(one(a0.x, a1.x), one(a0.y, a1.y), one(a0.z, a1.z), one(a0.w, a1.w));
+        m0 = top;
+    };
+#pragma unroll 4
+    for (int s = set % per_row; s < at.n_shares; s += per_row) {
+        const int64_t i = ((int64_t)(at.part + s) * a.sh.n_kv_heads + kvh) * kChunkRows + r;
+        join(m, l, acc, a.part_m[i], a.part_l[i], *reinterpret_cast<const float4 *>(a.part_o + i * D + 4 * c4));
+    }
+    if (per_row > 1) {                           // uniform over the workgroup
+        s_acc[set][c4] = acc;
+        if (c4 == 0) {
+            s_m[set] = m;
+            s_l[set] = l;
+        }
+        __syncthreads();
+        if (set % per_row) return;
+        for (int i = 1; i < per_row; ++i) join(m, l, acc, s_m[set + i], s_l[set + i], s_acc[set + i][c4]);
+    }
+    if (mine >= rows) return;
+    const RowPlace rp(a, seq, at.unit, kvh, r);
+    const bool none = l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    const float x[4] = {none ? 0.f : acc.x * inv, none ? 0.f : acc.y * inv, none ? 0.f : acc.z * inv, none ? 0.f : acc.w * inv};
+    if (a.o_bf16)
+        *reinterpret_cast<uint2 *>(static_cast<char *>(a.o) + 2 * (rp.out * D + 4 * c4)) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    else
+        *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + rp.out * D + 4 * c4) = make_float4(x[0], x[1], x[2], x[3]);
+    if (c4 == 0) a.lse[rp.out] = none ? -INFINITY : (__builtin_amdgcn_logf(l) + m) * kLn2;
+}
+
+}  // namespace
+
+hipError_t launch_chunk_rows_bf16(int head_dim, const ChunkArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((int64_t)a.slots * a.sh.n_kv_heads)), block(kChunkBlock);
+    const int mode = a.slopes ? kBiased : a.cap > 0.f ? kCapped : kPlainScores;
+#define HGCA_CHUNK(D, PP)                                                                                          \
+    do {                                                                                                           \
+        if (mode == kPlainScores) hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kPlainScores>), grid, block, 0, s, a); \
+        else if (mode == kCapped) hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kCapped>), grid, block, 0, s, a);   \
+        else hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kBiased>), grid, block, 0, s, a);                        \
+    } while (0)
+    if (head_dim == 64 && a.o_bf16) HGCA_CHUNK(64, 1);
+    else if (head_dim == 64) HGCA_CHUNK(64, 3);
+    else if (a.o_bf16) HGCA_CHUNK(128, 1);
+    else HGCA_CHUNK(128, 3);
+#undef HGCA_CHUNK
+    return hipGetLastError();
+}
+
+hipError_t launch_chunk_attn(int dtype, int head_dim, const ChunkArgs &a, hipStream_t s)
+{
+    hipError_t rc;
+    if (a.sh.batch > kWave) {
+        hipLaunchKernelGGL(chunk_cut_kernel, dim3(1), dim3(kCutBlock), 0, s, a);
+        if ((rc = hipGetLastError()) != hipSuccess) return rc;
+    }
+    rc = dtype == 0 ? launch_chunk_rows_f32(head_dim, a, s) : launch_chunk_rows_bf16(head_dim, a, s);
+    if (rc != hipSuccess || a.parts == 0) return rc;
+    // a unit with several shares has two at least
+    const dim3 grid((unsigned)std::max(a.parts / 2, 1), (unsigned)a.sh.n_kv_heads, kChunkRows / kChunkFoldRows);
+    if (head_dim == 64) hipLaunchKernelGGL(chunk_fold_kernel<64>, grid, dim3(kChunkFoldRows * 64 / 4), 0, s, a);
+    else hipLaunchKernelGGL(chunk_fold_kernel<128>, grid, dim3(kChunkFoldRows * 128 / 4), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace hgca

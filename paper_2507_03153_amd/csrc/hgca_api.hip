@@ -361,6 +361,62 @@ int check_kv8(const hgca_shape *s, const hgca_kv8_view *k8, hgca_kv_view *rows)
     return HGCA_OK;
 }
 
+// ---- a server's step: plans, packed chunks ----
+
+int check_blocks(const hgca_block_state *t)
+{
+    if (!t || t->batch < 0 || t->block_size < 1 || t->max_blocks < 0 || t->n_blocks < 0) return HGCA_ERR_INVALID_ARG;
+    if (t->batch > 65535 || t->max_blocks > kMaxRowsCap || (int64_t)t->max_blocks * t->block_size > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
+    if ((int64_t)t->n_blocks * t->block_size > INT32_MAX) return HGCA_ERR_UNSUPPORTED;
+    if (t->batch == 0) return HGCA_OK;
+    if (!t->held || !t->lens || !t->free_count || !t->scratch) return HGCA_ERR_INVALID_ARG;
+    if ((t->max_blocks > 0 && !t->block_table) || (t->n_blocks > 0 && !t->free_blocks)) return HGCA_ERR_INVALID_ARG;
+    return HGCA_OK;
+}
+
+PlanArgs plan_args(const hgca_block_state *t)
+{
+    PlanArgs a{};
+    a.table = t->block_table;
+    a.held = t->held;
+    a.lens = t->lens;
+    a.free_blocks = t->free_blocks;
+    a.free_count = t->free_count;
+    a.status = t->status;
+    a.scratch = t->scratch;
+    a.batch = t->batch;
+    a.block_size = t->block_size;
+    a.max_blocks = t->max_blocks;
+    a.n_blocks = t->n_blocks;
+    return a;
+}
+
+// Shares of a chunk call (chunk_device.hpp): about this many workgroups, two per compute unit.
+#ifndef HGCA_TARGET_WGS_CHUNK
+#define HGCA_TARGET_WGS_CHUNK 512
+#endif
+struct ChunkLayout {
+    int64_t slots, parts, target;                // per KV head
+    size_t part_m, part_l, cut, total;
+};
+
+ChunkLayout chunk_layout(const hgca_shape *s, int64_t n_tokens, int64_t cap)
+{
+    ChunkLayout t{};
+    const int64_t units = n_tokens * group_of(s) / kChunkRows + std::min<int64_t>(n_tokens, s->batch);       // at most
+    t.target = std::max<int64_t>(1, HGCA_TARGET_WGS_CHUNK / s->n_kv_heads);
+    // a share has 256 tokens at least, so a unit has so many at most, and one where the tier is that short
+    const int64_t shares = std::max<int64_t>(1, (cap + 255) / 256);
+    t.slots = std::min(t.target + units, units * shares);
+    t.parts = shares > 1 ? std::min(2 * t.target, units * shares) : 0;
+    const size_t rows = (size_t)t.parts * s->n_kv_heads * kChunkRows;
+    t.part_m = align_up(rows * s->head_dim * sizeof(float));
+    t.part_l = t.part_m + align_up(rows * sizeof(float));
+    t.cut = t.part_l + align_up(rows * sizeof(float));
+    t.total = t.cut + align_up((3 * (size_t)s->batch + 4) * sizeof(int32_t));
+    return t;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1707,6 +1763,194 @@ int hgca_kv8_attn(const hgca_shape *shape, const void *q, int32_t n_q, const hgc
     a.k_scale = static_cast<const char *>(kv8->k_scale);
     a.v_scale = static_cast<const char *>(kv8->v_scale);
     return rows_attention(shape, q, n_q, true, a, o_out, o_dtype, lse_out, ws, ws_bytes, hip_stream);
+}
+
+// ---- a server's step ----
+
+int hgca_kv_plan(const hgca_block_state *state, const int32_t *n_new, int32_t max_tokens, int32_t *cu_out, int32_t *positions_out,
+                 int32_t *slots_out, void *hip_stream)
+{
+    int rc = check_blocks(state);
+    if (rc != HGCA_OK) return rc;
+    if (max_tokens < 0) return HGCA_ERR_INVALID_ARG;
+    if (max_tokens > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
+    if (state->batch == 0) return HGCA_OK;
+    if (!n_new || !cu_out || (max_tokens > 0 && (!positions_out || !slots_out))) return HGCA_ERR_INVALID_ARG;
+    // the outputs are written while the state and n_new are still read
+    const int64_t B = state->batch;
+    const Range outs[3] = {Range(cu_out, 4 * (B + 1)), Range(positions_out, 4 * (int64_t)max_tokens), Range(slots_out, 4 * (int64_t)max_tokens)};
+    const Range ins[8] = {Range(n_new, 4 * B), Range(state->held, 4 * B), Range(state->lens, 4 * B), Range(state->free_count, 4),
+                          Range(state->scratch, 4 * (3 * B + 1)), Range(state->block_table, 4 * B * state->max_blocks),
+                          Range(state->free_blocks, 4 * (int64_t)state->n_blocks), Range(state->status, state->status ? 4 : 0)};
+    for (int i = 0; i < 3; ++i) {
+        for (const Range &in : ins)
+            if (outs[i].bytes && in.bytes && outs[i].meets(in)) return HGCA_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (outs[i].bytes && outs[i].meets(outs[j])) return HGCA_ERR_INVALID_ARG;
+    }
+    if (ins[0].meets(ins[1]) || ins[0].meets(ins[2]) || ins[0].meets(ins[4])) return HGCA_ERR_INVALID_ARG;
+    PlanArgs a = plan_args(state);
+    a.n_new = n_new;
+    a.max_tokens = max_tokens;
+    a.cu = cu_out;
+    a.positions = positions_out;
+    a.slots = slots_out;
+    return from_hip(launch_kv_plan(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int hgca_kv_release(const hgca_block_state *state, const int32_t *new_lens, void *hip_stream)
+{
+    int rc = check_blocks(state);
+    if (rc != HGCA_OK || state->batch == 0) return rc;
+    if (!new_lens) return HGCA_ERR_INVALID_ARG;
+    const int64_t B = state->batch;
+    const Range in(new_lens, 4 * B);
+    if (in.meets(Range(state->held, 4 * B)) || in.meets(Range(state->free_blocks, 4 * (int64_t)state->n_blocks)) ||
+        in.meets(Range(state->free_count, 4)) || (new_lens != state->lens && in.meets(Range(state->lens, 4 * B))))
+        return HGCA_ERR_INVALID_ARG;
+    PlanArgs a = plan_args(state);
+    a.new_lens = new_lens;
+    return from_hip(launch_kv_release(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_slots, const int32_t *slots, const void *k_in,
+                  int64_t k_token_stride, const void *v_in, int64_t v_token_stride, int32_t n_tokens, void *hip_stream)
+{
+    int rc = check_shape(shape);
+    if (rc != HGCA_OK) return rc;
+    if ((rc = check_view(shape, tier, true)) != HGCA_OK) return rc;
+    if (n_tokens < 0 || n_slots < 0) return HGCA_ERR_INVALID_ARG;
+    const int64_t per_block = tier->block_table ? tier->block_size : std::max(tier->cap, 1);
+    if (!tier->block_table && n_slots > (int64_t)shape->batch * tier->cap) return HGCA_ERR_INVALID_ARG;
+    if (n_slots >= int64_t(1) << 31 || n_slots * shape->n_kv_heads >= int64_t(1) << 32) return HGCA_ERR_UNSUPPORTED;
+    if (shape->batch == 0 || n_tokens == 0 || n_slots == 0) return HGCA_OK;
+    const int64_t e = shape->dtype == HGCA_BF16 ? 2 : 4, row = shape->head_dim * e, token = shape->n_kv_heads * row;
+    const int64_t ks = k_token_stride ? k_token_stride * e : token, vs = v_token_stride ? v_token_stride * e : token;
+    if (!slots || !k_in || !v_in || !aligned16(k_in) || !aligned16(v_in) || !tier->k || !tier->v) return HGCA_ERR_INVALID_ARG;
+    if (ks < token || vs < token || ks % 16 != 0 || vs % 16 != 0) return HGCA_ERR_INVALID_ARG;
+    // offsets stay far from 2^63, threads of the grid below 2^32
+    if (ks > (int64_t(1) << 42) / n_tokens || vs > (int64_t(1) << 42) / n_tokens || n_tokens > 1 << 23) return HGCA_ERR_UNSUPPORTED;
+    const int64_t rows = n_slots / per_block * per_block * token;
+    for (const void *out : {tier->k, tier->v}) {
+        const Range to(out, rows);
+        if (to.meets(Range(k_in, (n_tokens - 1) * ks + token)) || to.meets(Range(v_in, (n_tokens - 1) * vs + token)) ||
+            to.meets(Range(slots, 4 * (int64_t)n_tokens)))
+            return HGCA_ERR_INVALID_ARG;
+    }
+    WriteArgs a{};
+    a.k = static_cast<char *>(const_cast<void *>(tier->k));
+    a.v = static_cast<char *>(const_cast<void *>(tier->v));
+    a.k_in = static_cast<const char *>(k_in);
+    a.v_in = static_cast<const char *>(v_in);
+    a.k_stride = ks;
+    a.v_stride = vs;
+    a.slots = slots;
+    a.n_tokens = n_tokens;
+    a.n_kv_heads = shape->n_kv_heads;
+    a.row_bytes = (int32_t)row;
+    a.per_block = (int32_t)per_block;
+    a.n_slots = (int32_t)(n_slots / per_block * per_block);      // whole blocks
+    return from_hip(launch_kv_write(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t hgca_chunk_workspace_bytes(const hgca_shape *shape, int32_t n_tokens, int32_t max_tokens)
+{
+    if (check_shape(shape) != HGCA_OK || n_tokens < 0 || max_tokens < 0) return 0;
+    return chunk_layout(shape, n_tokens, max_tokens).total;
+}
+
+int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stride, const int32_t *cu, int32_t n_tokens,
+                    const hgca_kv_view *tier, int32_t flags, int32_t window, float softcap, const float *slopes,
+                    const int32_t *prefix_lens, const int32_t *first, void *o_out, int32_t o_dtype, float *lse_out,
+                    void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_shape(shape);
+    if (rc != HGCA_OK) return rc;
+    if ((rc = check_view(shape, tier, true)) != HGCA_OK) return rc;
+    if (n_tokens < 0 || (flags & ~HGCA_CHUNK_CAUSAL) || window < 0 || !(softcap >= 0.f) || softcap > 2.0e38f) return HGCA_ERR_INVALID_ARG;
+    if (!(shape->sm_scale > 0.f) || shape->sm_scale > 2.0e38f) return HGCA_ERR_INVALID_ARG;
+    if (softcap > 0.f && !(shape->sm_scale / softcap > 0.f && shape->sm_scale / softcap < 2.0e38f)) return HGCA_ERR_INVALID_ARG;
+    if (tier->cap > kMaxRowsCap || (o_dtype != HGCA_F32 && o_dtype != HGCA_BF16)) return HGCA_ERR_UNSUPPORTED;
+    if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
+    const int64_t e = shape->dtype == HGCA_BF16 ? 2 : 4, token = (int64_t)shape->n_q_heads * shape->head_dim;
+    const int64_t qs = q_token_stride ? q_token_stride : token;
+    if (!q || !aligned16(q) || !cu || !o_out || !aligned16(o_out) || !lse_out) return HGCA_ERR_INVALID_ARG;
+    if (qs < token || qs * e % 16 != 0) return HGCA_ERR_INVALID_ARG;
+    const ChunkLayout t = chunk_layout(shape, n_tokens, tier->cap);
+    // threads of a flat grid are counted in 32 bits; offsets stay far from 2^63
+    if (t.slots * shape->n_kv_heads > int64_t(1) << 23 || qs > (int64_t(1) << 40) / n_tokens) return HGCA_ERR_UNSUPPORTED;
+    if (!ws || ws_bytes < t.total || !aligned16(ws)) return HGCA_ERR_WORKSPACE;
+    char *const base = static_cast<char *>(ws);
+    ChunkArgs a{};
+    a.sh = to_dev(shape);
+    a.q = static_cast<const char *>(q);
+    a.q_stride = qs * e;
+    a.cu = cu;
+    a.kv = to_dev(tier);
+    a.n_tokens = n_tokens;
+    a.causal = flags & HGCA_CHUNK_CAUSAL ? 1 : 0;
+    a.window = window > 0 && window < kMaxRowsCap ? window : INT32_MAX;          // (no two tokens are further apart)
+    a.cap = softcap;
+    a.slopes = slopes;
+    a.prefix = prefix_lens;
+    a.first = first;
+    a.o_bf16 = o_dtype == HGCA_BF16;
+    a.o = o_out;
+    a.lse = lse_out;
+    a.slots = (int32_t)t.slots;
+    a.parts = (int32_t)t.parts;
+    a.target = (int32_t)t.target;
+    a.cut = reinterpret_cast<int32_t *>(base + t.cut);
+    a.part_o = reinterpret_cast<float *>(base);
+    a.part_m = reinterpret_cast<float *>(base + t.part_m);
+    a.part_l = reinterpret_cast<float *>(base + t.part_l);
+    return from_hip(launch_chunk_attn(shape->dtype, shape->head_dim, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t hgca_verify_workspace_bytes(int32_t batch, int32_t vocab)
+{
+    if (batch < 0 || vocab < 1) return 0;
+    return std::max<size_t>(kAlign, align_up((size_t)batch * (((size_t)vocab + kVerifySegment - 1) / kVerifySegment) * sizeof(double)));
+}
+
+int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p_dtype, const void *target, int64_t target_row_stride,
+                       int64_t target_seq_stride, const void *draft, int64_t draft_row_stride, int64_t draft_seq_stride,
+                       const int32_t *tokens, const int32_t *parents, const float *u, const float *u_next, int32_t *path_out,
+                       int32_t *cnt_out, int32_t *next_out, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    if (batch < 0 || n_drafts < 1 || vocab < 1) return HGCA_ERR_INVALID_ARG;
+    if (batch > 65535 || n_drafts > HGCA_MAX_DRAFTS || vocab > kMaxRowsCap) return HGCA_ERR_UNSUPPORTED;
+    if (p_dtype != HGCA_F32 && p_dtype != HGCA_BF16) return HGCA_ERR_UNSUPPORTED;
+    if (batch == 0) return HGCA_OK;
+    if (!target || !tokens || !u || !u_next || !path_out || !cnt_out || !next_out) return HGCA_ERR_INVALID_ARG;
+    const uintptr_t e = p_dtype == HGCA_BF16 ? 2 : 4;
+    if (reinterpret_cast<uintptr_t>(target) % e != 0 || reinterpret_cast<uintptr_t>(draft) % e != 0) return HGCA_ERR_INVALID_ARG;
+    const int64_t tr = target_row_stride ? target_row_stride : vocab, dr = draft_row_stride ? draft_row_stride : vocab;
+    const int64_t most = int64_t(1) << 40;       // offsets stay far from 2^63
+    if (tr < vocab || dr < vocab || target_seq_stride < 0 || draft_seq_stride < 0) return HGCA_ERR_INVALID_ARG;
+    if (tr > most / HGCA_MAX_DRAFTS || dr > most / HGCA_MAX_DRAFTS) return HGCA_ERR_UNSUPPORTED;
+    const int64_t ts = target_seq_stride ? target_seq_stride : tr * n_drafts, ds = draft_seq_stride ? draft_seq_stride : dr * n_drafts;
+    if (ts > most || ds > most) return HGCA_ERR_UNSUPPORTED;
+    if (!ws || ws_bytes < hgca_verify_workspace_bytes(batch, vocab) || reinterpret_cast<uintptr_t>(ws) % 8 != 0) return HGCA_ERR_WORKSPACE;
+    VerifyArgs a{};
+    a.target = static_cast<const char *>(target);
+    a.draft = static_cast<const char *>(draft);
+    a.target_row = tr;
+    a.target_seq = ts;
+    a.draft_row = dr;
+    a.draft_seq = ds;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.u = u;
+    a.u_next = u_next;
+    a.path = path_out;
+    a.cnt = cnt_out;
+    a.next = next_out;
+    a.sums = static_cast<double *>(ws);
+    a.batch = batch;
+    a.n = n_drafts;
+    a.vocab = vocab;
+    return from_hip(launch_verify_drafts(p_dtype, a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

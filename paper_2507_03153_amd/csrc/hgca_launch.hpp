@@ -323,4 +323,70 @@ hipError_t launch_tree_attn(int dtype, int head_dim, bool kv8, const TreeArgs &a
 // the splits with 128 rows per workgroup (bf16 queries; called by launch_tree_attn)
 hipError_t launch_tree_rows(int head_dim, bool kv8, const TreeArgs &a, int batch, hipStream_t s);
 
+// ---- a server's step: plans of tokens and blocks, packed rows, attention of packed chunks, verification of drafts ----
+
+struct PlanArgs {
+    int32_t *table, *held, *lens;         // [B, max_blocks], [B], [B]
+    int32_t *free_blocks, *free_count;    // [n_blocks], [1]
+    int32_t *status;           // optional
+    int32_t *scratch;          // [3 B + 1]: what the second launch of a plan goes by
+    int32_t batch, block_size, max_blocks, n_blocks;
+    const int32_t *n_new;      // plan: [B]
+    int32_t max_tokens;
+    int32_t *cu, *positions, *slots;      // [B + 1], [max_tokens], [max_tokens]
+    const int32_t *new_lens;   // release: [B]
+};
+hipError_t launch_kv_plan(const PlanArgs &a, hipStream_t s);
+hipError_t launch_kv_release(const PlanArgs &a, hipStream_t s);
+
+struct WriteArgs {
+    char *k, *v;               // rows of the tier
+    const char *k_in, *v_in;   // rows of n_kv_heads * row_bytes, k_stride / v_stride bytes from token to token
+    int64_t k_stride, v_stride;
+    const int32_t *slots;      // [n_tokens]
+    int32_t n_tokens, n_kv_heads, row_bytes, per_block, n_slots;         // per_block: tokens of a block (or of a sequence)
+};
+hipError_t launch_kv_write(const WriteArgs &a, hipStream_t s);
+
+struct VerifyArgs {
+    const char *target, *draft;           // [B, n, V] with rows of V elements, strides in elements; draft may be null
+    int64_t target_row, target_seq, draft_row, draft_seq;
+    const int32_t *tokens, *parents;      // [B, n]; parents may be null (i - 1)
+    const float *u, *u_next;   // [B, n], [B]
+    int32_t *path, *cnt, *next;           // [B, n], [B], [B]
+    double *sums;              // [B, segments]
+    int32_t batch, n, vocab;
+};
+constexpr int kVerifySegment = 2048;      // elements of a row that one partial sum covers
+hipError_t launch_verify_drafts(int dtype, const VerifyArgs &a, hipStream_t s);
+
+// Attention of packed new tokens.  The tokens of a sequence, times the heads of a group, are rows; kChunkRows of them are a unit, of
+// which a KV head's tokens are gone through in shares of at most so many steps that all units' shares are about `target` workgroups
+// (chunk_device.hpp).
+constexpr int kChunkRows = 128;
+struct ChunkArgs {
+    ShapeDev sh;
+    const char *q;             // [T, Hq, d], q_stride bytes from token to token
+    int64_t q_stride;
+    const int32_t *cu;         // [B + 1]
+    KvDev kv;
+    int32_t n_tokens;          // T
+    int32_t causal, window;    // window: INT32_MAX for none
+    float cap;                 // 0: none
+    const float *slopes;       // [Hq] or null
+    const int32_t *prefix;     // [B] or null
+    const int32_t *first;      // [T] or null
+    int32_t o_bf16;
+    void *o;                   // [T, Hq, d]
+    float *lse;                // [T, Hq]
+    int32_t slots, parts;      // per KV head: slots of the launch; those of them that leave partials, at most
+    int32_t target;            // shares that all units together aim at, per KV head
+    int32_t *cut;              // more than 64 sequences: what chunk_cut_kernel worked out, [3 B + 4]
+    float *part_o, *part_m, *part_l;      // [parts, Hkv, kChunkRows (, d)]
+};
+hipError_t launch_chunk_attn(int dtype, int head_dim, const ChunkArgs &a, hipStream_t s);
+// the attention itself, by type (called by launch_chunk_attn)
+hipError_t launch_chunk_rows_bf16(int head_dim, const ChunkArgs &a, hipStream_t s);
+hipError_t launch_chunk_rows_f32(int head_dim, const ChunkArgs &a, hipStream_t s);
+
 }  // namespace hgca

@@ -1,0 +1,337 @@
+// Drafted tokens accepted or refused by the target's probabilities p, the draft model's q and given random numbers, and the token that
+// follows the accepted ones.
+//
+// At a node of the tree its children x are tried in order: x is accepted if u q(x) < p'(x), p' = p at first; if it is refused p'
+// becomes max(p' - q, 0), divided by its sum.  Dividing the k-th of these out, p' is max(p - c q, 0) / S(c) with S(c) its sum: c = 0
+// and S = 1 before the first refusal, c becomes c + S(c) with each.  So what a node's refusals have left of the target is one number, a
+// test is two elements of the rows, u q(x) S < max(p(x) - c q(x), 0), and only a refusal asks for a pass over the rows.  Without q (the
+// draft model was sure) q is 1 at x: p' is p without the refused tokens, S the sum over the rest.  Where the walk ends one more
+// token is drawn from p': the first at which the running sum passes u_next times the whole.
+//
+// Sums are fp64: the order of additions is then in no result that a plain running sum would not give as well but once in some 10^10 draws, and
+// the pass is bound by memory all the same.
+//
+// The first pass is the only one of most sequences, and which row and c it is of is known from single elements: every workgroup of the first
+// launch finds it for itself (walk_first), and leaves the sums of its segments.  The second launch, a workgroup per sequence, goes on from
+// there: more refusals at the same node, or further down, are passes of its own.  The draw takes one more segment.
+#include <algorithm>
+
+#include "hgca_launch.hpp"
+
+namespace hgca {
+
+namespace {
+
+constexpr int kSumBlock = 256, kSumWaves = kSumBlock / kWave;
+constexpr int kWalkBlock = 1024, kWalkWaves = kWalkBlock / kWave;
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) v += __shfl_xor(v, step);
+    return v;
+}
+
+// A probability as it counts: what is negative, infinite or NaN is 0.
+__device__ __forceinline__ float sane(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
+
+template <typename T> __device__ __forceinline__ float element(const char *row, int i);
+template <> __device__ __forceinline__ float element<float>(const char *row, int i) { return sane(reinterpret_cast<const float *>(row)[i]); }
+template <> __device__ __forceinline__ float element<bf16_t>(const char *row, int i) {
+    return sane(__uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(row)[i] << 16));
+}
+
+// What is known of every drafted token before the walk, a lane each (there are at most 64).
+struct Nodes {
+    int parent, token;                           // parent -1: not in the tree
+    float u, p, q;                               // p, q: of the token in its parent's rows
+    template <typename T> __device__ __forceinline__ void load(const VerifyArgs &a, int b) {
+        const int j = threadIdx.x % kWave;
+        parent = -1;
+        token = 0;
+        u = p = q = 0.f;
+        if (j < 1 || j >= a.n) return;
+        const int64_t at = (int64_t)b * a.n + j;
+        const int up = a.parents ? a.parents[at] : j - 1, x = a.tokens[at];
+        if (up < 0 || up >= j || x < 0 || x >= a.vocab) return;
+        parent = up;
+        token = x;
+        u = a.u[at];
+        p = element<T>(target_row(a, b, up, sizeof(T)), x);
+        q = a.draft ? element<T>(draft_row(a, b, up, sizeof(T)), x) : 1.f;
+    }
+    static __device__ __forceinline__ const char *target_row(const VerifyArgs &a, int b, int node, int e) {
+        return a.target + (b * a.target_seq + node * a.target_row) * e;
+    }
+    static __device__ __forceinline__ const char *draft_row(const VerifyArgs &a, int b, int node, int e) {
+        return a.draft + (b * a.draft_seq + node * a.draft_row) * e;
+    }
+    // children of `node` behind drafted token j, a bit each
+    __device__ __forceinline__ uint64_t children(int node, int j) const {
+        return __ballot(parent == node) & (j >= 63 ? 0ull : ~0ull << (j + 1));
+    }
+};
+
+// Where a walk stands: at `node`, the drafted tokens up to `tried` have been seen to, c and mass (S) of what is left of the target.
+struct Walk {
+    int node, tried;
+    double c, mass;
+    uint64_t path;                               // accepted tokens, a bit each
+    uint64_t gone;                               // without q: refused children of the node
+};
+
+__device__ __forceinline__ double lane_value(float x, int lane) {
+    return (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+
+// Goes on until a refusal (true: mass is to be formed anew, for c or without the tokens of `gone`) or the end of the walk (false).
+// Uniform over the wave; every wave of a workgroup does the same.
+__device__ __forceinline__ bool walk_on(Walk &w, const Nodes &nodes, bool with_q) {
+    while (true) {
+        const uint64_t next = nodes.children(w.node, w.tried);
+        if (next == 0) return false;
+        const int j = __builtin_ctzll(next);
+        double left = lane_value(nodes.p, j);
+        if (with_q) {
+            const double less = w.c * lane_value(nodes.q, j);
+            left = left > less ? left - less : 0.0;
+        } else {
+            const int x = __builtin_amdgcn_readlane(nodes.token, j);
+            if (__ballot((w.gone >> (threadIdx.x % kWave) & 1) && nodes.token == x)) left = 0.0;         // refused before
+        }
+        w.tried = j;
+        if (lane_value(nodes.u, j) * lane_value(nodes.q, j) * w.mass < left) {
+            w.node = j;
+            w.c = 0.0;
+            w.mass = 1.0;
+            w.path |= 1ull << j;
+            w.gone = 0;
+            continue;
+        }
+        w.c += w.mass;
+        w.gone |= 1ull << j;
+        return true;
+    }
+}
+
+// max(p - c q, 0) of 4 adjacent elements from i on (those behind the end: 0); the row begins at an address of any alignment.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void four(const char *row, int i, int vocab, float *x) {
+    if (ALIGNED && i + 4 <= vocab) {
+        if (sizeof(T) == 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(row + 4 * (int64_t)i);
+            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(row + 2 * (int64_t)i);
+            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
+            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = sane(x[k]);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = i + k < vocab ? element<T>(row, i + k) : 0.f;
+}
+
+// What is left of the target at a node, by element.
+template <typename T>
+struct Rest {
+    const char *p, *q;                           // q null: without
+    double c;
+    uint64_t gone;
+    int vocab;
+    bool aligned;                                // both rows begin at 4 elements' alignment
+    __device__ __forceinline__ Rest(const VerifyArgs &a, int b, const Walk &w) {
+        p = Nodes::target_row(a, b, w.node, sizeof(T));
+        q = a.draft && w.c > 0.0 ? Nodes::draft_row(a, b, w.node, sizeof(T)) : nullptr;
+        c = w.c;
+        gone = a.draft ? 0 : w.gone;
+        vocab = a.vocab;
+        aligned = ((uintptr_t)p | (uintptr_t)q) % (4 * sizeof(T)) == 0;
+    }
+    template <bool ALIGNED> __device__ __forceinline__ void load(const Nodes &nodes, int i, double *x) const {
+        float v[4], d[4];
+        four<T, ALIGNED>(p, i, vocab, v);
+        if (q) {
+            four<T, ALIGNED>(q, i, vocab, d);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = fmax(fma(-c, (double)d[k], (double)v[k]), 0.0);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = (double)v[k];
+        for (uint64_t m = gone; m; m &= m - 1) { // (uniform over the wave)
+            const int t = __builtin_amdgcn_readlane(nodes.token, __builtin_ctzll(m));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = i + k == t ? 0.0 : x[k];
+        }
+    }
+    // sum of a segment, in every lane of the wave
+    template <bool ALIGNED> __device__ __forceinline__ double segment(const Nodes &nodes, int seg) const {
+        constexpr int kRounds = kVerifySegment / (4 * kWave);
+        double s[kRounds];
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            double x[4];
+            load<ALIGNED>(nodes, seg * kVerifySegment + 4 * (r * kWave + (int)threadIdx.x % kWave), x);
+            s[r] = (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        double sum = s[0];
+#pragma unroll
+        for (int r = 1; r < kRounds; ++r) sum += s[r];
+        return wave_sum64(sum);
+    }
+};
+
+__device__ __forceinline__ int segments_of(const VerifyArgs &a) { return (a.vocab + kVerifySegment - 1) / kVerifySegment; }
+
+// The walk up to its first refusal, or to its end.
+template <typename T> __device__ __forceinline__ bool walk_first(const VerifyArgs &a, int b, Nodes &nodes, Walk &w) {
+    nodes.load<T>(a, b);
+    w = Walk{0, 0, 0.0, 1.0, 1ull, 0};
+    return walk_on(w, nodes, a.draft != nullptr);
+}
+
+// The sums of all segments of the row where the walk first stops, a wave per segment.
+template <typename T>
+__global__ __launch_bounds__(kSumBlock) void verify_sums_kernel(VerifyArgs a)
+{
+    const int b = blockIdx.y, seg = blockIdx.x * kSumWaves + threadIdx.x / kWave, segs = segments_of(a);
+    Nodes nodes;
+    Walk w;
+    walk_first<T>(a, b, nodes, w);
+    if (seg >= segs) return;
+    const Rest<T> rest(a, b, w);
+    const double sum = rest.aligned ? rest.template segment<true>(nodes, seg) : rest.template segment<false>(nodes, seg);
+    if (threadIdx.x % kWave == 0) a.sums[(int64_t)b * segs + seg] = sum;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
+{
+    __shared__ double s_sum[kWalkWaves];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, segs = segments_of(a);
+    double *const sums = a.sums + (int64_t)b * segs;
+    Nodes nodes;
+    Walk w;
+    bool refused = walk_first<T>(a, b, nodes, w);
+    // the sum over all segments' sums, in every thread, always in the same order
+    auto whole = [&] {
+        double s = 0.0;
+        for (int i = tid; i < segs; i += kWalkBlock) s += sums[i];
+        s = wave_sum64(s);
+        __syncthreads();
+        if (lane == 0) s_sum[wave] = s;
+        __syncthreads();
+        s = s_sum[0];
+#pragma unroll
+        for (int i = 1; i < kWalkWaves; ++i) s += s_sum[i];
+        return s;
+    };
+    auto pass = [&] {
+        const Rest<T> rest(a, b, w);
+        __syncthreads();                         // nobody reads the old sums any more
+        for (int seg = wave; seg < segs; seg += kWalkWaves) {
+            const double sum = rest.aligned ? rest.template segment<true>(nodes, seg) : rest.template segment<false>(nodes, seg);
+            if (lane == 0) sums[seg] = sum;
+        }
+        __syncthreads();
+        return whole();
+    };
+    double total = whole();
+    while (refused) {                            // (uniform: every wave has the same numbers)
+        w.mass = total;
+        refused = walk_on(w, nodes, a.draft != nullptr);
+        // another refusal, or the end at a node of which no sums are there
+        if (refused || w.c == 0.0) total = pass();
+        if (!refused) break;
+    }
+    if (!(total > 0.0)) {                        // nothing is left: the target itself
+        w.c = 0.0;
+        w.gone = 0;
+        total = pass();
+    }
+    // path and number of tokens
+    if (wave == 0 && lane < a.n) {
+        const int at = __popcll(w.path & ((1ull << lane) - 1)), cnt = __popcll(w.path);
+        int32_t *const out = a.path + (int64_t)b * a.n;
+        if (w.path >> lane & 1) out[at] = lane;
+        if (lane >= cnt) out[lane] = -1;
+        if (lane == 0) a.cnt[b] = cnt;
+    }
+    if (wave != 0) return;
+    // the draw, by one wave: the segment, then the element
+    int found = -1;
+    if (total > 0.0) {
+        const double t = (double)a.u_next[b] * total;
+        auto scan = [&](double v) {
+#pragma unroll
+            for (int step = 1; step < kWave; step *= 2) {
+                const double o = __shfl_up(v, step);
+                if (lane >= step) v += o;
+            }
+            return v;
+        };
+        double run = 0.0, before = 0.0;          // sum of what comes before the segment
+        int seg = -1;
+        for (int s0 = 0; s0 < segs; s0 += kWave) {
+            const double mine = s0 + lane < segs ? sums[s0 + lane] : 0.0, upto = run + scan(mine);
+            // the last segment that holds anything is the fallback where rounding leaves none
+            const uint64_t over = __ballot(upto > t && mine > 0.0), some = __ballot(mine > 0.0);
+            if (over) {
+                const int l = __builtin_ctzll(over);
+                seg = s0 + l;
+                before = __shfl(upto - mine, l);
+                break;
+            }
+            if (some) {
+                const int l = 63 - __builtin_clzll(some);
+                seg = s0 + l;
+                before = __shfl(upto - mine, l);
+            }
+            run = __shfl(upto, kWave - 1);
+        }
+        const Rest<T> rest(a, b, w);
+        for (int r = 0; r < kVerifySegment / (4 * kWave); ++r) {
+            const int i = seg * kVerifySegment + 4 * (r * kWave + lane);
+            double x[4];
+            if (rest.aligned) rest.template load<true>(nodes, i, x); else rest.template load<false>(nodes, i, x);
+            const double mine = (x[0] + x[1]) + (x[2] + x[3]), upto = scan(mine);
+            double at = before + (upto - mine);
+            int hit = -1, last = -1;             // the first over the threshold, the last that holds anything
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                at += x[k];
+                if (x[k] > 0.0) {
+                    if (hit < 0 && at > t) hit = i + k;
+                    last = i + k;
+                }
+            }
+            const uint64_t over = __ballot(hit >= 0), some = __ballot(last >= 0);
+            if (over) {
+                found = __shfl(hit, __builtin_ctzll(over));
+                break;
+            }
+            if (some) found = __shfl(last, 63 - __builtin_clzll(some));
+            before += __shfl(upto, kWave - 1);
+        }
+    }
+    if (lane == 0) a.next[b] = found;
+}
+
+}  // namespace
+
+hipError_t launch_verify_drafts(int dtype, const VerifyArgs &a, hipStream_t s)
+{
+    const int segs = (a.vocab + kVerifySegment - 1) / kVerifySegment;
+    const dim3 grid((segs + kSumWaves - 1) / kSumWaves, a.batch);
+    if (dtype == 0) hipLaunchKernelGGL(verify_sums_kernel<float>, grid, dim3(kSumBlock), 0, s, a);
+    else hipLaunchKernelGGL(verify_sums_kernel<bf16_t>, grid, dim3(kSumBlock), 0, s, a);
+    hipError_t rc = hipGetLastError();
+    if (rc != hipSuccess) return rc;
+    if (dtype == 0) hipLaunchKernelGGL(verify_walk_kernel<float>, dim3(a.batch), dim3(kWalkBlock), 0, s, a);
+    else hipLaunchKernelGGL(verify_walk_kernel<bf16_t>, dim3(a.batch), dim3(kWalkBlock), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace hgca

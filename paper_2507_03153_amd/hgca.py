@@ -30,9 +30,11 @@ EXPORTS = ("hgca_status_string", "hgca_workspace_bytes", "hgca_dense_window_attn
            "hgca_managed_decode_step", "hgca_dense_window_attn_static", "hgca_hybrid_decode_step_selected", "hgca_kv_append_tokens",
            "hgca_managed_append_workspace_bytes", "hgca_managed_append_step",
            "hgca_qk_norm_rope", "hgca_tree_workspace_bytes", "hgca_tree_attn", "hgca_kv_commit", "hgca_kv8_write_tokens",
-           "hgca_kv8_write_tier", "hgca_kv8_read", "hgca_kv8_workspace_bytes", "hgca_kv8_attn")
+           "hgca_kv8_write_tier", "hgca_kv8_read", "hgca_kv8_workspace_bytes", "hgca_kv8_attn",
+           "hgca_kv_plan", "hgca_kv_release", "hgca_kv_write", "hgca_chunk_workspace_bytes", "hgca_chunk_attn",
+           "hgca_verify_workspace_bytes", "hgca_verify_drafts")
 STATIC_SCRATCH_BYTES = 16 << 20                  # HGCA_STATIC_SCRATCH_BYTES of include/hgca.h
-CACHE_WINDOW_FULL, CACHE_CONTEXT_FULL, CACHE_LIST_FULL = 1, 2, 4
+CACHE_WINDOW_FULL, CACHE_CONTEXT_FULL, CACHE_LIST_FULL, CACHE_BLOCKS_OUT, CACHE_TOKENS_FULL = 1, 2, 4, 8, 16
 
 
 class Shape(ctypes.Structure):
@@ -57,6 +59,11 @@ class CacheState(ctypes.Structure):
                                                "status")] + \
                [(n, ctypes.c_int32) for n in ("block_size", "max_blocks", "win_blocks", "k_max", "pool_cap",
                                                "win_cap_blocks")]
+
+
+class BlockStateView(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("block_table", "held", "lens", "free_blocks", "free_count", "status", "scratch")] + \
+               [(n, ctypes.c_int32) for n in ("batch", "block_size", "max_blocks", "n_blocks")]
 
 
 class HgcaError(RuntimeError):
@@ -163,6 +170,21 @@ def lib() -> ctypes.CDLL:
         L.hgca_kv8_workspace_bytes.argtypes = [ps, i32, i32]
         L.hgca_kv8_attn.restype = ctypes.c_int
         L.hgca_kv8_attn.argtypes = [ps, vp, i32, p8, vp, i32, vp, vp, sz, vp]
+        pb, f32 = ctypes.POINTER(BlockStateView), ctypes.c_float
+        L.hgca_kv_plan.restype = ctypes.c_int
+        L.hgca_kv_plan.argtypes = [pb, vp, i32, vp, vp, vp, vp]
+        L.hgca_kv_release.restype = ctypes.c_int
+        L.hgca_kv_release.argtypes = [pb, vp, vp]
+        L.hgca_kv_write.restype = ctypes.c_int
+        L.hgca_kv_write.argtypes = [ps, pk, i64, vp, vp, i64, vp, i64, i32, vp]
+        L.hgca_chunk_workspace_bytes.restype = sz
+        L.hgca_chunk_workspace_bytes.argtypes = [ps, i32, i32]
+        L.hgca_chunk_attn.restype = ctypes.c_int
+        L.hgca_chunk_attn.argtypes = [ps, vp, i64, vp, i32, pk, i32, i32, f32, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+        L.hgca_verify_workspace_bytes.restype = sz
+        L.hgca_verify_workspace_bytes.argtypes = [i32, i32]
+        L.hgca_verify_drafts.restype = ctypes.c_int
+        L.hgca_verify_drafts.argtypes = [i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -812,3 +834,166 @@ def kv8_workspace(shape: Shape, n_q: int, max_tokens: int, device) -> torch.Tens
 def kv8_attn(shape: Shape, q, tier: Kv8Tier, o_out, lse_out, ws, stream=None) -> None:
     """Attention of q [B,n,Hq,d] over every valid token of an 8-bit tier; o_out [B,n,Hq,d] fp32 or bf16, lse_out fp32."""
     _rows_call("hgca_kv8_attn", shape, q, tier, torch.uint8, None, o_out, lse_out, ws, stream)
+
+
+# ---- a server's step: requests of different size, packed one behind the other ----
+
+CHUNK_CAUSAL = 1
+
+
+@dataclass
+class BlockState:
+    """Blocks of a paged tier dealt out on the GPU (all int32): row b of block_table [B,max_blocks] has held[b] entries in use, which
+    hold lens[b] tokens; free_blocks[0 .. free_count[0]) is the stack of free blocks.  status [1] collects CACHE_* bits."""
+    block_table: torch.Tensor
+    held: torch.Tensor
+    lens: torch.Tensor
+    free_blocks: torch.Tensor
+    free_count: torch.Tensor
+    block_size: int
+    status: Optional[torch.Tensor] = None
+    scratch: Optional[torch.Tensor] = None       # [3 B + 1], made here if not given
+
+    def __post_init__(self):
+        if self.scratch is None:
+            self.scratch = torch.empty(3 * int(self.held.numel()) + 1, dtype=torch.int32, device=self.held.device)
+
+    def view(self, dev: int) -> BlockStateView:
+        B, i32 = self.held.numel(), torch.int32
+        _need("state.held", self.held, i32, (B,), dev)
+        mb = int(self.block_table.shape[1])
+        _need("state.block_table", self.block_table, i32, (B, mb), dev)
+        _need("state.lens", self.lens, i32, (B,), dev)
+        _need("state.free_blocks", self.free_blocks, i32, (self.free_blocks.numel(),), dev)
+        _need("state.free_count", self.free_count, i32, (1,), dev)
+        _need("state.scratch", self.scratch, i32, (3 * B + 1,), dev)
+        if self.status is not None:
+            _need("state.status", self.status, i32, (1,), dev)
+        return BlockStateView(self.block_table.data_ptr(), self.held.data_ptr(), self.lens.data_ptr(), self.free_blocks.data_ptr(),
+                              self.free_count.data_ptr(), _ptr(self.status), self.scratch.data_ptr(), B, int(self.block_size), mb,
+                              self.free_blocks.numel())
+
+
+def kv_plan(state: BlockState, n_new, cu_out, positions_out, slots_out, stream=None) -> None:
+    """n_new int32 [B] more tokens per sequence: blocks granted, lengths grown, and the tokens laid out one sequence behind the other:
+    cu_out int32 [B+1], positions_out and slots_out int32 [max_tokens] (0 and -1 behind the last one)."""
+    dev = _gpu_of(n_new)
+    view = state.view(dev)
+    B, T = view.batch, positions_out.numel()
+    _need("n_new", n_new, torch.int32, (B,), dev)
+    _need("cu_out", cu_out, torch.int32, (B + 1,), dev)
+    _need("positions_out", positions_out, torch.int32, (T,), dev)
+    _need("slots_out", slots_out, torch.int32, (T,), dev)
+    _launch("hgca_kv_plan", stream, dev, ctypes.byref(view), n_new.data_ptr(), T, cu_out.data_ptr(), positions_out.data_ptr(),
+            slots_out.data_ptr())
+
+
+def kv_release(state: BlockState, new_lens, stream=None) -> None:
+    """Sequences are cut down to new_lens int32 [B] tokens (may be state.lens); blocks behind go back on the stack."""
+    dev = _gpu_of(new_lens)
+    view = state.view(dev)
+    _need("new_lens", new_lens, torch.int32, (view.batch,), dev)
+    _launch("hgca_kv_release", stream, dev, ctypes.byref(view), new_lens.data_ptr())
+
+
+def _packed_stride(name: str, t: torch.Tensor) -> int:
+    """Elements between consecutive tokens of [T,H,d], whose heads lie side by side."""
+    (T, H, d), (s0, s1, s2) = t.shape, t.stride()
+    step = s0 if T > 1 else H * d
+    if s2 != 1 or (s1 != d and H > 1) or step < H * d:
+        raise ValueError(f"{name}: heads have to lie side by side and tokens one behind the other")
+    return step
+
+
+def _packed(name: str, t: torch.Tensor, dtype, size: tuple, dev: int) -> int:
+    if t.dtype is not dtype or t.shape != size or t.get_device() != dev:
+        _refuse(name, t, dtype, size, dev)
+    return _packed_stride(name, t)
+
+
+def kv_write(shape: Shape, tier: Tier, slots, k_in, v_in, stream=None) -> None:
+    """Rows k_in / v_in [T,Hkv,d] (may be parts of wider rows) go to slots int32 [T] of the tier: block * block_size + offset, or b *
+    cap + position in a contiguous one; tokens whose slot is outside are left out."""
+    B, _, Hkv, d, dt = _heads(shape)
+    dev, T = _gpu_of(slots), slots.numel()
+    _need("slots", slots, torch.int32, (T,), dev)
+    ks, vs = _packed("k_in", k_in, dt, (T, Hkv, d), dev), _packed("v_in", v_in, dt, (T, Hkv, d), dev)
+    kv = _tier_view(tier, B, Hkv, d, dt, dev)
+    _launch("hgca_kv_write", stream, dev, ctypes.byref(shape), ctypes.byref(kv), tier.k.shape[0] * tier.k.shape[2], slots.data_ptr(),
+            k_in.data_ptr(), ks, v_in.data_ptr(), vs, T)
+
+
+def chunk_workspace(shape: Shape, n_tokens: int, max_tokens: int, device) -> torch.Tensor:
+    n = int(lib().hgca_chunk_workspace_bytes(ctypes.byref(shape), int(n_tokens), int(max_tokens)))
+    if n == 0:
+        raise HgcaError(ERR_INVALID_ARG, "hgca_chunk_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def chunk_attn(shape: Shape, q, cu, tier: Tier, o_out, lse_out, ws, causal: bool = True, window: int = 0, cap: float = 0.0, slopes=None,
+               prefix_lens=None, first=None, stream=None) -> None:
+    """Attention of packed new tokens q [T,Hq,d] (may be parts of wider rows), sequence b's in rows cu[b] .. cu[b+1] - 1 (int32 [B+1]),
+    which are the last tokens of the tier.  A row sees tokens below prefix_lens[b] (int32 [B]) and those from first[t] (int32 [T]) on that
+    are no later than itself (causal) and less than `window` tokens back (0: any); scores are capped to cap * tanh(s / cap) (0: not) and
+    lose slopes[h] (fp32 [Hq]) per token of distance.  o_out [T,Hq,d] fp32 or bf16, lse_out [T,Hq] fp32."""
+    B, Hq, Hkv, d, dt = _heads(shape)
+    dev, T = _gpu_of(q), q.shape[0]
+    qs = _packed("q", q, dt, (T, Hq, d), dev)
+    _need("cu", cu, torch.int32, (B + 1,), dev)
+    _need("o_out", o_out, torch.bfloat16 if o_out.dtype is torch.bfloat16 else torch.float32, (T, Hq, d), dev)
+    _need("lse_out", lse_out, torch.float32, (T, Hq), dev)
+    _need("ws", ws, torch.uint8, (ws.numel(),), dev)
+    if slopes is not None:
+        _need("slopes", slopes, torch.float32, (Hq,), dev)
+    if prefix_lens is not None:
+        _need("prefix_lens", prefix_lens, torch.int32, (B,), dev)
+    if first is not None:
+        _need("first", first, torch.int32, (T,), dev)
+    kv = _tier_view(tier, B, Hkv, d, dt, dev)
+    _launch("hgca_chunk_attn", stream, dev, ctypes.byref(shape), q.data_ptr(), qs, cu.data_ptr(), T, ctypes.byref(kv),
+            CHUNK_CAUSAL if causal else 0, int(window), cap, _ptr(slopes), _ptr(prefix_lens), _ptr(first), o_out.data_ptr(),
+            _dtype_code(o_out), lse_out.data_ptr(), ws.data_ptr(), ws.numel())
+
+
+def verify_workspace(batch: int, vocab: int, device) -> torch.Tensor:
+    n = int(lib().hgca_verify_workspace_bytes(int(batch), int(vocab)))
+    if n == 0:
+        raise HgcaError(ERR_INVALID_ARG, "hgca_verify_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _prob_strides(name: str, t: torch.Tensor, dtype, size: tuple, dev: int):
+    if t.dtype is not dtype or t.shape != size or t.get_device() != dev:
+        _refuse(name, t, dtype, size, dev)
+    B, n, V = size
+    s0, s1, s2 = t.stride()
+    row = s1 if n > 1 else V
+    seq = s0 if B > 1 else n * row
+    # (0 is the library's word for rows one behind the other, not for an expanded tensor's)
+    if (s2 != 1 and V > 1) or row < V or (seq == 0 and B > 1):
+        raise ValueError(f"{name}: a row's elements have to lie side by side, rows apart from each other")
+    return row, seq
+
+
+def verify_drafts(target, draft, tokens, u, u_next, path_out, cnt_out, next_out, ws, parents=None, stream=None) -> None:
+    """Which drafted tokens stay and which one follows them.  target and draft [B,n,V] fp32 or bf16: the two models' distributions after
+    each drafted token (draft None: tokens chosen without chance); tokens int32 [B,n], parents int32 [B,n] (None: a chain); u [B,n] and
+    u_next [B] fp32 random numbers in [0, 1).  path_out int32 [B,n] and cnt_out int32 [B] are kv_commit's path and cnt, next_out int32
+    [B] the token drawn behind them."""
+    dev = _gpu_of(target)
+    B, n, V = target.shape
+    dt = torch.bfloat16 if target.dtype is torch.bfloat16 else torch.float32
+    tr, ts = _prob_strides("target", target, dt, (B, n, V), dev)
+    dr, ds = (0, 0) if draft is None else _prob_strides("draft", draft, dt, (B, n, V), dev)
+    _need("tokens", tokens, torch.int32, (B, n), dev)
+    if parents is not None:
+        _need("parents", parents, torch.int32, (B, n), dev)
+    _need("u", u, torch.float32, (B, n), dev)
+    _need("u_next", u_next, torch.float32, (B,), dev)
+    _need("path_out", path_out, torch.int32, (B, n), dev)
+    _need("cnt_out", cnt_out, torch.int32, (B,), dev)
+    _need("next_out", next_out, torch.int32, (B,), dev)
+    _need("ws", ws, torch.uint8, (ws.numel(),), dev)
+    _launch("hgca_verify_drafts", stream, dev, B, n, V, BF16 if dt is torch.bfloat16 else F32, target.data_ptr(), tr, ts, _ptr(draft), dr,
+            ds, tokens.data_ptr(), _ptr(parents), u.data_ptr(), u_next.data_ptr(), path_out.data_ptr(), cnt_out.data_ptr(),
+            next_out.data_ptr(), ws.data_ptr(), ws.numel())
