@@ -12,6 +12,9 @@ constexpr int kChunkStep = kStepTokens;          // tokens of a step
 constexpr int kChunkWaves = kTreeWaves, kChunkBlock = kTreeBlock;
 static_assert(kChunkRows == 32 * kChunkWaves, "32 rows per wave");
 
+// true where a lane has it, uniform over the wave
+__device__ __forceinline__ bool any_lane(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
+
 // ---- the cut ----
 // A sequence of n tokens has u = ceil(n * group / kChunkRows) units, each over at most `steps` steps of its tokens.  Units are cut into shares
 // of at most C steps, C = the steps of all units over the number of shares aimed at (and kChunkLeast at least): s = ceil(steps / C)
@@ -32,6 +35,10 @@ struct SeqWork {
         int64_t tokens = len;                    // that a unit's rows may see
         if (a.causal) tokens = min(tokens, (int64_t)a.window + kChunkRows / a.sh.group + pre + 3 * kChunkStep);
         steps = max((int)((tokens + kChunkStep - 1) / kChunkStep), 1);
+    }
+    // all lanes have the same: the compiler is told so, and keeps them, and what follows from them, in scalar registers
+    __device__ __forceinline__ void unify() {
+        for (int *x : {&n0, &nq, &len, &pre, &units, &steps}) *x = __builtin_amdgcn_readfirstlane(*x);
     }
 };
 
@@ -96,6 +103,11 @@ struct Place {
             n_shares = shares_of(q, a.cut[0]);
             part = parts[b];
         }
+        b = __builtin_amdgcn_readfirstlane(b);
+        inside = __builtin_amdgcn_readfirstlane(inside);
+        units = __builtin_amdgcn_readfirstlane(units);
+        n_shares = __builtin_amdgcn_readfirstlane(n_shares);
+        part = __builtin_amdgcn_readfirstlane(part);
         // the units of a share run side by side (they read the same tokens), those that see most first
         share = FOLD ? 0 : inside / units;
         unit = FOLD ? inside : units - 1 - inside % units;
@@ -153,7 +165,7 @@ struct WaveSees {
 
 // The steps of a share: those of the prefix and those from the first token that a row of the unit sees to the last.
 struct Steps {
-    int begin[2], end[2];
+    int begin0, end0, begin1, end1;
     __device__ __forceinline__ Steps(int pre, int lo, int hi, int share, int n_shares) {
         int head = (pre + kChunkStep - 1) / kChunkStep, from = 0, to = 0;
         if (hi > lo) {
@@ -166,11 +178,13 @@ struct Steps {
         }
         const int total = head + (to - from), per = (total + n_shares - 1) / n_shares;
         const int i0 = min(share * per, total), i1 = min(i0 + per, total);
-        begin[0] = min(i0, head);
-        end[0] = min(i1, head);
-        begin[1] = from + max(i0 - head, 0);
-        end[1] = from + max(i1 - head, 0);
+        begin0 = min(i0, head);
+        end0 = min(i1, head);
+        begin1 = from + max(i0 - head, 0);
+        end1 = from + max(i1 - head, 0);
     }
+    __device__ __forceinline__ int begin(int range) const { return range ? begin1 : begin0; }
+    __device__ __forceinline__ int end(int range) const { return range ? end1 : end0; }
 };
 
 // ---- scores ----
@@ -221,7 +235,7 @@ template <int MODE, bool FINE> struct ScoreMap {
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(c[t][r]));
-        const bool near = !__any(!(most * kx <= kTanhNear));
+        const bool near = !any_lane(!(most * kx <= kTanhNear));
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -284,7 +298,7 @@ __device__ void settle_odd(const ChunkArgs &a, int b, int kvh, const RowSees &se
 #pragma unroll
         for (int r = 0; r < 16; ++r) z[r % 4] = fmaf(acc[dt][r], 0.f, z[r % 4]);
     const float all = (z[0] + z[1]) + (z[2] + z[3]);
-    met = __any(all != all) || met;
+    met = any_lane(all != all) || met;
     if (lane == 0) s_odd[w] = met;
     __syncthreads();
     bool any = false;
@@ -293,7 +307,7 @@ __device__ void settle_odd(const ChunkArgs &a, int b, int kvh, const RowSees &se
     if (!any) return;                            // uniform over the workgroup
     uint64_t kinds[3] = {0, 0, 0};               // a bit per element of acc
     for (int part = 0; part < 2; ++part)
-        for (int s = steps.begin[part]; s < steps.end[part]; ++s) {
+        for (int s = steps.begin(part); s < steps.end(part); ++s) {
             const int first = s * kChunkStep;
             notes.template note<T>(a, b, kvh, first, len);
             const uint64_t seen = sees.mask(first);
@@ -350,8 +364,8 @@ __device__ __forceinline__ void unit_range(const WaveSees &w, int (&s_range)[2],
         atomicMax(&s_range[1], w.any_hi);
     }
     __syncthreads();
-    lo = s_range[0];
-    hi = s_range[1];
+    lo = __builtin_amdgcn_readfirstlane(s_range[0]);
+    hi = __builtin_amdgcn_readfirstlane(s_range[1]);
 }
 
 // A row's result, or its share's partial: l over all tokens of the share, sums relative to 2^-shift.
@@ -360,30 +374,40 @@ __device__ __forceinline__ void store_row(const ChunkArgs &a, const Place &at, i
                                           const floatx16 (&acc)[D / 32]) {
     if (!rp.live) return;
     const int hw = threadIdx.x % kWave / 32;
-    const bool whole = at.n_shares == 1;
-    const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-    const int64_t to = whole ? rp.out : ((int64_t)(at.part + at.share) * a.sh.n_kv_heads + kvh) * kChunkRows + rp.row;
+    auto each = [&](auto store) {                // four adjacent columns at a time
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
+        for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-            const int64_t e = to * D + 32 * dt + 8 * q4 + 4 * hw;
-            float x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = whole && l == 0.f ? 0.f : acc[dt][4 * q4 + i] * inv;
-            if (whole && a.o_bf16)
-                *reinterpret_cast<uint2 *>(static_cast<char *>(a.o) + 2 * e) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-            else
-                *reinterpret_cast<float4 *>((whole ? static_cast<float *>(a.o) : a.part_o) + e) = make_float4(x[0], x[1], x[2], x[3]);
-        }
-    if (hw == 0) {
-        if (whole) {
-            a.lse[to] = l == 0.f ? -INFINITY : (__builtin_amdgcn_logf(l) - shift) * kLn2;
-        } else {
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const floatx16 &x = acc[dt];
+                store(32 * dt + 8 * q4 + 4 * hw, make_float4(x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]));
+            }
+    };
+    if (at.n_shares > 1) {                       // uniform over the workgroup
+        const int64_t to = ((int64_t)(at.part + at.share) * a.sh.n_kv_heads + kvh) * kChunkRows + rp.row;
+        float *const o = a.part_o + to * D;
+        each([&](int col, const float4 &x) { *reinterpret_cast<float4 *>(o + col) = x; });
+        if (hw == 0) {
             a.part_m[to] = l == 0.f ? -INFINITY : -shift;
             a.part_l[to] = l;
         }
+        return;
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    auto result = [&](const float4 &x) {         // (sums of a row that sees nothing are 0)
+        return make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    };
+    if (a.o_bf16) {
+        char *const o = static_cast<char *>(a.o) + 2 * rp.out * D;
+        each([&](int col, const float4 &x) {
+            const float4 y = result(x);
+            *reinterpret_cast<uint2 *>(o + 2 * col) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+        });
+    } else {
+        float *const o = static_cast<float *>(a.o) + rp.out * D;
+        each([&](int col, const float4 &x) { *reinterpret_cast<float4 *>(o + col) = result(x); });
+    }
+    if (hw == 0) a.lse[rp.out] = l == 0.f ? -INFINITY : (__builtin_amdgcn_logf(l) - shift) * kLn2;
 }
 
 // The running maximum, sum and rescaling of a row over a step's scores (as left by ScoreMap): returns the shift of a weight 2^(k2 c + shift).
@@ -396,11 +420,11 @@ template <int DT> struct Running {
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, c[t][r]);
-        if (__any(mx > m)) {                     // uniform over the wave
+        if (any_lane(mx > m)) {                     // uniform over the wave
             const float m_new = fmaxf(m, halves_max(mx)), to = shift_of(m_new, k2), corr = rescale_factor(m, m_new, k2);
             m = m_new;
             shift = is_far(to) ? 0.f : to;
-            far = __any(is_far(to));
+            far = any_lane(is_far(to));
             l *= corr;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) acc[dt] *= corr;

@@ -7,7 +7,6 @@
 //
 // What bounds it: the matrix cores, 64 cycles of a SIMD for 32 x 32 x 2.
 #include <algorithm>
-#include <type_traits>
 
 #include "chunk_device.hpp"
 
@@ -54,10 +53,8 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
 {
     using S = StageF32<D>;
     constexpr int KP = D / 8, DT = D / 32;       // pairs of pieces of a row, column tiles
-    __shared__ __attribute__((aligned(1024))) char s_k0[S::kBytes];
-    __shared__ __attribute__((aligned(1024))) char s_k1[S::kBytes];
-    __shared__ __attribute__((aligned(1024))) char s_v0[S::kBytes];
-    __shared__ __attribute__((aligned(1024))) char s_v1[S::kBytes];
+    constexpr int kV = 2 * S::kBytes;            // the stages: K of even and odd half steps, V of even and odd ones
+    __shared__ __attribute__((aligned(4 * S::kBytes))) char s_kv[4 * S::kBytes];
     __shared__ uint32_t s_row[kSub];
     __shared__ int s_odd[kChunkWaves], s_range[2];
 
@@ -65,10 +62,11 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
     Place at;
     at.find<false>(a, blockIdx.x / a.sh.n_kv_heads);
     if (at.idle) return;                         // uniform over the workgroup
-    const SeqWork seq(a, at.b);
+    SeqWork seq(a, at.b);
+    seq.unify();
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
     const RowPlace rp(a, seq, at.unit, kvh, 32 * w + n);
-    const bool wave_live = __any(rp.live);       // uniform over the wave
+    const bool wave_live = any_lane(rp.live);       // uniform over the wave
     float4 qop[KP];
     {
         const char *const q = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * S::kRowBytes;
@@ -92,19 +90,18 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = floatx16{};
 
-    auto body = [&](auto masked, const char *k_stage, const char *v_stage, int tok) {
-        constexpr bool MASKED = decltype(masked)::value;
+    auto body = [&](const char *stage, int tok) {
         floatx16 c[1] = {floatx16{}};
 #pragma unroll
         for (int j = 0; j < KP; ++j) {
-            const float4 k = *reinterpret_cast<const float4 *>(k_stage + S::offset(n, 2 * j + hw));
+            const float4 k = *reinterpret_cast<const float4 *>(stage + S::offset(n, 2 * j + hw));
             c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, qop[j].x, c[0], 0, 0, 0);
             c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, qop[j].y, c[0], 0, 0, 0);
             c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, qop[j].z, c[0], 0, 0, 0);
             c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, qop[j].w, c[0], 0, 0, 0);
         }
         map.apply(c, pos, tok + 4 * hw);
-        if constexpr (MASKED) {
+        if (!wave.all(tok, kHalfStep)) {         // uniform over the wave
             const uint64_t seen = sees.mask(tok + 4 * hw);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
@@ -118,53 +115,47 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
             const float p = __builtin_amdgcn_exp2f(fmaf(c[0][r], map.k2, run.shift));            // masked scores give 0
             sum[r % 4] += p;
             // piece 8 dt + n / 4 of row 8 (r / 4) + 4 hw + r % 4 lies at their exclusive or
-            const char *const v = v_stage + 8 * (r / 4) * S::kRowBytes + v_lane[r % 4];
+            const char *const v = stage + kV + 8 * (r / 4) * S::kRowBytes + v_lane[r % 4];
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
+            for (int dt = 0; dt < DT; ++dt) {    // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
                 float x = *reinterpret_cast<const float *>(v + 128 * (dt ^ (r / 4) % (S::kPieces / 8)));
-                if constexpr (MASKED) {          // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
-                    const bool bad = !(fabsf(x) < INFINITY);
-                    odd = odd || bad;
-                    x = bad ? 0.f : x;
-                }
+                const bool bad = !(fabsf(x) < INFINITY);
+                odd = odd || bad;
+                x = bad ? 0.f : x;
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p, acc[dt], 0, 0, 0);
             }
         }
-        if constexpr (MASKED) met_odd = met_odd || __any(odd);
+        met_odd = met_odd || any_lane(odd);
         run.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
 
 #pragma unroll 1
     for (int range = 0; range < 2; ++range) {
-        const int from = steps.begin[range] * kChunkStep, total = min(steps.end[range] * kChunkStep, seq.len) - from;
+        const int from = steps.begin(range) * kChunkStep, total = min(steps.end(range) * kChunkStep, seq.len) - from;
         const int sub_len = pass_length(a.kv, total);
 #pragma unroll 1
         for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
             const int nsub = min(sub_len, total - sub0), first = from + sub0, count = (nsub + kHalfStep - 1) / kHalfStep;
             __syncthreads();                     // the previous table and stages are no longer in use
             const BlockRows where = make_block_rows<kChunkBlock>(s_row, a.kv, a.sh.n_kv_heads, at.b, kvh, first, nsub);
-            load_half_step<D>(a.kv, where, 0, nsub, s_k0, s_v0);
+            load_half_step<D>(a.kv, where, 0, nsub, s_kv, s_kv + kV);
             // Half step s reads the stages of its parity, and the rows of s + 1 go to those of the other parity, which were last read in
             // s - 1: the barrier at its top orders both.
-            auto step = [&](int s, const char *k_cur, const char *v_cur, char *k_next, char *v_next) {
+#pragma unroll 1
+            for (int s = 0; s < count; ++s) {
                 wait_for_own_loads();            // the barrier alone does not wait for LDS-direct loads
                 __syncthreads();
-                if (s + 1 < count) load_half_step<D>(a.kv, where, s + 1, nsub, k_next, v_next);
+                char *const next = s_kv + (s + 1) % 2 * S::kBytes;
+                if (s + 1 < count) load_half_step<D>(a.kv, where, s + 1, nsub, next, next + kV);
                 const int tok = first + s * kHalfStep;
-                if (!wave_live || wave.none(tok, kHalfStep)) return;
-                if (wave.all(tok, kHalfStep)) body(std::false_type{}, k_cur, v_cur, tok);
-                else body(std::true_type{}, k_cur, v_cur, tok);
-            };
-            for (int s = 0; s < count; s += 2) {
-                step(s, s_k0, s_v0, s_k1, s_v1);
-                if (s + 1 < count) step(s + 1, s_k1, s_v1, s_k0, s_v0);
+                if (wave_live && !wave.none(tok, kHalfStep)) body(s_kv + s % 2 * S::kBytes, tok);
             }
         }
     }
 
     __syncthreads();                             // all waves have read the stages
-    OddTokens<D> &notes = *reinterpret_cast<OddTokens<D> *>(s_v1);
-    static_assert(sizeof(OddTokens<D>) <= sizeof(s_v1), "the notes lie in a stage");
+    OddTokens<D> &notes = *reinterpret_cast<OddTokens<D> *>(s_kv);
+    static_assert(sizeof(OddTokens<D>) <= sizeof(s_kv), "the notes lie in a stage");
     settle_odd<float, D>(a, at.b, kvh, sees, steps, seq.len, met_odd, s_odd, notes, acc);
     store_row<D>(a, at, kvh, rp, halves_sum(run.l), shift_of(run.m, map.k2), acc);
 }

@@ -10,7 +10,6 @@
 // out of the first product are the operand of the second.
 // A wave tells by its rows' ranges which steps all of them see (no mask), and which none (left out).
 #include <algorithm>
-#include <type_traits>
 
 #include "chunk_device.hpp"
 
@@ -23,10 +22,8 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 {
     using S = DmaStage<D, kChunkWaves>;
     constexpr int KK = D / 16, DT = D / 32, NT = kChunkStep / 32;
-    __shared__ __attribute__((aligned(1024))) char s_k0[S::kBytes];
-    __shared__ __attribute__((aligned(1024))) char s_k1[S::kBytes];
-    __shared__ __attribute__((aligned(1024))) char s_v0[S::kBytes];
-    __shared__ __attribute__((aligned(1024))) char s_v1[S::kBytes];
+    constexpr int kV = 2 * S::kBytes;            // the stages: K of even and odd steps, V of even and odd steps
+    __shared__ __attribute__((aligned(4 * S::kBytes))) char s_kv[4 * S::kBytes];
     __shared__ uint32_t s_row[kSub];
     __shared__ int s_odd[kChunkWaves], s_range[2];
 
@@ -34,10 +31,11 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
     Place at;
     at.find<false>(a, blockIdx.x / a.sh.n_kv_heads);
     if (at.idle) return;                         // uniform over the workgroup
-    const SeqWork seq(a, at.b);
+    SeqWork seq(a, at.b);
+    seq.unify();
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
     const RowPlace rp(a, seq, at.unit, kvh, 32 * w + n);
-    const bool wave_live = __any(rp.live);       // uniform over the wave
+    const bool wave_live = any_lane(rp.live);       // uniform over the wave
     uint4 qop[KK];
     {
         const char *const q = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * S::kRowBytes;
@@ -64,15 +62,15 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 
     // One step.  c[t][r] is the score of step token 32 t + 8 (r / 4) + 4 hw + r % 4; group g of the second product is 16 tokens, of
     // which the lane holds eight.
-    auto body = [&](auto masked, const char *k_stage, const char *v_stage, int tok) {
-        constexpr bool MASKED = decltype(masked)::value;
+    auto body = [&](const char *stage, int tok) {
+        const bool masked = !wave.all(tok, kChunkStep);          // uniform over the wave
         floatx16 c[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) c[t] = floatx16{};
         uint4 kf[KK][NT];
         auto read_slice = [&](int kk) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) kf[kk][t] = *reinterpret_cast<const uint4 *>(k_stage + t * 32 * S::kRowBytes + k_lane[kk]);
+            for (int t = 0; t < NT; ++t) kf[kk][t] = *reinterpret_cast<const uint4 *>(stage + t * 32 * S::kRowBytes + k_lane[kk]);
         };
         read_slice(0);
         read_slice(1);
@@ -86,7 +84,7 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
         }
         uint4 vop[2][DT];
         auto read_v = [&](int g, uint4 (&x)[DT]) {
-            const char *v = v_stage + S::v_offset(16 * g, 0) + v_lane;
+            const char *v = stage + kV + S::v_offset(16 * g, 0) + v_lane;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const short4v x0 = lds_read_tr16(v + 256 * dt), x1 = lds_read_tr16(v + S::v_offset(8, 0) + 256 * dt);
@@ -97,7 +95,7 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
         read_v(0, vop[0]);
         __builtin_amdgcn_sched_barrier(0);
         map.apply(c, pos, tok + 4 * hw);
-        if constexpr (MASKED) {
+        if (masked) {
             const uint64_t seen = sees.mask(tok + 4 * hw);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -133,11 +131,11 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
             __builtin_amdgcn_sched_barrier(0);
             uint4(&v)[DT] = vop[g % 2];
             if (g + 1 < 2 * NT) read_v(g + 1, vop[(g + 1) % 2]);
-            if constexpr (MASKED) {              // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
+            if (masked) {                        // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
                 uint32_t odd = 0;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) odd |= odd_carry(v[dt].x) | odd_carry(v[dt].y) | odd_carry(v[dt].z) | odd_carry(v[dt].w);
-                if (__any((odd & kSigns) != 0)) {
+                if (any_lane((odd & kSigns) != 0)) {
                     met_odd = true;
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
@@ -163,35 +161,31 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 
 #pragma unroll 1
     for (int range = 0; range < 2; ++range) {
-        const int from = steps.begin[range] * kChunkStep, total = min(steps.end[range] * kChunkStep, seq.len) - from;
+        const int from = steps.begin(range) * kChunkStep, total = min(steps.end(range) * kChunkStep, seq.len) - from;
         const int sub_len = pass_length(a.kv, total);
 #pragma unroll 1
         for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
             const int nsub = min(sub_len, total - sub0), first = from + sub0, count = (nsub + kChunkStep - 1) / kChunkStep;
             __syncthreads();                     // the previous table and stages are no longer in use
             const BlockRows where = make_block_rows<kChunkBlock>(s_row, a.kv, a.sh.n_kv_heads, at.b, kvh, first, nsub);
-            dma_step<D, kChunkWaves, 0, 0>(a.kv, where, 0, nsub, s_k0, s_v0);
+            dma_step<D, kChunkWaves, 0, 0>(a.kv, where, 0, nsub, s_kv, s_kv + kV);
             // Step s reads the stages of its parity, and the rows of step s + 1 go to those of the other parity, which were last read in
             // step s - 1: the barrier at its top orders both.
-            auto step = [&](int s, const char *k_cur, const char *v_cur, char *k_next, char *v_next) {
+#pragma unroll 1
+            for (int s = 0; s < count; ++s) {
                 wait_for_own_loads();            // the barrier alone does not wait for LDS-direct loads
                 __syncthreads();
-                if (s + 1 < count) dma_step<D, kChunkWaves, 0, 0>(a.kv, where, s + 1, nsub, k_next, v_next);
+                char *const next = s_kv + (s + 1) % 2 * S::kBytes;
+                if (s + 1 < count) dma_step<D, kChunkWaves, 0, 0>(a.kv, where, s + 1, nsub, next, next + kV);
                 const int tok = first + s * kChunkStep;
-                if (!wave_live || wave.none(tok, kChunkStep)) return;
-                if (wave.all(tok, kChunkStep)) body(std::false_type{}, k_cur, v_cur, tok);
-                else body(std::true_type{}, k_cur, v_cur, tok);
-            };
-            for (int s = 0; s < count; s += 2) {
-                step(s, s_k0, s_v0, s_k1, s_v1);
-                if (s + 1 < count) step(s + 1, s_k1, s_v1, s_k0, s_v0);
+                if (wave_live && !wave.none(tok, kChunkStep)) body(s_kv + s % 2 * S::kBytes, tok);
             }
         }
     }
 
     __syncthreads();                             // all waves have read the stages
-    OddTokens<D> &notes = *reinterpret_cast<OddTokens<D> *>(s_v1);
-    static_assert(sizeof(OddTokens<D>) <= sizeof(s_v1), "the notes lie in a stage");
+    OddTokens<D> &notes = *reinterpret_cast<OddTokens<D> *>(s_kv);
+    static_assert(sizeof(OddTokens<D>) <= sizeof(s_kv), "the notes lie in a stage");
     settle_odd<bf16_t, D>(a, at.b, kvh, sees, steps, seq.len, met_odd, s_odd, notes, acc);
     store_row<D>(a, at, kvh, rp, halves_sum(run.l), shift_of(run.m, map.k2), acc);
 }

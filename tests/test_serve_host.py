@@ -180,7 +180,7 @@ def test_verify_pin():
     three quarters."""
     p, q = np.array([[[.5, .3, .2]] * 2]), np.array([[[.2, .7, .1]] * 2])
     for u, un, want in ((.42, .9, ([0, 1], 2, 2)), (.43, .74, ([0, -1], 1, 0)), (.43, .76, ([0, -1], 1, 2))):
-        path, cnt, nxt, _ = so.verify(p, q, [[0, 1]], [[0, u]], [un])
+        path, cnt, nxt, _ = so.verify(p, q, np.array([[0, 1]]), np.array([[0, u]]), [un])
         assert (path[0].tolist(), cnt[0], nxt[0]) == want
-    path, cnt, nxt, _ = so.verify(p, None, [[0, 1]], [[0, .31]], [.72])        # without q: .5 and .2 are left
+    path, cnt, nxt, _ = so.verify(p, None, np.array([[0, 1]]), np.array([[0, .31]]), [.72])        # without q: .5 and .2 are left
     assert (cnt[0], nxt[0]) == (1, 2)
