@@ -216,36 +216,32 @@ template <int MODE, bool FINE> struct ScoreMap {
         slope2 = MODE == kBiased ? a.slopes[head] * kTreeLog2e : 0.f;
         k2 = MODE == kPlainScores ? scale2 : MODE == kCapped ? cap2 : 1.f;
     }
-    // c[t][r] is the product with token first + 32 t + 8 (r / 4) + r % 4 of a row at position pos
-    template <int NT> __device__ __forceinline__ void apply(floatx16 (&c)[NT], int pos, int first) const {
+    // The N values of a lane, get(i) and set(i, x): products with tokens first + off(i) of a row at position pos.
+    template <int N, typename Get, typename Set, typename Off>
+    __device__ __forceinline__ void each(Get get, Set set, Off off, int pos, int first) const {
         if constexpr (MODE == kPlainScores) return;
         const float d = (float)(pos - first);
-        auto biased = [&](float x, float factor, int t, int r) {
-            return fmaf(-slope2, fabsf(d - (float)(32 * t + 8 * (r / 4) + r % 4)), x * factor);
-        };
+        auto biased = [&](float x, float factor, int i) { return fmaf(-slope2, fabsf(d - (float)off(i)), x * factor); };
         if (MODE == kBiased && kx == 0.f) {      // uniform over the launch
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) c[t][r] = biased(c[t][r], scale2, t, r);
+            for (int i = 0; i < N; ++i) set(i, biased(get(i), scale2, i));
             return;
         }
         float most = 0.f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(c[t][r]));
+        for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(get(i)));
         const bool near = !any_lane(!(most * kx <= kTanhNear));
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) c[t][r] = near ? tanh_near<FINE>(c[t][r] * kx) : tanh_any<FINE>(c[t][r] * kx);
+        for (int i = 0; i < N; ++i) set(i, near ? tanh_near<FINE>(get(i) * kx) : tanh_any<FINE>(get(i) * kx));
         if constexpr (MODE == kBiased) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) c[t][r] = biased(c[t][r], cap2, t, r);
+            for (int i = 0; i < N; ++i) set(i, biased(get(i), cap2, i));
         }
+    }
+    // c[t][r]: token first + 32 t + 8 (r / 4) + r % 4
+    template <int NT> __device__ __forceinline__ void apply(floatx16 (&c)[NT], int pos, int first) const {
+        each<16 * NT>([&](int i) { return c[i / 16][i % 16]; }, [&](int i, float x) { c[i / 16][i % 16] = x; },
+                      [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; }, pos, first);
     }
 };
 

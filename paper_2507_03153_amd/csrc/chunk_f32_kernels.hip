@@ -8,7 +8,7 @@
 // What bounds it: the matrix cores, 64 cycles of a SIMD for 32 x 32 x 2.
 #include <algorithm>
 
-#include "chunk_device.hpp"
+#include "chunk_few.hpp"
 
 namespace hgca {
 
@@ -66,6 +66,17 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
     seq.unify();
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
     const RowPlace rp(a, seq, at.unit, kvh, 32 * w + n);
+    const RowSees sees(a, seq, rp.query);
+    const WaveSees wave(sees);
+    int lo, hi;
+    unit_range(wave, s_range, lo, hi);
+    const Steps steps(seq.pre, lo, hi, at.share, at.n_shares);
+    if (((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows <= kFewRows) {      // uniform over the workgroup
+        FewShared<D> &few = *reinterpret_cast<FewShared<D> *>(s_kv);
+        static_assert(sizeof(FewShared<D>) <= sizeof(s_kv), "the waves' results lie in the stages");
+        few_rows_f32<D, MODE>(few, s_row, a, at, seq, steps, kvh);
+        return;
+    }
     const bool wave_live = any_lane(rp.live);       // uniform over the wave
     float4 qop[KP];
     {
@@ -73,11 +84,6 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
 #pragma unroll
         for (int j = 0; j < KP; ++j) qop[j] = __builtin_bit_cast(float4, load16(q + 16 * (2 * j + hw)));
     }
-    const RowSees sees(a, seq, rp.query);
-    const WaveSees wave(sees);
-    int lo, hi;
-    unit_range(wave, s_range, lo, hi);
-    const Steps steps(seq.pre, lo, hi, at.share, at.n_shares);
     const int pos = seq.len - seq.nq + rp.query;
     const ScoreMap<MODE, true> map(a, rp.head);
     int v_lane[4];                               // of token 4 hw + i, columns n / 4 ..

@@ -11,7 +11,7 @@
 // A wave tells by its rows' ranges which steps all of them see (no mask), and which none (left out).
 #include <algorithm>
 
-#include "chunk_device.hpp"
+#include "chunk_few.hpp"
 
 namespace hgca {
 
@@ -35,6 +35,17 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
     seq.unify();
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
     const RowPlace rp(a, seq, at.unit, kvh, 32 * w + n);
+    const RowSees sees(a, seq, rp.query);
+    const WaveSees wave(sees);
+    int lo, hi;
+    unit_range(wave, s_range, lo, hi);
+    const Steps steps(seq.pre, lo, hi, at.share, at.n_shares);
+    if (((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows <= kFewRows) {      // uniform over the workgroup
+        FewShared<D> &few = *reinterpret_cast<FewShared<D> *>(s_kv);
+        static_assert(sizeof(FewShared<D>) <= sizeof(s_kv), "the waves' results lie in the stages");
+        few_rows_bf16<D, PP, MODE>(few, s_row, a, at, seq, steps, kvh);
+        return;
+    }
     const bool wave_live = any_lane(rp.live);       // uniform over the wave
     uint4 qop[KK];
     {
@@ -42,11 +53,6 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) qop[kk] = load16(q + 16 * (2 * kk + hw));
     }
-    const RowSees sees(a, seq, rp.query);
-    const WaveSees wave(sees);
-    int lo, hi;
-    unit_range(wave, s_range, lo, hi);
-    const Steps steps(seq.pre, lo, hi, at.share, at.n_shares);
     const int pos = seq.len - seq.nq + rp.query;
     const ScoreMap<MODE, PP != 1> map(a, rp.head);
     int k_lane[KK];
