@@ -17,6 +17,29 @@ namespace hgca {
 
 namespace {
 
+// kinds of instructions for sched_group_barrier: the matrix ones, the other vector ones, LDS reads
+constexpr int kSchedMatrix = 0x8, kSchedVector = 0x402, kSchedLds = 0x100;
+
+// Takes infinities and NaN out of a step's V rows, for all waves; true if there were any (settle_odd brings them to the rows that see them).
+// Called by waves of which some row does not see all of the step; one that reads the rows before or while they change has sums that are
+// not finite.
+template <int D> __device__ __forceinline__ bool clean_stage(char *v_stage)
+{
+    constexpr int kPieces = kChunkStep * 2 * D / 16;
+    uint32_t odd = 0;
+#pragma unroll 4
+    for (int i = threadIdx.x % kWave; i < kPieces; i += kWave) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(v_stage + 16 * i);
+        odd |= odd_carry(x.x) | odd_carry(x.y) | odd_carry(x.z) | odd_carry(x.w);
+    }
+    if (!any_lane((odd & kSigns) != 0)) return false;
+    for (int i = threadIdx.x % kWave; i < kPieces; i += kWave) {
+        uint4 &x = *reinterpret_cast<uint4 *>(v_stage + 16 * i);
+        x = make_uint4(x.x & ~odd_halves(x.x), x.y & ~odd_halves(x.y), x.z & ~odd_halves(x.z), x.w & ~odd_halves(x.w));
+    }
+    return true;
+}
+
 template <int D, int PP, int MODE>
 __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 {
@@ -68,7 +91,7 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 
     // One step.  c[t][r] is the score of step token 32 t + 8 (r / 4) + 4 hw + r % 4; group g of the second product is 16 tokens, of
     // which the lane holds eight.
-    auto body = [&](const char *stage, int tok) {
+    auto body = [&](char *stage, int tok) {
         const bool masked = !wave.all(tok, kChunkStep);          // uniform over the wave
         floatx16 c[NT];
 #pragma unroll
@@ -88,6 +111,7 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
             for (int t = 0; t < NT; ++t) c[t] = score_mfma(kf[kk][t], qop[kk], c[t]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (masked) met_odd = clean_stage<D>(stage + kV) || met_odd;
         uint4 vop[2][DT];
         auto read_v = [&](int g, uint4 (&x)[DT]) {
             const char *v = stage + kV + S::v_offset(16 * g, 0) + v_lane;
@@ -132,24 +156,13 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
             }
         };
         weigh(0);
+        // The weights of the next group are worked out between the matrix instructions of this one: left to itself the compiler puts these side by
+        // side, and a wave waits for each.
 #pragma unroll
         for (int g = 0; g < 2 * NT; ++g) {
             __builtin_amdgcn_sched_barrier(0);
             uint4(&v)[DT] = vop[g % 2];
             if (g + 1 < 2 * NT) read_v(g + 1, vop[(g + 1) % 2]);
-            if (masked) {                        // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
-                uint32_t odd = 0;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) odd |= odd_carry(v[dt].x) | odd_carry(v[dt].y) | odd_carry(v[dt].z) | odd_carry(v[dt].w);
-                if (any_lane((odd & kSigns) != 0)) {
-                    met_odd = true;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        uint4 &x = v[dt];
-                        x = make_uint4(x.x & ~odd_halves(x.x), x.y & ~odd_halves(x.y), x.z & ~odd_halves(x.z), x.w & ~odd_halves(x.w));
-                    }
-                }
-            }
             uint32_t now[PP][4];
 #pragma unroll
             for (int t = 0; t < PP; ++t)
@@ -160,7 +173,15 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt)
                     acc[dt] = score_mfma(v[dt], make_uint4(now[t][0], now[t][1], now[t][2], now[t][3]), acc[dt]);
-            if (g + 1 < 2 * NT) weigh(g + 1);
+            if (g + 1 < 2 * NT) {
+                weigh(g + 1);
+                __builtin_amdgcn_sched_group_barrier(kSchedLds, 2 * DT, 0);
+#pragma unroll
+                for (int i = 0; i < PP * DT; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kSchedVector, (20 + 16 * PP) / (PP * DT), 0);
+                }
+            }
         }
         run.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
