@@ -187,6 +187,45 @@ struct Steps {
     __device__ __forceinline__ int end(int range) const { return range ? end1 : end0; }
 };
 
+// ---- where the tokens lie ----
+// A wave keeps the rows of 64 granules of 16 tokens in a register, a lane each, and requests the next 64 when it comes to them: a step's
+// rows are then read off by number, with no round trip to LDS or memory before its loads.  (Blocks are whole granules.)
+struct GranuleRows {
+    const int32_t *blocks;                       // the sequence's table row, or null: contiguous
+    uint32_t head;                               // first row of the KV head, of a block's heads if paged
+    int bs, heads, last;                         // last: granule of the sequence's last token
+    int base;
+    uint32_t now, next;                          // of granules base + lane and base + 64 + lane
+    __device__ __forceinline__ GranuleRows(const ChunkArgs &a, int b, int kvh, int len) {
+        blocks = a.kv.block_table ? a.kv.block_table + (int64_t)b * a.kv.max_blocks + (a.kv.first_block ? a.kv.first_block[b] : 0) : nullptr;
+        head = a.kv.block_table ? (uint32_t)kvh : (uint32_t)(((int64_t)b * a.sh.n_kv_heads + kvh) * a.kv.cap);
+        bs = a.kv.block_size;
+        heads = a.sh.n_kv_heads;
+        last = max(len - 1, 0) / kGranule;
+        base = 0;
+        now = next = 0;
+    }
+    __device__ __forceinline__ uint32_t fetch(int first) const {
+        const int g = min(first + (int)(threadIdx.x % kWave), last), tok = g * kGranule;
+        if (!blocks) return head + (uint32_t)tok;
+        const int blk = tok / bs;
+        return ((uint32_t)blocks[blk] * (uint32_t)heads + head) * (uint32_t)bs + (uint32_t)(tok - blk * bs);
+    }
+    __device__ __forceinline__ void start(int granule) {
+        base = granule;
+        now = fetch(base);
+        next = fetch(base + kWave);
+    }
+    // granules up to `granule` + 3 are to be had; called with ascending ones, by whole waves
+    __device__ __forceinline__ void reach(int granule) {
+        if (granule + 3 < base + kWave) return;
+        base += kWave;
+        now = next;
+        next = fetch(base + kWave);
+    }
+    __device__ __forceinline__ uint32_t row(int granule) const { return __builtin_amdgcn_readlane(now, granule - base); }
+};
+
 // ---- scores ----
 // kPlainScores: what the softmax runs over is the product, times sm_scale log2 e in the exponent of 2.  kCapped: tanh(product * sm_scale / cap), times
 // cap log2 e.  kBiased: the score itself in units of ln 2, capped or not, less slope * distance.

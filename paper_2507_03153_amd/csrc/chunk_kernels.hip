@@ -40,6 +40,49 @@ template <int D> __device__ __forceinline__ bool clean_stage(char *v_stage)
     return true;
 }
 
+// Requests K and V rows of tokens tok .. tok + 63, `there` of which exist (the others repeat the last one).  A load of a wave covers kGroupRows
+// rows of one granule, so that in a full step its address is a scalar and an offset that is the lane's for good.
+template <int D>
+__device__ __forceinline__ void request_step(const ChunkArgs &a, const GranuleRows &rows, int tok, int there, char *k_stage, char *v_stage)
+{
+    using S = DmaStage<D, kChunkWaves>;
+    static_assert(16 % S::kSwizzled == 0 && kChunkWaves * S::kGroupRows % kGranule == 0, "the lane's offsets are those of every group of the wave");
+    constexpr int kQuadLanes = 4 * S::kRowBytes / 16;
+    typedef const __attribute__((address_space(1))) char *GlobalBytes;
+    typedef const __attribute__((address_space(1))) void *GlobalPtr;
+    typedef __attribute__((address_space(3))) void *LdsPtr;
+    const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), granule = tok / kGranule;
+    // what lands at byte 16 * lane of a group: the row inside the group and the byte of the row
+    const int k_row = lane / S::kPieces, v_row = 4 * (lane / kQuadLanes) + (lane % 8) / 2;
+    const int k_byte = 16 * ((lane % S::kPieces) ^ S::k_swizzle(w * S::kGroupRows + k_row)), v_byte = 16 * (2 * ((lane % kQuadLanes) / 8) + lane % 2);
+    const GlobalBytes k = (GlobalBytes)a.kv.k, v = (GlobalBytes)a.kv.v;
+    auto scalar = [](GlobalBytes p) {            // keeps the address in scalar registers: the compiler adds the lane's offset to it first
+        uint64_t x = (uint64_t)p;
+        asm("" : "+s"(x));
+        return (GlobalBytes)x;
+    };
+    if (there >= kChunkStep) {                   // uniform over the workgroup
+        const uint32_t k_off = k_row * S::kRowBytes + k_byte, v_off = v_row * S::kRowBytes + v_byte;
+#pragma unroll
+        for (int u = 0; u < S::kLoads; ++u) {
+            const int group = w + kChunkWaves * u, first = group * S::kGroupRows;
+            const size_t at = (size_t)(rows.row(granule + first / kGranule) + first % kGranule) * S::kRowBytes;
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(scalar(k + at) + k_off), (LdsPtr)(k_stage + group * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(scalar(v + at) + v_off), (LdsPtr)(v_stage + group * 1024), 16, 0, 0);
+        }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < S::kLoads; ++u) {
+        const int group = w + kChunkWaves * u;
+        const int kt = min(group * S::kGroupRows + k_row, there - 1), vt = min(group * S::kGroupRows + v_row, there - 1);
+        const uint32_t kr = __shfl(rows.now, granule + kt / kGranule - rows.base) + kt % kGranule;
+        const uint32_t vr = __shfl(rows.now, granule + vt / kGranule - rows.base) + vt % kGranule;
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(k + (size_t)kr * S::kRowBytes + k_byte), (LdsPtr)(k_stage + group * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(v + (size_t)vr * S::kRowBytes + v_byte), (LdsPtr)(v_stage + group * 1024), 16, 0, 0);
+    }
+}
+
 template <int D, int PP, int MODE>
 __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 {
@@ -186,27 +229,30 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
         run.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
 
+    GranuleRows rows(a, at.b, kvh, seq.len);
 #pragma unroll 1
     for (int range = 0; range < 2; ++range) {
-        const int from = steps.begin(range) * kChunkStep, total = min(steps.end(range) * kChunkStep, seq.len) - from;
-        const int sub_len = pass_length(a.kv, total);
+        const int begin = steps.begin(range), end = steps.end(range);
+        if (begin >= end) continue;
+        __syncthreads();                         // the stages are no longer in use
+        rows.start(begin * (kChunkStep / kGranule));
+        request_step<D>(a, rows, begin * kChunkStep, seq.len - begin * kChunkStep, s_kv, s_kv + kV);
+        // A step reads the stages of its parity, and the rows of the next one go to those of the other parity, which were last read in
+        // the step before: the barrier at its top orders both.
+        char *stage = s_kv, *other = s_kv + S::kBytes;
 #pragma unroll 1
-        for (int sub0 = 0; sub0 < total; sub0 += sub_len) {
-            const int nsub = min(sub_len, total - sub0), first = from + sub0, count = (nsub + kChunkStep - 1) / kChunkStep;
-            __syncthreads();                     // the previous table and stages are no longer in use
-            const BlockRows where = make_block_rows<kChunkBlock>(s_row, a.kv, a.sh.n_kv_heads, at.b, kvh, first, nsub);
-            dma_step<D, kChunkWaves, 0, 0>(a.kv, where, 0, nsub, s_kv, s_kv + kV);
-            // Step s reads the stages of its parity, and the rows of step s + 1 go to those of the other parity, which were last read in
-            // step s - 1: the barrier at its top orders both.
-#pragma unroll 1
-            for (int s = 0; s < count; ++s) {
-                wait_for_own_loads();            // the barrier alone does not wait for LDS-direct loads
-                __syncthreads();
-                char *const next = s_kv + (s + 1) % 2 * S::kBytes;
-                if (s + 1 < count) dma_step<D, kChunkWaves, 0, 0>(a.kv, where, s + 1, nsub, next, next + kV);
-                const int tok = first + s * kChunkStep;
-                if (wave_live && !wave.none(tok, kChunkStep)) body(s_kv + s % 2 * S::kBytes, tok);
+        for (int s = begin; s < end; ++s) {
+            const int tok = s * kChunkStep;
+            wait_for_own_loads();                // the barrier alone does not wait for LDS-direct loads
+            __syncthreads();
+            if (s + 1 < end) {
+                rows.reach((tok + kChunkStep) / kGranule);
+                request_step<D>(a, rows, tok + kChunkStep, seq.len - tok - kChunkStep, other, other + kV);
             }
+            if (wave_live && !wave.none(tok, kChunkStep)) body(stage, tok);
+            char *const t = stage;
+            stage = other;
+            other = t;
         }
     }
 
