@@ -15,12 +15,24 @@ static_assert(kChunkRows == 32 * kChunkWaves, "32 rows per wave");
 // true where a lane has it, uniform over the wave
 __device__ __forceinline__ bool any_lane(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
 
+__device__ __forceinline__ int wave_min_int(int v) {
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) v = min(v, __shfl_xor(v, step));
+    return v;
+}
+__device__ __forceinline__ int wave_max_int(int v) {
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) v = max(v, __shfl_xor(v, step));
+    return v;
+}
+
 // ---- the cut ----
 // A sequence of n tokens has u = ceil(n * group / kChunkRows) units, each over at most `steps` steps of its tokens.  Units are cut into shares
-// of at most C steps, C = the steps of all units over the number of shares aimed at (and kChunkLeast at least): s = ceil(steps / C)
-// shares each, so that there are at most target + (number of units) shares, and at most 2 target in units that have several.
-// One long sequence among many short ones, a prompt among single tokens: a share is as long as any other.  Up to 64 sequences every wave works it
-// out for itself, a lane per sequence, from the lengths on the device; more are worked out by a launch before.
+// of at most C steps: s = ceil(steps / C) each.  C is at least kChunkLeast, and the least with which there are no more shares than the
+// `target` that runs at once; where there are more units than that, the steps of all units over the target.  So there are at
+// most target + (number of units) shares, and at most 2 target in units that have several.  One long sequence among many short ones, a
+// prompt among single tokens: a share is as long as any other.  Up to 64 sequences every wave works it out for itself, a lane per
+// sequence, from the lengths on the device; more are worked out by a launch before.
 constexpr int kChunkLeast = 4;
 
 struct SeqWork {
@@ -42,8 +54,20 @@ struct SeqWork {
     }
 };
 
-__device__ __forceinline__ int share_steps(const ChunkArgs &a, float all) {
-    return max((int)(all / (float)a.target * 1.0001f) + 1, kChunkLeast);
+// C, for sums over the sequences of units and of units * steps, the longest steps, and shares(c), the number of shares of at most c steps (saturated, fp32)
+template <typename Shares> __device__ __forceinline__ int share_steps(const ChunkArgs &a, float units, float work, int longest, Shares shares) {
+    const float target = (float)a.target;
+    int c = max((int)(work / target), kChunkLeast);
+    if (units > target) return max((int)(work / target * 1.0001f) + 1, kChunkLeast);
+    if (c >= longest || shares(c) <= target) return c;
+    // shares(c) <= work / c + units, and one share each is few enough
+    int enough = units < target ? (int)min(work / (target - units) * 1.0001f + 1.f, (float)longest) : longest;
+#pragma unroll 1
+    while (enough - c > max(c / 32, 1)) {
+        const int mid = c + (enough - c) / 2;
+        if (shares(mid) <= target) enough = mid; else c = mid;
+    }
+    return max(enough, kChunkLeast);
 }
 // 0 for a sequence without new tokens
 __device__ __forceinline__ int shares_of(const SeqWork &q, int c) { return q.units > 0 ? (q.steps + c - 1) / c : 0; }
@@ -73,15 +97,14 @@ struct Place {
         idle = true;
         if (B <= kWave) {
             units = n_shares = 0;
-            float work = 0.f;
-            int steps = 1;
+            int steps = 0;
             if (lane < B) {
                 const SeqWork q(a, lane);
                 units = q.units;
-                steps = q.steps;
-                work = (float)units * (float)steps;
+                steps = units > 0 ? q.steps : 0;
             }
-            const int c = share_steps(a, wave_sum(work));
+            const int c = share_steps(a, wave_sum((float)units), wave_sum((float)units * (float)steps), wave_max_int(steps),
+                                      [&](int c) { return wave_sum((float)units * (float)((steps + c - 1) / c)); });
             const int shares = units > 0 ? (steps + c - 1) / c : 0, slots = units * shares, several = shares > 1 ? slots : 0;
             const int parts = (int)wave_inclusive_scan((uint32_t)several) - several;
             const int mine = FOLD ? (shares > 1 ? units : 0) : slots, upto = (int)wave_inclusive_scan((uint32_t)mine);
@@ -136,17 +159,6 @@ struct RowSees {
         return below(pre) | (below(hi) & ~below(lo));
     }
 };
-
-__device__ __forceinline__ int wave_min_int(int v) {
-#pragma unroll
-    for (int step = kWave / 2; step > 0; step /= 2) v = min(v, __shfl_xor(v, step));
-    return v;
-}
-__device__ __forceinline__ int wave_max_int(int v) {
-#pragma unroll
-    for (int step = kWave / 2; step > 0; step /= 2) v = max(v, __shfl_xor(v, step));
-    return v;
-}
 
 // What the rows of a wave see together: everything in [0, pre) and [all_lo, all_hi), nothing outside [0, pre) and [any_lo, any_hi).
 struct WaveSees {

@@ -272,18 +272,32 @@ __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
     __shared__ float s_work[kCutWaves];
     __shared__ uint32_t s_sum[3][kCutWaves];
     const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, B = a.sh.batch;
-    float work = 0.f;
+    auto over_all = [&](float x, bool largest) { // a workgroup's sum or maximum, in every thread
+        x = largest ? wave_max(x) : wave_sum(x);
+        __syncthreads();
+        if (lane == 0) s_work[w] = x;
+        __syncthreads();
+        x = s_work[0];
+#pragma unroll
+        for (int i = 1; i < kCutWaves; ++i) x = largest ? fmaxf(x, s_work[i]) : x + s_work[i];
+        return x;
+    };
+    float units = 0.f, work = 0.f, longest = 0.f;
     for (int b = tid; b < B; b += kCutBlock) {
         const SeqWork q(a, b);
+        if (q.units == 0) continue;
+        units += (float)q.units;
         work += (float)q.units * (float)q.steps;
+        longest = fmaxf(longest, (float)q.steps);
     }
-    work = wave_sum(work);
-    if (lane == 0) s_work[w] = work;
-    __syncthreads();
-    work = s_work[0];
-#pragma unroll
-    for (int i = 1; i < kCutWaves; ++i) work += s_work[i];
-    const int c = share_steps(a, work);
+    const int c = share_steps(a, over_all(units, false), over_all(work, false), (int)over_all(longest, true), [&](int c) {
+        float n = 0.f;
+        for (int b = tid; b < B; b += kCutBlock) {
+            const SeqWork q(a, b);
+            n += (float)q.units * (float)shares_of(q, c);
+        }
+        return over_all(n, false);
+    });
     int32_t *const lists = a.cut + 1;            // three lists of B + 1 beginnings: slots, partials, units with several shares
     if (tid == 0) a.cut[0] = c;
     if (tid < 3) lists[tid * (B + 1)] = 0;
@@ -319,25 +333,19 @@ __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
 
 constexpr int kChunkFoldRows = 8;                // rows of a workgroup
 
-// Rows of a unit that has several shares: O = sum o_s 2^(m_s - M) / L, L = sum l_s 2^(m_s - M), m_s in powers of 2.  A row's columns are held by D / 4
-// lanes, four each; where a unit has fewer rows than a workgroup takes, several sets of lanes share a row's partials.
+// Rows row0 .. of a unit that has several shares, kChunkFoldRows of them or as many as there are left: O = sum o_s 2^(m_s - M) / L, L = sum l_s 2^(m_s -
+// M), m_s in powers of 2.  A row's columns are held by D / 4 lanes, four each; where there are fewer rows than a workgroup takes,
+// several sets of lanes share a row's partials.
 template <int D>
-__global__ __launch_bounds__(kChunkFoldRows * D / 4) void chunk_fold_kernel(ChunkArgs a)
+__device__ __forceinline__ void fold_rows(const ChunkArgs &a, const Place &at, const SeqWork &seq, int kvh, int row0, int rows)
 {
     constexpr int C4 = D / 4;
     __shared__ float4 s_acc[kChunkFoldRows][C4];
     __shared__ float s_m[kChunkFoldRows], s_l[kChunkFoldRows];
-    const int kvh = blockIdx.y, set = threadIdx.x / C4, c4 = threadIdx.x % C4;
-    Place at;
-    at.find<true>(a, blockIdx.x);
-    if (at.idle) return;                         // uniform over the workgroup
-    const SeqWork seq(a, at.b);
-    const int64_t left = ((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows;
-    const int rows = (int)min(left, (int64_t)kChunkRows) - (int)blockIdx.z * kChunkFoldRows;         // from this workgroup's first on
-    if (rows <= 0) return;
+    const int set = threadIdx.x / C4, c4 = threadIdx.x % C4;
     int per_row = 1;                             // sets of lanes that share a row
     while (per_row * 2 * rows <= kChunkFoldRows) per_row *= 2;
-    const int mine = set / per_row, r = blockIdx.z * kChunkFoldRows + min(mine, rows - 1);
+    const int mine = set / per_row, r = row0 + min(mine, rows - 1);
     float m = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     auto join = [](float &m0, float &l0, float4 &a0, float m1, float l1, const float4 &a1) {
@@ -357,7 +365,7 @@ __global__ __launch_bounds__(kChunkFoldRows * D / 4) void chunk_fold_kernel(Chun
         const int64_t i = ((int64_t)(at.part + s) * a.sh.n_kv_heads + kvh) * kChunkRows + r;
         join(m, l, acc, a.part_m[i], a.part_l[i], *reinterpret_cast<const float4 *>(a.part_o + i * D + 4 * c4));
     }
-    if (per_row > 1) {                           // uniform over the workgroup
+    if (per_row > 1) {                           // uniform over the workgroup; then there are no further rows
         s_acc[set][c4] = acc;
         if (c4 == 0) {
             s_m[set] = m;
@@ -377,6 +385,18 @@ __global__ __launch_bounds__(kChunkFoldRows * D / 4) void chunk_fold_kernel(Chun
     else
         *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + rp.out * D + 4 * c4) = make_float4(x[0], x[1], x[2], x[3]);
     if (c4 == 0) a.lse[rp.out] = none ? -INFINITY : (__builtin_amdgcn_logf(l) + m) * kLn2;
+}
+
+template <int D>
+__global__ __launch_bounds__(kChunkFoldRows * D / 4) void chunk_fold_kernel(ChunkArgs a)
+{
+    Place at;
+    at.find<true>(a, blockIdx.x);
+    if (at.idle) return;                         // uniform over the workgroup
+    const SeqWork seq(a, at.b);
+    const int rows = (int)min(((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows, (int64_t)kChunkRows);
+    for (int row0 = blockIdx.z * kChunkFoldRows; row0 < rows; row0 += gridDim.z * kChunkFoldRows)
+        fold_rows<D>(a, at, seq, blockIdx.y, row0, rows - row0);
 }
 
 }  // namespace
@@ -408,8 +428,12 @@ hipError_t launch_chunk_attn(int dtype, int head_dim, const ChunkArgs &a, hipStr
     }
     rc = dtype == 0 ? launch_chunk_rows_f32(head_dim, a, s) : launch_chunk_rows_bf16(head_dim, a, s);
     if (rc != hipSuccess || a.parts == 0) return rc;
-    // a unit with several shares has two at least
-    const dim3 grid((unsigned)std::max(a.parts / 2, 1), (unsigned)a.sh.n_kv_heads, kChunkRows / kChunkFoldRows);
+    // a unit with several shares has two at least; how many there are is known on the device only, and most workgroups of a large grid leave
+    // at once
+    const int64_t rows = std::min<int64_t>(kChunkRows, (int64_t)a.n_tokens * a.sh.group), units = std::max(std::min(a.parts / 2, a.units), 1);
+    int64_t z = (rows + kChunkFoldRows - 1) / kChunkFoldRows;
+    while (z > 2 && units * a.sh.n_kv_heads * z > 2048) z = (z + 1) / 2;
+    const dim3 grid((unsigned)units, (unsigned)a.sh.n_kv_heads, (unsigned)z);
     if (head_dim == 64) hipLaunchKernelGGL(chunk_fold_kernel<64>, grid, dim3(kChunkFoldRows * 64 / 4), 0, s, a);
     else hipLaunchKernelGGL(chunk_fold_kernel<128>, grid, dim3(kChunkFoldRows * 128 / 4), 0, s, a);
     return hipGetLastError();

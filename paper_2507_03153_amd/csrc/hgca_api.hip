@@ -396,14 +396,14 @@ PlanArgs plan_args(const hgca_block_state *t)
 #define HGCA_TARGET_WGS_CHUNK 512
 #endif
 struct ChunkLayout {
-    int64_t slots, parts, target;                // per KV head
+    int64_t units, slots, parts, target;         // per KV head
     size_t part_m, part_l, cut, total;
 };
 
 ChunkLayout chunk_layout(const hgca_shape *s, int64_t n_tokens, int64_t cap)
 {
     ChunkLayout t{};
-    const int64_t units = n_tokens * group_of(s) / kChunkRows + std::min<int64_t>(n_tokens, s->batch);       // at most
+    const int64_t units = t.units = n_tokens * group_of(s) / kChunkRows + std::min<int64_t>(n_tokens, s->batch);         // at most
     t.target = std::max<int64_t>(1, HGCA_TARGET_WGS_CHUNK / s->n_kv_heads);
     // a share has 256 tokens at least, so a unit has so many at most, and one where the tier is that short
     const int64_t shares = std::max<int64_t>(1, (cap + 255) / 256);
@@ -1899,6 +1899,7 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
     a.lse = lse_out;
     a.slots = (int32_t)t.slots;
     a.parts = (int32_t)t.parts;
+    a.units = (int32_t)t.units;
     a.target = (int32_t)t.target;
     a.cut = reinterpret_cast<int32_t *>(base + t.cut);
     a.part_o = reinterpret_cast<float *>(base);

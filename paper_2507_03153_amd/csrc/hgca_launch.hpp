@@ -379,7 +379,7 @@ struct ChunkArgs {
     int32_t o_bf16;
     void *o;                   // [T, Hq, d]
     float *lse;                // [T, Hq]
-    int32_t slots, parts;      // per KV head: slots of the launch; those of them that leave partials, at most
+    int32_t slots, parts, units;          // per KV head: slots of the launch; those of them that leave partials, and units, at most
     int32_t target;            // shares that all units together aim at, per KV head
     int32_t *cut;              // more than 64 sequences: what chunk_cut_kernel worked out, [3 B + 4]
     float *part_o, *part_m, *part_l;      // [parts, Hkv, kChunkRows (, d)]
