@@ -15,43 +15,46 @@ namespace hgca {
 
 namespace {
 
-constexpr int kPlanBlock = 1024, kPlanWaves = kPlanBlock / kWave;
+// threads of the workgroup of the sums, and the sequences of one round of them
+constexpr int kPlanSmall = 256, kPlanLarge = 1024;
 constexpr int kPlanOneLaunch = 4096;             // tokens that the workgroup of the sums maps itself
 
 constexpr int kContextFull = 2, kBlocksOut = 8, kTokensFull = 16;        // HGCA_CACHE_* bits of the status
 
-__device__ __forceinline__ int64_t wave_scan64(int64_t v) {
-    const int lane = threadIdx.x % kWave;
+// Inclusive prefix sums over the workgroup of N values, and their totals, in 32 bits; contains barriers, all threads take part.
+template <int BLOCK, int N>
+__device__ __forceinline__ void scan(uint32_t (&v)[N], uint32_t (&total)[N], uint32_t (&s)[N][BLOCK / kWave]) {
+    constexpr int W = BLOCK / kWave;
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
 #pragma unroll
-    for (int step = 1; step < kWave; step *= 2) {
-        const int64_t o = __shfl_up(v, step);
-        if (lane >= step) v += o;
+    for (int k = 0; k < N; ++k) v[k] = wave_inclusive_scan(v[k]);
+    __syncthreads();                             // the last use of s is over
+    if (lane == kWave - 1) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k][w] = v[k];
     }
-    return v;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        total[k] = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            v[k] += i < w ? s[k][i] : 0;
+            total[k] += s[k][i];
+        }
+    }
 }
 
-// Inclusive prefix sums of two values over the workgroup; contains barriers, all threads take part.
+// The same of two values below 2^31 each, whose sums may need more bits: in parts of 20 and 11 bits.
 struct TwoSums {
     int64_t a, b;
 };
-__device__ TwoSums scan_two(int64_t a, int64_t b, int64_t (&s)[2][kPlanWaves], TwoSums &total) {
-    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
-    a = wave_scan64(a);
-    b = wave_scan64(b);
-    __syncthreads();                             // the last use of s is over
-    if (lane == kWave - 1) {
-        s[0][w] = a;
-        s[1][w] = b;
-    }
-    __syncthreads();
-    TwoSums before{0, 0};
-    total = TwoSums{0, 0};
-#pragma unroll
-    for (int i = 0; i < kPlanWaves; ++i) {
-        if (i < w) before = TwoSums{before.a + s[0][i], before.b + s[1][i]};
-        total = TwoSums{total.a + s[0][i], total.b + s[1][i]};
-    }
-    return TwoSums{before.a + a, before.b + b};
+template <int BLOCK>
+__device__ __forceinline__ TwoSums scan_two(int64_t a, int64_t b, uint32_t (&s)[4][BLOCK / kWave], TwoSums &total) {
+    uint32_t v[4] = {(uint32_t)a & 0xfffffu, (uint32_t)(a >> 20), (uint32_t)b & 0xfffffu, (uint32_t)(b >> 20)}, t[4];
+    scan<BLOCK, 4>(v, t, s);
+    total = TwoSums{((int64_t)t[1] << 20) + t[0], ((int64_t)t[3] << 20) + t[2]};
+    return TwoSums{((int64_t)v[1] << 20) + v[0], ((int64_t)v[3] << 20) + v[2]};
 }
 
 // The first index i of ascending at[0 .. n] with at[i + 1] > t, for at[0] <= t < at[n].
@@ -82,16 +85,16 @@ __device__ __forceinline__ void place_token(const PlanArgs &a, int b, int i, int
 }
 
 // MAP: the workgroup maps the tokens itself, else it leaves each sequence's old length, old number of blocks and first granted block in scratch.
-template <bool MAP>
-__global__ __launch_bounds__(kPlanBlock) void kv_plan_kernel(PlanArgs a)
+template <int BLOCK, bool MAP>
+__global__ __launch_bounds__(BLOCK) void kv_plan_kernel(PlanArgs a)
 {
-    __shared__ int64_t s_sums[2][kPlanWaves];
-    __shared__ int32_t s_cu[kPlanBlock + 1], s_len[kPlanBlock], s_held[kPlanBlock], s_first[kPlanBlock];
+    __shared__ uint32_t s_sums[4][BLOCK / kWave], s_got[2][BLOCK / kWave];
+    __shared__ int32_t s_cu[BLOCK + 1], s_len[BLOCK], s_held[BLOCK], s_first[BLOCK];
     const int tid = threadIdx.x, bs = a.block_size;
     const int64_t count = min(max(a.free_count[0], 0), a.n_blocks), room = (int64_t)a.max_blocks * bs;
     TwoSums asked{0, 0}, granted{0, 0};          // of the sequences before this round's; a: blocks, b: tokens
     int32_t bits = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += kPlanBlock) {
+    for (int b0 = 0; b0 < a.batch; b0 += BLOCK) {
         const int b = b0 + tid;
         const bool real = b < a.batch;
         const int64_t len = real ? max(a.lens[b], 0) : 0, held = real ? min(max(a.held[b], 0), a.max_blocks) : 0;
@@ -103,15 +106,17 @@ __global__ __launch_bounds__(kPlanBlock) void kv_plan_kernel(PlanArgs a)
         }
         int64_t need = fits ? max((len + n + bs - 1) / bs - held, (int64_t)0) : 0;
         TwoSums all;
-        const TwoSums upto = scan_two(need, n, s_sums, all);
+        const TwoSums upto = scan_two<BLOCK>(need, n, s_sums, all);
         // first come, first served: a sequence that is refused keeps later ones from what it asked for
         const bool blocks = need == 0 || asked.a + upto.a <= count, tokens = n == 0 || asked.b + upto.b <= a.max_tokens;
         if (!blocks) bits |= kBlocksOut;
         if (!tokens) bits |= kTokensFull;
         if (!blocks || !tokens) need = n = 0;
         asked = TwoSums{asked.a + all.a, asked.b + all.b};
-        const TwoSums got = scan_two(need, n, s_sums, all);
-        const int64_t first = granted.a + got.a - need, cu = granted.b + got.b;
+        // what is granted is at most the free blocks and max_tokens
+        uint32_t got[2] = {(uint32_t)need, (uint32_t)n}, sum[2];
+        scan<BLOCK, 2>(got, sum, s_got);
+        const int64_t first = granted.a + got[0] - need, cu = granted.b + got[1];
         if (real) {
             a.cu[b + 1] = (int32_t)cu;
             if (n > 0) a.lens[b] = (int32_t)(len + n);
@@ -129,13 +134,13 @@ __global__ __launch_bounds__(kPlanBlock) void kv_plan_kernel(PlanArgs a)
             s_held[tid] = (int32_t)held;
             s_first[tid] = (int32_t)first;
             __syncthreads();
-            const int end = (int)(granted.b + all.b);
-            for (int t = (int)granted.b + tid; t < end; t += kPlanBlock) {
-                const int i = segment_of([&](int x) { return s_cu[x]; }, kPlanBlock, t);
+            const int end = (int)(granted.b + sum[1]);
+            for (int t = (int)granted.b + tid; t < end; t += BLOCK) {
+                const int i = segment_of([&](int x) { return s_cu[x]; }, BLOCK, t);
                 place_token(a, b0 + i, t - s_cu[i], s_len[i], s_held[i], s_first[i], (int)count, t);
             }
         }
-        granted = TwoSums{granted.a + all.a, granted.b + all.b};
+        granted = TwoSums{granted.a + sum[0], granted.b + sum[1]};
     }
     if (bits && a.status) atomicOr(a.status, bits);
     if (tid == 0) {
@@ -144,7 +149,7 @@ __global__ __launch_bounds__(kPlanBlock) void kv_plan_kernel(PlanArgs a)
         if (!MAP) a.scratch[3 * a.batch] = (int32_t)count;
     }
     if (MAP) {
-        for (int t = (int)granted.b + tid; t < a.max_tokens; t += kPlanBlock) {
+        for (int t = (int)granted.b + tid; t < a.max_tokens; t += BLOCK) {
             a.positions[t] = 0;
             a.slots[t] = -1;
         }
@@ -167,10 +172,11 @@ __global__ __launch_bounds__(kMapBlock) void kv_plan_tokens_kernel(PlanArgs a)
 }
 
 // What each sequence gives back is counted first: the stack's new top decides where the first block goes.
-__global__ __launch_bounds__(kPlanBlock) void kv_release_kernel(PlanArgs a)
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void kv_release_kernel(PlanArgs a)
 {
-    __shared__ int64_t s_sums[2][kPlanWaves];
-    __shared__ int32_t s_upto[kPlanBlock + 1], s_keep[kPlanBlock];
+    __shared__ uint32_t s_sums[4][BLOCK / kWave];
+    __shared__ int32_t s_upto[BLOCK + 1], s_keep[BLOCK];
     const int tid = threadIdx.x, bs = a.block_size;
     const int64_t count = min(max(a.free_count[0], 0), a.n_blocks);
     auto share = [&](int b, int32_t &len, int32_t &keep) {       // blocks that sequence b gives back
@@ -182,19 +188,20 @@ __global__ __launch_bounds__(kPlanBlock) void kv_release_kernel(PlanArgs a)
         return held - keep;
     };
     int64_t total = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += kPlanBlock) {
+    for (int b0 = 0; a.batch > BLOCK && b0 < a.batch; b0 += BLOCK) {         // (one round finds the total on its way)
         int32_t len, keep;
         TwoSums all;
-        scan_two(share(b0 + tid, len, keep), 0, s_sums, all);
+        scan_two<BLOCK>(share(b0 + tid, len, keep), 0, s_sums, all);
         total += all.a;
     }
     int64_t before = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += kPlanBlock) {
+    for (int b0 = 0; b0 < a.batch; b0 += BLOCK) {
         const int b = b0 + tid;
         int32_t len, keep;
         TwoSums all;
         const int give = share(b, len, keep);
-        const TwoSums upto = scan_two(give, 0, s_sums, all);
+        const TwoSums upto = scan_two<BLOCK>(give, 0, s_sums, all);
+        if (a.batch <= BLOCK) total = all.a;
         s_upto[tid + 1] = (int32_t)upto.a;
         if (tid == 0) s_upto[0] = 0;
         s_keep[tid] = keep;
@@ -203,8 +210,8 @@ __global__ __launch_bounds__(kPlanBlock) void kv_release_kernel(PlanArgs a)
             if (give > 0) a.held[b] = keep;
         }
         __syncthreads();
-        for (int k = tid; k < (int)all.a; k += kPlanBlock) {
-            const int i = segment_of([&](int x) { return s_upto[x]; }, kPlanBlock, k);
+        for (int k = tid; k < (int)all.a; k += BLOCK) {
+            const int i = segment_of([&](int x) { return s_upto[x]; }, BLOCK, k);
             const int64_t to = count + total - 1 - (before + k);
             if (to < a.n_blocks)                 // (more blocks than there are: held or count is wrong)
                 a.free_blocks[to] = a.table[(int64_t)(b0 + i) * a.max_blocks + s_keep[i] + (k - s_upto[i])];
@@ -248,9 +255,10 @@ int log2_up(int64_t x) {
 
 hipError_t launch_kv_plan(const PlanArgs &a, hipStream_t s)
 {
-    const bool one = a.max_tokens <= kPlanOneLaunch;
-    if (one) hipLaunchKernelGGL(kv_plan_kernel<true>, dim3(1), dim3(kPlanBlock), 0, s, a);
-    else hipLaunchKernelGGL(kv_plan_kernel<false>, dim3(1), dim3(kPlanBlock), 0, s, a);
+    const bool one = a.max_tokens <= kPlanOneLaunch, small = a.batch <= kPlanSmall && a.max_tokens <= kPlanSmall;
+    if (small) hipLaunchKernelGGL((kv_plan_kernel<kPlanSmall, true>), dim3(1), dim3(kPlanSmall), 0, s, a);
+    else if (one) hipLaunchKernelGGL((kv_plan_kernel<kPlanLarge, true>), dim3(1), dim3(kPlanLarge), 0, s, a);
+    else hipLaunchKernelGGL((kv_plan_kernel<kPlanLarge, false>), dim3(1), dim3(kPlanLarge), 0, s, a);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess || one) return rc;
     hipLaunchKernelGGL(kv_plan_tokens_kernel, dim3((unsigned)(((int64_t)a.max_tokens + kMapBlock - 1) / kMapBlock)), dim3(kMapBlock), 0, s, a);
@@ -259,7 +267,8 @@ hipError_t launch_kv_plan(const PlanArgs &a, hipStream_t s)
 
 hipError_t launch_kv_release(const PlanArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(kv_release_kernel, dim3(1), dim3(kPlanBlock), 0, s, a);
+    if (a.batch <= kPlanSmall) hipLaunchKernelGGL(kv_release_kernel<kPlanSmall>, dim3(1), dim3(kPlanSmall), 0, s, a);
+    else hipLaunchKernelGGL(kv_release_kernel<kPlanLarge>, dim3(1), dim3(kPlanLarge), 0, s, a);
     return hipGetLastError();
 }
 

@@ -31,6 +31,15 @@ __device__ __forceinline__ double wave_sum64(double v) {
     return v;
 }
 
+__device__ __forceinline__ double wave_scan64(double v) {
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+        const double o = __shfl_up(v, step);
+        if ((int)threadIdx.x % kWave >= step) v += o;
+    }
+    return v;
+}
+
 // A probability as it counts: what is negative, infinite or NaN is 0.
 __device__ __forceinline__ float sane(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
 
@@ -133,6 +142,9 @@ __device__ __forceinline__ void four(const char *row, int i, int vocab, float *x
     for (int k = 0; k < 4; ++k) x[k] = i + k < vocab ? element<T>(row, i + k) : 0.f;
 }
 
+// The walk's last segment is drawn from by a whole workgroup: this many elements a lane.
+constexpr int kDrawPer = kVerifySegment / kWalkBlock;
+
 // What is left of the target at a node, by element.
 template <typename T>
 struct Rest {
@@ -165,6 +177,14 @@ struct Rest {
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[k] = i + k == t ? 0.0 : x[k];
         }
+    }
+    __device__ __forceinline__ double one(const Nodes &nodes, int i) const {
+        if (i >= vocab) return 0.0;
+        const double v = (double)element<T>(p, i);
+        if (q) return fmax(fma(-c, (double)element<T>(q, i), v), 0.0);
+        bool out = false;
+        for (uint64_t m = gone; m; m &= m - 1) out = out || i == __builtin_amdgcn_readlane(nodes.token, __builtin_ctzll(m));
+        return out ? 0.0 : v;
     }
     // sum of a segment, in every lane of the wave
     template <bool ALIGNED> __device__ __forceinline__ double segment(const Nodes &nodes, int seg) const {
@@ -210,6 +230,7 @@ template <typename T>
 __global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
 {
     __shared__ double s_sum[kWalkWaves];
+    __shared__ int s_hit[kWalkWaves], s_last[kWalkWaves];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, segs = segments_of(a);
     double *const sums = a.sums + (int64_t)b * segs;
     Nodes nodes;
@@ -259,64 +280,63 @@ __global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
         if (lane >= cnt) out[lane] = -1;
         if (lane == 0) a.cnt[b] = cnt;
     }
-    if (wave != 0) return;
-    // the draw, by one wave: the segment, then the element
-    int found = -1;
-    if (total > 0.0) {
-        const double t = (double)a.u_next[b] * total;
-        auto scan = [&](double v) {
-#pragma unroll
-            for (int step = 1; step < kWave; step *= 2) {
-                const double o = __shfl_up(v, step);
-                if (lane >= step) v += o;
-            }
-            return v;
-        };
-        double run = 0.0, before = 0.0;          // sum of what comes before the segment
-        int seg = -1;
-        for (int s0 = 0; s0 < segs; s0 += kWave) {
-            const double mine = s0 + lane < segs ? sums[s0 + lane] : 0.0, upto = run + scan(mine);
-            // the last segment that holds anything is the fallback where rounding leaves none
-            const uint64_t over = __ballot(upto > t && mine > 0.0), some = __ballot(mine > 0.0);
-            if (over) {
-                const int l = __builtin_ctzll(over);
-                seg = s0 + l;
-                before = __shfl(upto - mine, l);
-                break;
-            }
-            if (some) {
-                const int l = 63 - __builtin_clzll(some);
-                seg = s0 + l;
-                before = __shfl(upto - mine, l);
-            }
-            run = __shfl(upto, kWave - 1);
+    // The draw: the segment at which the running sum passes the threshold (every wave finds it), then the element, by the whole workgroup.
+    // Where rounding leaves none, the last one that holds anything.
+    if (!(total > 0.0)) {
+        if (tid == 0) a.next[b] = -1;
+        return;
+    }
+    const double t = (double)a.u_next[b] * total;
+    double run = 0.0, before = 0.0;              // sum of what comes before the segment
+    int seg = 0;
+    for (int s0 = 0; s0 < segs; s0 += kWave) {
+        const double mine = s0 + lane < segs ? sums[s0 + lane] : 0.0, upto = run + wave_scan64(mine);
+        const uint64_t over = __ballot(upto > t && mine > 0.0), some = __ballot(mine > 0.0);
+        const int l = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : -1;
+        if (l >= 0) {
+            seg = s0 + l;
+            before = __shfl(upto - mine, l);
         }
-        const Rest<T> rest(a, b, w);
-        for (int r = 0; r < kVerifySegment / (4 * kWave); ++r) {
-            const int i = seg * kVerifySegment + 4 * (r * kWave + lane);
-            double x[4];
-            if (rest.aligned) rest.template load<true>(nodes, i, x); else rest.template load<false>(nodes, i, x);
-            const double mine = (x[0] + x[1]) + (x[2] + x[3]), upto = scan(mine);
-            double at = before + (upto - mine);
-            int hit = -1, last = -1;             // the first over the threshold, the last that holds anything
+        if (over) break;
+        run = __shfl(upto, kWave - 1);
+    }
+    const Rest<T> rest(a, b, w);
+    const int first = seg * kVerifySegment + kDrawPer * tid;
+    double x[kDrawPer], mine = 0.0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                at += x[k];
-                if (x[k] > 0.0) {
-                    if (hit < 0 && at > t) hit = i + k;
-                    last = i + k;
-                }
-            }
-            const uint64_t over = __ballot(hit >= 0), some = __ballot(last >= 0);
-            if (over) {
-                found = __shfl(hit, __builtin_ctzll(over));
-                break;
-            }
-            if (some) found = __shfl(last, 63 - __builtin_clzll(some));
-            before += __shfl(upto, kWave - 1);
+    for (int k = 0; k < kDrawPer; ++k) mine += x[k] = rest.one(nodes, first + k);
+    const double upto = wave_scan64(mine);
+    __syncthreads();
+    if (lane == kWave - 1) s_sum[wave] = upto;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) before += s_sum[i];
+    before += upto - mine;
+    int hit = INT32_MAX, last = -1;              // the first over the threshold, the last that holds anything
+#pragma unroll
+    for (int k = 0; k < kDrawPer; ++k) {
+        before += x[k];
+        if (x[k] > 0.0) {
+            if (before > t) hit = min(hit, first + k);
+            last = first + k;
         }
     }
-    if (lane == 0) a.next[b] = found;
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2) {
+        hit = min(hit, __shfl_xor(hit, step));
+        last = max(last, __shfl_xor(last, step));
+    }
+    if (lane == 0) {
+        s_hit[wave] = hit;
+        s_last[wave] = last;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        for (int i = 0; i < kWalkWaves; ++i) {
+            hit = min(hit, s_hit[i]);
+            last = max(last, s_last[i]);
+        }
+        a.next[b] = hit != INT32_MAX ? hit : last;
+    }
 }
 
 }  // namespace
