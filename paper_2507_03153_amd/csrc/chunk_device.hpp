@@ -26,6 +26,9 @@ __device__ __forceinline__ int wave_max_int(int v) {
     return v;
 }
 
+// a value that all lanes have, in a scalar register
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
 // ---- the cut ----
 // A sequence of n tokens has u = ceil(n * group / kChunkRows) units, each over at most `steps` steps of its tokens.  Units are cut into shares
 // of at most C steps: s = ceil(steps / C) each.  C is at least kChunkLeast, and the least with which there are no more shares than the
@@ -239,54 +242,79 @@ struct GranuleRows {
 };
 
 // ---- scores ----
-// kPlainScores: what the softmax runs over is the product, times sm_scale log2 e in the exponent of 2.  kCapped: tanh(product * sm_scale / cap), times
-// cap log2 e.  kBiased: the score itself in units of ln 2, capped or not, less slope * distance.
+// kPlainScores: the softmax runs over the product, times sm_scale log2 e in the exponent of 2.  kCapped: cap tanh(product * sm_scale / cap), in
+// units of ln 2.  kBiased: the product less slope / sm_scale * distance, kCapped + kBiased: the capped score less slope * distance.
 enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
 
-// tanh x.  Up to kTanhNear it is x + x^3 P(x^2), P fitted to the least largest relative error (3.5e-7 with four terms, 1.5e-8 with
-// five); beyond, 1 - 2 / (1 + e^2x), whose rounding is then small against the result.
+// tanh x.  Up to kTanhNear it is x P(x^2), P fitted to the least largest relative error (3.0e-7 of degree 4, 1.4e-8 of degree 5); beyond, 1 - 2 / (1 +
+// e^2x), whose rounding is then small against the result.  The factors before and behind are in P's coefficients: six instructions a
+// score.  (Four more for the other form, two of them slow; steps in which no score is beyond are the rule.)
 constexpr float kTanhNear = 0.7f;
-template <bool FINE> __device__ __forceinline__ float tanh_near(float x) {
-    const float z = x * x;
-    const float p = FINE ? fmaf(z, fmaf(z, fmaf(z, fmaf(z, -0.00513866264f, 0.0200919714f), -0.0535588600f), 0.133291110f), -0.333331913f)
-                         : fmaf(z, fmaf(z, fmaf(z, 0.0139381709f, -0.0510163754f), 0.132876605f), -0.333310843f);
-    return fmaf(x * z, p, x);
-}
-template <bool FINE> __device__ __forceinline__ float tanh_any(float x) {
-    const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kTreeLog2e * fabsf(x))), 1.f);
-    return fabsf(x) <= kTanhNear ? tanh_near<FINE>(x) : copysignf(far, x);
+template <bool FINE> struct TanhNear {
+    static constexpr int kTerms = FINE ? 6 : 5;
+    float a[kTerms];
+    bool usable;                                 // the coefficients are ordinary numbers
+    __device__ __forceinline__ TanhNear() : usable(false) {}
+    __device__ __forceinline__ TanhNear(float in, float out) {   // of out * tanh(in * x)
+        constexpr float kFine[6] = {1.f, -0.33333131671f, 0.13328415155f, -0.05352601036f, 0.02002445795f, -0.00508833630f};
+        constexpr float kCoarse[6] = {0.99999970198f, -0.33330214024f, 0.13281112909f, -0.05083623528f, 0.01377371047f, 0.f};
+        float power = in * out;
+#pragma unroll
+        for (int i = 0; i < kTerms; ++i) {
+            a[i] = uniform((FINE ? kFine[i] : kCoarse[i]) * power);
+            power *= in * in;
+        }
+        usable = in >= 1e-4f && in <= 1e4f;      // (in^11 is one)
+    }
+    __device__ __forceinline__ float operator()(float x) const {
+        const float z = x * x;
+        float p = a[kTerms - 1];
+#pragma unroll
+        for (int i = kTerms - 2; i >= 0; --i) p = fmaf(z, p, a[i]);
+        return x * p;
+    }
+};
+__device__ __forceinline__ float tanh_far(float x) {
+    return copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kTreeLog2e * fabsf(x))), 1.f), x);
 }
 
 template <int MODE, bool FINE> struct ScoreMap {
+    static constexpr bool kCaps = (MODE & kCapped) != 0, kBiases = (MODE & kBiased) != 0;
     float k2;                                    // a weight is 2^(k2 * (what apply leaves) - its maximum's)
     float kx, scale2, cap2, slope2;
+    TanhNear<FINE> near_zero;
     __device__ __forceinline__ ScoreMap(const ChunkArgs &a, int head) {
-        scale2 = a.sh.sm_scale * kTreeLog2e;
-        kx = MODE == kPlainScores || a.cap <= 0.f ? 0.f : a.sh.sm_scale / a.cap;
-        cap2 = a.cap * kTreeLog2e;
-        slope2 = MODE == kBiased ? a.slopes[head] * kTreeLog2e : 0.f;
-        k2 = MODE == kPlainScores ? scale2 : MODE == kCapped ? cap2 : 1.f;
+        scale2 = uniform(a.sh.sm_scale * kTreeLog2e);
+        kx = kCaps ? uniform(a.sh.sm_scale / a.cap) : 0.f;
+        cap2 = uniform(a.cap * kTreeLog2e);
+        slope2 = kBiases ? a.slopes[head] * (kCaps ? kTreeLog2e : 1.f / a.sh.sm_scale) : 0.f;
+        k2 = kCaps ? 1.f : scale2;
+        if (kCaps) near_zero = TanhNear<FINE>(kx, cap2);
     }
     // The N values of a lane, get(i) and set(i, x): products with tokens first + off(i) of a row at position pos.
     template <int N, typename Get, typename Set, typename Off>
     __device__ __forceinline__ void each(Get get, Set set, Off off, int pos, int first) const {
         if constexpr (MODE == kPlainScores) return;
         const float d = (float)(pos - first);
-        auto biased = [&](float x, float factor, int i) { return fmaf(-slope2, fabsf(d - (float)off(i)), x * factor); };
-        if (MODE == kBiased && kx == 0.f) {      // uniform over the launch
+        auto biased = [&](float x, int i) { return kBiases ? fmaf(-slope2, fabsf(d - (float)off(i)), x) : x; };
+        if constexpr (!kCaps) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) set(i, biased(get(i), scale2, i));
+            for (int i = 0; i < N; ++i) set(i, biased(get(i), i));
             return;
-        }
-        float most = 0.f;
+        } else {
+            float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(get(i)));
-        const bool near = !any_lane(!(most * kx <= kTanhNear));
+            for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(get(i)));
+            if (near_zero.usable && !any_lane(!(most * kx <= kTanhNear))) {          // uniform over the wave
 #pragma unroll
-        for (int i = 0; i < N; ++i) set(i, near ? tanh_near<FINE>(get(i) * kx) : tanh_any<FINE>(get(i) * kx));
-        if constexpr (MODE == kBiased) {
+                for (int i = 0; i < N; ++i) set(i, biased(near_zero(get(i)), i));
+            } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) set(i, biased(get(i), cap2, i));
+                for (int i = 0; i < N; ++i) {
+                    const float x = get(i) * kx;
+                    set(i, biased(near_zero.usable && fabsf(x) <= kTanhNear ? near_zero(get(i)) : cap2 * tanh_far(x), i));
+                }
+            }
         }
     }
     // c[t][r]: token first + 32 t + 8 (r / 4) + r % 4

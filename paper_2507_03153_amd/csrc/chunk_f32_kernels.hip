@@ -171,12 +171,13 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
 hipError_t launch_chunk_rows_f32(int head_dim, const ChunkArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((int64_t)a.slots * a.sh.n_kv_heads)), block(kChunkBlock);
-    const int mode = a.slopes ? kBiased : a.cap > 0.f ? kCapped : kPlainScores;
+    const int mode = (a.slopes ? kBiased : 0) + (a.cap > 0.f ? kCapped : 0);
 #define HGCA_CHUNK(D)                                                                                                \
     do {                                                                                                             \
         if (mode == kPlainScores) hipLaunchKernelGGL((chunk_attn_f32_kernel<D, kPlainScores>), grid, block, 0, s, a); \
         else if (mode == kCapped) hipLaunchKernelGGL((chunk_attn_f32_kernel<D, kCapped>), grid, block, 0, s, a);     \
-        else hipLaunchKernelGGL((chunk_attn_f32_kernel<D, kBiased>), grid, block, 0, s, a);                          \
+        else if (mode == kBiased) hipLaunchKernelGGL((chunk_attn_f32_kernel<D, kBiased>), grid, block, 0, s, a);     \
+        else hipLaunchKernelGGL((chunk_attn_f32_kernel<D, kCapped + kBiased>), grid, block, 0, s, a);                \
     } while (0)
     if (head_dim == 64) HGCA_CHUNK(64);
     else HGCA_CHUNK(128);

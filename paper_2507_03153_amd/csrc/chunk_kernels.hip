@@ -404,12 +404,13 @@ __global__ __launch_bounds__(kChunkFoldRows * D / 4) void chunk_fold_kernel(Chun
 hipError_t launch_chunk_rows_bf16(int head_dim, const ChunkArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((int64_t)a.slots * a.sh.n_kv_heads)), block(kChunkBlock);
-    const int mode = a.slopes ? kBiased : a.cap > 0.f ? kCapped : kPlainScores;
+    const int mode = (a.slopes ? kBiased : 0) + (a.cap > 0.f ? kCapped : 0);
 #define HGCA_CHUNK(D, PP)                                                                                          \
     do {                                                                                                           \
         if (mode == kPlainScores) hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kPlainScores>), grid, block, 0, s, a); \
         else if (mode == kCapped) hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kCapped>), grid, block, 0, s, a);   \
-        else hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kBiased>), grid, block, 0, s, a);                        \
+        else if (mode == kBiased) hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kBiased>), grid, block, 0, s, a);   \
+        else hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kCapped + kBiased>), grid, block, 0, s, a);              \
     } while (0)
     if (head_dim == 64 && a.o_bf16) HGCA_CHUNK(64, 1);
     else if (head_dim == 64) HGCA_CHUNK(64, 3);

@@ -1869,6 +1869,7 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
     if ((rc = check_view(shape, tier, true)) != HGCA_OK) return rc;
     if (n_tokens < 0 || (flags & ~HGCA_CHUNK_CAUSAL) || window < 0 || !(softcap >= 0.f) || softcap > 2.0e38f) return HGCA_ERR_INVALID_ARG;
     if (!(shape->sm_scale > 0.f) || shape->sm_scale > 2.0e38f) return HGCA_ERR_INVALID_ARG;
+    if (slopes && shape->sm_scale < 1e-30f) return HGCA_ERR_UNSUPPORTED;         // (slopes are divided by it)
     if (softcap > 0.f && !(shape->sm_scale / softcap > 0.f && shape->sm_scale / softcap < 2.0e38f)) return HGCA_ERR_INVALID_ARG;
     if (tier->cap > kMaxRowsCap || (o_dtype != HGCA_F32 && o_dtype != HGCA_BF16)) return HGCA_ERR_UNSUPPORTED;
     if (shape->batch == 0 || n_tokens == 0) return HGCA_OK;
