@@ -41,7 +41,7 @@ __device__ __forceinline__ double wave_scan64(double v) {
 }
 
 // A probability as it counts: what is negative, infinite or NaN is 0.
-__device__ __forceinline__ float sane(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
+__device__ __forceinline__ float sane(float x) { return __float_as_uint(x) < 0x7f800000u ? x : 0.f; }
 
 template <typename T> __device__ __forceinline__ float element(const char *row, int i);
 template <> __device__ __forceinline__ float element<float>(const char *row, int i) { return sane(reinterpret_cast<const float *>(row)[i]); }
@@ -122,25 +122,24 @@ __device__ __forceinline__ bool walk_on(Walk &w, const Nodes &nodes, bool with_q
     }
 }
 
-// max(p - c q, 0) of 4 adjacent elements from i on (those behind the end: 0); the row begins at an address of any alignment.
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ void four(const char *row, int i, int vocab, float *x) {
-    if (ALIGNED && i + 4 <= vocab) {
-        if (sizeof(T) == 4) {
-            const float4 v = *reinterpret_cast<const float4 *>(row + 4 * (int64_t)i);
-            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-        } else {
-            const uint2 v = *reinterpret_cast<const uint2 *>(row + 2 * (int64_t)i);
-            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
-            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
+// 16 bytes of a row as elements.
+template <typename T> struct Piece {
+    static constexpr int kPer = Elem<T>::kPerLoad;
+    uint4 raw;
+    __device__ __forceinline__ void load(const char *row, int i) { raw = load16(row + (int64_t)i * (int)sizeof(T)); }
+    __device__ __forceinline__ void expand(float *x) const { Elem<T>::expand(raw, x); }
+    // below kAllSane if every element counts as it is: neither negative nor infinite or NaN
+    __device__ __forceinline__ uint32_t look(uint32_t so_far) const {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            so_far = max(so_far, w[k]);
+            if (sizeof(T) == 2) so_far = max(so_far, w[k] << 16);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = sane(x[k]);
-        return;
+        return so_far;
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = i + k < vocab ? element<T>(row, i + k) : 0.f;
-}
+};
+constexpr uint32_t kAllSane = 0x7f800000u;       // the bits of infinity; those of negative numbers and NaN are above
 
 // The walk's last segment is drawn from by a whole workgroup: this many elements a lane.
 constexpr int kDrawPer = kVerifySegment / kWalkBlock;
@@ -152,54 +151,84 @@ struct Rest {
     double c;
     uint64_t gone;
     int vocab;
-    bool aligned;                                // both rows begin at 4 elements' alignment
+    bool aligned;                                // both rows begin at 16 bytes' alignment
     __device__ __forceinline__ Rest(const VerifyArgs &a, int b, const Walk &w) {
         p = Nodes::target_row(a, b, w.node, sizeof(T));
         q = a.draft && w.c > 0.0 ? Nodes::draft_row(a, b, w.node, sizeof(T)) : nullptr;
         c = w.c;
         gone = a.draft ? 0 : w.gone;
         vocab = a.vocab;
-        aligned = ((uintptr_t)p | (uintptr_t)q) % (4 * sizeof(T)) == 0;
-    }
-    template <bool ALIGNED> __device__ __forceinline__ void load(const Nodes &nodes, int i, double *x) const {
-        float v[4], d[4];
-        four<T, ALIGNED>(p, i, vocab, v);
-        if (q) {
-            four<T, ALIGNED>(q, i, vocab, d);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = fmax(fma(-c, (double)d[k], (double)v[k]), 0.0);
-            return;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = (double)v[k];
-        for (uint64_t m = gone; m; m &= m - 1) { // (uniform over the wave)
-            const int t = __builtin_amdgcn_readlane(nodes.token, __builtin_ctzll(m));
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = i + k == t ? 0.0 : x[k];
-        }
+        aligned = ((uintptr_t)p | (uintptr_t)q) % 16 == 0;
     }
     __device__ __forceinline__ double one(const Nodes &nodes, int i) const {
         if (i >= vocab) return 0.0;
-        const double v = (double)element<T>(p, i);
-        if (q) return fmax(fma(-c, (double)element<T>(q, i), v), 0.0);
+        return gone ? left<true>(nodes, element<T>(p, i), 0.f, i) : left<false>(nodes, element<T>(p, i), q ? element<T>(q, i) : 0.f, i);
+    }
+    template <bool GONE> __device__ __forceinline__ double left(const Nodes &nodes, float v, float d, int i) const {
+        if constexpr (!GONE) {
+            double x = fma(-c, (double)d, (double)v);
+            asm("v_max_f64 %0, %0, 0" : "+v"(x));                // (the compiler's has two more for signalling NaN)
+            return x;
+        }
         bool out = false;
         for (uint64_t m = gone; m; m &= m - 1) out = out || i == __builtin_amdgcn_readlane(nodes.token, __builtin_ctzll(m));
-        return out ? 0.0 : v;
+        return out ? 0.0 : (double)v;
     }
-    // sum of a segment, in every lane of the wave
-    template <bool ALIGNED> __device__ __forceinline__ double segment(const Nodes &nodes, int seg) const {
-        constexpr int kRounds = kVerifySegment / (4 * kWave);
-        double s[kRounds];
+    // Sum of a segment, in every lane of the wave.  All of the lane's loads are under way before the first is waited for: a wave has a segment to
+    // itself, and one load after the other would take eight times memory's latency (a pass of one workgroup over 128 000 elements 17 us).
+    __device__ __forceinline__ double segment(const Nodes &nodes, int seg) const {
+        return gone ? segment_of<true>(nodes, seg) : segment_of<false>(nodes, seg);
+    }
+    template <bool GONE> __device__ __forceinline__ double segment_of(const Nodes &nodes, int seg) const {
+        const int lane = threadIdx.x % kWave, first = seg * kVerifySegment;
+        double s[4] = {0.0, 0.0, 0.0, 0.0};
+        bool done = false;
+        if (aligned && first + kVerifySegment <= vocab) {        // uniform over the wave
+            constexpr int kPer = Piece<T>::kPer, kRounds = kVerifySegment / (kPer * kWave);
+            Piece<T> pv[kRounds], pd[kRounds];
+            const int i0 = first + kPer * lane;
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
-            double x[4];
-            load<ALIGNED>(nodes, seg * kVerifySegment + 4 * (r * kWave + (int)threadIdx.x % kWave), x);
-            s[r] = (x[0] + x[1]) + (x[2] + x[3]);
+            for (int r = 0; r < kRounds; ++r) pv[r].load(p, i0 + r * kPer * kWave);
+            if (q) {
+#pragma unroll
+                for (int r = 0; r < kRounds; ++r) pd[r].load(q, i0 + r * kPer * kWave);
+            } else {
+#pragma unroll
+                for (int r = 0; r < kRounds; ++r) pd[r].raw = make_uint4(0, 0, 0, 0);
+            }
+            uint32_t most = 0;
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) most = pd[r].look(pv[r].look(most));
+            if (__builtin_amdgcn_ballot_w64(most >= kAllSane) == 0) {            // else element by element
+                done = true;
+#pragma unroll
+                for (int r = 0; r < kRounds; ++r) {
+                    float v[kPer], d[kPer];
+                    pv[r].expand(v);
+                    pd[r].expand(d);
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) s[k % 4] += left<GONE>(nodes, v[k], d[k], i0 + r * kPer * kWave + k);
+                }
+            }
         }
-        double sum = s[0];
+        if (!done) {                             // rows of any alignment, the last segment
+            constexpr int kRounds = 16;
+            for (int i0 = first + lane; i0 < first + kVerifySegment; i0 += kRounds * kWave) {
+                float v[kRounds], d[kRounds];
 #pragma unroll
-        for (int r = 1; r < kRounds; ++r) sum += s[r];
-        return wave_sum64(sum);
+                for (int r = 0; r < kRounds; ++r) {
+                    const int i = min(i0 + r * kWave, vocab - 1);
+                    v[r] = element<T>(p, i);
+                    d[r] = q ? element<T>(q, i) : 0.f;
+                }
+#pragma unroll
+                for (int r = 0; r < kRounds; ++r) {
+                    const int i = i0 + r * kWave;
+                    s[r % 4] += i < vocab ? left<GONE>(nodes, v[r], d[r], i) : 0.0;
+                }
+            }
+        }
+        return wave_sum64((s[0] + s[1]) + (s[2] + s[3]));
     }
 };
 
@@ -222,7 +251,7 @@ __global__ __launch_bounds__(kSumBlock) void verify_sums_kernel(VerifyArgs a)
     walk_first<T>(a, b, nodes, w);
     if (seg >= segs) return;
     const Rest<T> rest(a, b, w);
-    const double sum = rest.aligned ? rest.template segment<true>(nodes, seg) : rest.template segment<false>(nodes, seg);
+    const double sum = rest.segment(nodes, seg);
     if (threadIdx.x % kWave == 0) a.sums[(int64_t)b * segs + seg] = sum;
 }
 
@@ -253,7 +282,7 @@ __global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
         const Rest<T> rest(a, b, w);
         __syncthreads();                         // nobody reads the old sums any more
         for (int seg = wave; seg < segs; seg += kWalkWaves) {
-            const double sum = rest.aligned ? rest.template segment<true>(nodes, seg) : rest.template segment<false>(nodes, seg);
+            const double sum = rest.segment(nodes, seg);
             if (lane == 0) sums[seg] = sum;
         }
         __syncthreads();
