@@ -146,6 +146,7 @@ struct Place {
 // ---- what a row sees ----
 struct RowSees {
     int lo, hi, pre;                             // tokens [0, pre) and [lo, hi)
+    RowSees() = default;
     __device__ __forceinline__ RowSees(const ChunkArgs &a, const SeqWork &q, int query) {
         const int p = q.len - q.nq + query;
         pre = q.pre;
@@ -166,13 +167,22 @@ struct RowSees {
 // What the rows of a wave see together: everything in [0, pre) and [all_lo, all_hi), nothing outside [0, pre) and [any_lo, any_hi).
 struct WaveSees {
     int pre, all_lo, all_hi, any_lo, any_hi;
-    __device__ __forceinline__ WaveSees(const RowSees &r) {
-        pre = r.pre;
-        const bool some = r.hi > r.lo;
-        all_lo = __builtin_amdgcn_readfirstlane(wave_max_int(r.lo));
-        all_hi = __builtin_amdgcn_readfirstlane(wave_min_int(r.hi));
-        any_lo = __builtin_amdgcn_readfirstlane(wave_min_int(some ? r.lo : INT32_MAX));
-        any_hi = __builtin_amdgcn_readfirstlane(wave_max_int(some ? r.hi : 0));
+    template <int N> __device__ __forceinline__ explicit WaveSees(const RowSees (&rows)[N]) {     // a lane's N rows
+        pre = rows[0].pre;
+        all_lo = 0, all_hi = INT32_MAX, any_lo = INT32_MAX, any_hi = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            all_lo = max(all_lo, rows[i].lo);
+            all_hi = min(all_hi, rows[i].hi);
+            if (rows[i].hi > rows[i].lo) {
+                any_lo = min(any_lo, rows[i].lo);
+                any_hi = max(any_hi, rows[i].hi);
+            }
+        }
+        all_lo = __builtin_amdgcn_readfirstlane(wave_max_int(all_lo));
+        all_hi = __builtin_amdgcn_readfirstlane(wave_min_int(all_hi));
+        any_lo = __builtin_amdgcn_readfirstlane(wave_min_int(any_lo));
+        any_hi = __builtin_amdgcn_readfirstlane(wave_max_int(any_hi));
     }
     __device__ __forceinline__ bool all(int t, int n) const { return t + n <= pre || (t >= all_lo && t + n <= all_hi); }
     __device__ __forceinline__ bool none(int t, int n) const { return t >= pre && (t >= any_hi || t + n <= any_lo); }
@@ -283,11 +293,16 @@ template <int MODE, bool FINE> struct ScoreMap {
     float k2;                                    // a weight is 2^(k2 * (what apply leaves) - its maximum's)
     float kx, scale2, cap2, slope2;
     TanhNear<FINE> near_zero;
-    __device__ __forceinline__ ScoreMap(const ChunkArgs &a, int head) {
+    static __device__ __forceinline__ float slope_of(const ChunkArgs &a, int head) {
+        return kBiases ? a.slopes[head] * (kCaps ? kTreeLog2e : 1.f / a.sh.sm_scale) : 0.f;
+    }
+    // (slope2 is the row's: set, where there are several)
+    __device__ __forceinline__ ScoreMap(const ChunkArgs &a, int head) : ScoreMap(a) { slope2 = slope_of(a, head); }
+    __device__ __forceinline__ explicit ScoreMap(const ChunkArgs &a) {
+        slope2 = 0.f;
         scale2 = uniform(a.sh.sm_scale * kTreeLog2e);
         kx = kCaps ? uniform(a.sh.sm_scale / a.cap) : 0.f;
         cap2 = uniform(a.cap * kTreeLog2e);
-        slope2 = kBiases ? a.slopes[head] * (kCaps ? kTreeLog2e : 1.f / a.sh.sm_scale) : 0.f;
         k2 = kCaps ? 1.f : scale2;
         if (kCaps) near_zero = TanhNear<FINE>(kx, cap2);
     }

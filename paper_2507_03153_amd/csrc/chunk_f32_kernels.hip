@@ -66,15 +66,17 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
     seq.unify();
     const int lane = threadIdx.x % kWave, w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 32, hw = lane / 32;
     const RowPlace rp(a, seq, at.unit, kvh, 32 * w + n);
-    const RowSees sees(a, seq, rp.query);
-    const WaveSees wave(sees);
+    const RowSees sees(a, seq, rp.query), all_sees[1] = {sees};
+    const WaveSees wave(all_sees);
     int lo, hi;
     unit_range(wave, s_range, lo, hi);
     const Steps steps(seq.pre, lo, hi, at.share, at.n_shares);
-    if (((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows <= kFewRows) {      // uniform over the workgroup
+    const int64_t unit_rows = ((int64_t)seq.nq << __builtin_ctz(a.sh.group)) - (int64_t)at.unit * kChunkRows;
+    if (unit_rows <= kFewRows) {                 // uniform over the workgroup
         FewShared<D> &few = *reinterpret_cast<FewShared<D> *>(s_kv);
         static_assert(sizeof(FewShared<D>) <= sizeof(s_kv), "the waves' results lie in the stages");
-        few_rows_f32<D, MODE>(few, s_row, a, at, seq, steps, kvh);
+        if (unit_rows <= kFewTile) few_rows_f32<D, MODE, 1>(few, s_row, a, at, seq, steps, kvh);
+        else few_rows_f32<D, MODE, 2>(few, s_row, a, at, seq, steps, kvh);
         return;
     }
     const bool wave_live = any_lane(rp.live);       // uniform over the wave

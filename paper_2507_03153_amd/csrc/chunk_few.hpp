@@ -1,8 +1,9 @@
-// Units of up to 16 rows of a chunk call (a token's heads, a few tokens): a wave is the 16 rows against tokens of its own at a time, straight from
-// memory to the operands of 16 x 16 tiles, the next ones requested while these are worked on; the workgroup's four waves take turns
-// and join what they found at the end.  Nothing waits at a barrier, and the arithmetic is a quarter of the 32 x 32 tiles' or less.
+// Units of up to 16 rows of a chunk call (a token's heads, a few tokens), in fp32 of up to 32: a wave is the 16 rows (RT = 1) or 32 (RT = 2) against
+// tokens of its own at a time, straight from memory to the operands of 16 x 16 tiles, the next ones requested while these are worked on; the workgroup's four
+// waves take turns and join what they found at the end.  Nothing waits at a barrier, all four waves work, and 16 rows take a quarter of
+// the 32 x 32 tiles' arithmetic.
 //   S^T[token, row] = K . Q^T,  O^T[col, row] += V^T . P^T,
-// lane n + 16 g has row n in both: scores of tokens 4 g .. 4 g + 3 of a tile of 16, and columns e of E = D / 16 adjacent ones, product e, at
+// lane n + 16 g has row n of a tile in both: scores of tokens 4 g .. 4 g + 3 of a tile of 16, and columns e of E = D / 16 adjacent ones, product e, at
 // E m + e with m = 4 g + i.
 #pragma once
 
@@ -12,7 +13,7 @@ namespace hgca {
 
 namespace {
 
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 32, kFewTile = 16;
 
 __device__ __forceinline__ floatx4 few_mfma(const uint4 &a, const uint4 &b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -27,7 +28,7 @@ __device__ __forceinline__ float few_max(float x) {
 // The waves' results on their way to one.
 template <int D> struct FewShared {
     float m[kChunkWaves][kFewRows], l[kChunkWaves][kFewRows];
-    float o[kChunkWaves][kFewRows][D + 4];
+    float o[kChunkWaves][kFewTile][D + 4];       // a tile at a time
     int odd[kChunkWaves];
     OddTokens<D> notes;
 };
@@ -71,95 +72,105 @@ template <int E> struct FewState {
     }
 };
 
-// What the waves found becomes one result per row.  The unit's row r is lane group r of the workgroup, 16 lanes with E columns each.
-template <typename T, int D>
+// What the waves found becomes one result per row, a tile of 16 at a time: its row r is lane group r of the workgroup, 16 lanes with E columns each.
+template <typename T, int D, int RT>
 __device__ __forceinline__ void few_join(FewShared<D> &sh, const ChunkArgs &a, const Place &at, const SeqWork &seq, const Steps &steps, int kvh,
-                                         FewState<D / 16> &st, float k2, bool odd)
+                                         FewState<D / 16> (&st)[RT], float k2, bool odd)
 {
     constexpr int E = D / 16;
     const int tid = threadIdx.x, w = tid / kWave, lane = tid % kWave, n = lane % 16, g = lane / 16;
-    const float lw = strided_sum<16>(st.l);
-    if (g == 0) {
-        sh.m[w][n] = lw == 0.f ? -INFINITY : -shift_of(st.m, k2);
-        sh.l[w][n] = lw;
-    }
     float z[4] = {0.f, 0.f, 0.f, 0.f};           // NaN where a sum is not finite
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int t = 0; t < RT; ++t) {
+        const float lw = strided_sum<16>(st[t].l);
+        if (g == 0) {
+            sh.m[w][kFewTile * t + n] = lw == 0.f ? -INFINITY : -shift_of(st[t].m, k2);
+            sh.l[w][kFewTile * t + n] = lw;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = fmaf(st.o[e][i], 0.f, z[i]);
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = fmaf(st[t].o[e][i], 0.f, z[i]);
+    }
     const float all = (z[0] + z[1]) + (z[2] + z[3]);
     odd = any_lane(all != all || odd);
     if (lane == 0) sh.odd[w] = odd;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int t = 0; t < RT; ++t) {
+        if (t > 0) __syncthreads();              // the tile before has been read
 #pragma unroll
-        for (int e = 0; e < E; e += 4)
-            *reinterpret_cast<float4 *>(&sh.o[w][n][(4 * g + i) * E + e]) = make_float4(st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]);
-    __syncthreads();
-    const int r = tid / 16, c = tid % 16;
-    const RowPlace rp(a, seq, at.unit, kvh, r);
-    float M = -INFINITY, L = 0.f, x[E];
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < kChunkWaves; ++i) M = fmaxf(M, sh.m[i][r]);
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<float4 *>(&sh.o[w][n][(4 * g + i) * E + e]) =
+                    make_float4(st[t].o[e][i], st[t].o[e + 1][i], st[t].o[e + 2][i], st[t].o[e + 3][i]);
+        __syncthreads();
+        const int r = tid / 16, c = tid % 16, row = kFewTile * t + r;
+        const RowPlace rp(a, seq, at.unit, kvh, row);
+        float M = -INFINITY, L = 0.f, x[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.f;
+        for (int i = 0; i < kChunkWaves; ++i) M = fmaxf(M, sh.m[i][row]);
 #pragma unroll
-    for (int i = 0; i < kChunkWaves; ++i) {
-        const float m = sh.m[i][r];
-        if (m == -INFINITY) continue;            // the wave saw nothing of the row
-        const float f = __builtin_amdgcn_exp2f(m - M);
-        L = fmaf(sh.l[i][r], f, L);
+        for (int e = 0; e < E; ++e) x[e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            const float4 o = *reinterpret_cast<const float4 *>(&sh.o[i][r][c * E + e]);
-            x[e] = fmaf(o.x, f, x[e]);
-            x[e + 1] = fmaf(o.y, f, x[e + 1]);
-            x[e + 2] = fmaf(o.z, f, x[e + 2]);
-            x[e + 3] = fmaf(o.w, f, x[e + 3]);
-        }
-    }
-    bool any = false;
+        for (int i = 0; i < kChunkWaves; ++i) {
+            const float m = sh.m[i][row];
+            if (m == -INFINITY) continue;        // the wave saw nothing of the row
+            const float f = __builtin_amdgcn_exp2f(m - M);
+            L = fmaf(sh.l[i][row], f, L);
 #pragma unroll
-    for (int i = 0; i < kChunkWaves; ++i) any = any || sh.odd[i];
-    if (any) {                                   // uniform over the workgroup
-        const RowSees sees(a, seq, rp.query);
-        uint32_t kinds[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) kinds[e] = 0;
-        for (int part = 0; part < 2; ++part)
-            for (int s = steps.begin(part); s < steps.end(part); ++s) {
-                sh.notes.template note<T>(a, at.b, kvh, s * kChunkStep, seq.len);
-                const uint64_t seen = sees.mask(s * kChunkStep);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) kinds[e] |= sh.notes.bits[k][c * E + e] & seen ? 1u << k : 0u;
+            for (int e = 0; e < E; e += 4) {
+                const float4 o = *reinterpret_cast<const float4 *>(&sh.o[i][r][c * E + e]);
+                x[e] = fmaf(o.x, f, x[e]);
+                x[e + 1] = fmaf(o.y, f, x[e + 1]);
+                x[e + 2] = fmaf(o.z, f, x[e + 2]);
+                x[e + 3] = fmaf(o.w, f, x[e + 3]);
             }
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = kinds[e] == 0 ? x[e] : kinds[e] == 1 ? INFINITY : kinds[e] == 2 ? -INFINITY : NAN;
-    }
-    if (!rp.live) return;
-    auto store = [&](auto four) {
-#pragma unroll
-        for (int e = 0; e < E; e += 4) four(c * E + e, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
-    };
-    if (at.n_shares > 1) {
-        const int64_t to = ((int64_t)(at.part + at.share) * a.sh.n_kv_heads + kvh) * kChunkRows + r;
-        store([&](int col, const float4 &y) { *reinterpret_cast<float4 *>(a.part_o + to * D + col) = y; });
-        if (c == 0) {
-            a.part_m[to] = M;
-            a.part_l[to] = L;
         }
-        return;
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kChunkWaves; ++i) any = any || sh.odd[i];
+        if (any) {                               // uniform over the workgroup
+            const RowSees sees(a, seq, rp.query);
+            uint32_t kinds[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) kinds[e] = 0;
+            for (int part = 0; part < 2; ++part)
+                for (int s = steps.begin(part); s < steps.end(part); ++s) {
+                    sh.notes.template note<T>(a, at.b, kvh, s * kChunkStep, seq.len);
+                    const uint64_t seen = sees.mask(s * kChunkStep);
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) kinds[e] |= sh.notes.bits[k][c * E + e] & seen ? 1u << k : 0u;
+                }
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = kinds[e] == 0 ? x[e] : kinds[e] == 1 ? INFINITY : kinds[e] == 2 ? -INFINITY : NAN;
+        }
+        if (!rp.live) continue;                  // (barriers are reached by all: the loop is unrolled and uniform)
+        auto store = [&](auto four) {
+#pragma unroll
+            for (int e = 0; e < E; e += 4) four(c * E + e, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
+        };
+        if (at.n_shares > 1) {
+            const int64_t to = ((int64_t)(at.part + at.share) * a.sh.n_kv_heads + kvh) * kChunkRows + row;
+            store([&](int col, const float4 &y) { *reinterpret_cast<float4 *>(a.part_o + to * D + col) = y; });
+            if (c == 0) {
+                a.part_m[to] = M;
+                a.part_l[to] = L;
+            }
+            continue;
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        store([&](int col, const float4 &y) {
+            const float4 v = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+            if (a.o_bf16)
+                *reinterpret_cast<uint2 *>(static_cast<char *>(a.o) + 2 * (rp.out * D + col)) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            else
+                *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + rp.out * D + col) = v;
+        });
+        if (c == 0) a.lse[rp.out] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    store([&](int col, const float4 &y) {
-        const float4 v = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
-        if (a.o_bf16) *reinterpret_cast<uint2 *>(static_cast<char *>(a.o) + 2 * (rp.out * D + col)) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-        else *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + rp.out * D + col) = v;
-    });
-    if (c == 0) a.lse[rp.out] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }
 
 // What both types' loops go through: the share in passes that the table of a paged tier covers; of every kChunkWaves * kTokens tokens a wave takes
@@ -192,24 +203,31 @@ __device__ __forceinline__ void few_tokens(uint32_t *s_row, const ChunkArgs &a, 
 
 constexpr uint32_t kFewLow = 0x05040100u, kFewHigh = 0x07060302u;                // byte selectors: (b.lo, a.lo) and (b.hi, a.hi)
 
-// bf16: 32 tokens of a wave at a time.  V needs tokens side by side where rows have columns side by side: pairs of tokens are put together by
+// bf16: one tile of 16 rows and 32 tokens of a wave at a time.  V needs tokens side by side where rows have columns side by side: pairs of tokens are put together by
 // byte permutations.
 template <int D, int PP, int MODE>
 __device__ __forceinline__ void few_rows_bf16(FewShared<D> &sh, uint32_t *s_row, const ChunkArgs &a, const Place &at, const SeqWork &seq,
                                               const Steps &steps, int kvh)
 {
-    constexpr int KS = D / 32, E = D / 16, W = E / 2;
+    constexpr int KS = D / 32, E = D / 16, W = E / 2, RT = 1;
     const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
-    const RowPlace rp(a, seq, at.unit, kvh, n);
-    uint4 q[KS];
-    const char *const qp = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * (2 * D) + 16 * g;
+    uint4 q[RT][KS];
+    RowSees sees[RT];
+    int pos[RT];
+    float slope[RT];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) q[s] = load16(qp + 64 * s);
-    const RowSees sees(a, seq, rp.query);
+    for (int r = 0; r < RT; ++r) {
+        const RowPlace rp(a, seq, at.unit, kvh, kFewTile * r + n);
+        const char *const qp = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * (2 * D) + 16 * g;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[r][s] = load16(qp + 64 * s);
+        sees[r] = RowSees(a, seq, rp.query);
+        pos[r] = seq.len - seq.nq + rp.query;
+        slope[r] = ScoreMap<MODE, PP != 1>::slope_of(a, rp.head);
+    }
     const WaveSees wave(sees);
-    const ScoreMap<MODE, PP != 1> map(a, rp.head);
-    const int pos = seq.len - seq.nq + rp.query;
-    FewState<E> st;
+    ScoreMap<MODE, PP != 1> map(a);
+    FewState<E> st[RT];
     bool met_odd = false;                        // of the lane
     uint4 k[2][KS];
     uint32_t v[2][4][W];
@@ -241,33 +259,41 @@ __device__ __forceinline__ void few_rows_bf16(FewShared<D> &sh, uint32_t *s_row,
         }
     };
     auto use = [&](int tok, auto next) {
-        floatx4 s[2] = {floatx4{}, floatx4{}};
+        floatx4 s[RT][2];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) s[r][0] = s[r][1] = floatx4{};
 #pragma unroll
         for (int i = 0; i < KS; ++i)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) s[t] = few_mfma(k[t][i], q[i], s[t]);
-        next(fetch_k);
-        map.template each<8>([&](int i) { return s[i / 4][i % 4]; }, [&](int i, float x) { s[i / 4][i % 4] = x; },
-                             [](int i) { return 16 * (i / 4) + i % 4; }, pos, tok + 4 * g);
-        const bool masked = !wave.all(tok, 32);
-        if (masked) {
-            const uint32_t seen = (uint32_t)sees.mask(tok + 4 * g);
-#pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!(seen >> (16 * t + i) & 1u)) s[t][i] = -INFINITY;
-        }
-        st.weigh(s, map.k2);
-        uint32_t part[PP][4];
+                for (int r = 0; r < RT; ++r) s[r][t] = few_mfma(k[t][i], q[r][i], s[r][t]);
+        next(fetch_k);
+        const bool masked = !wave.all(tok, 32);
+        uint32_t part[RT][PP][4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            float x0 = s[c / 2][2 * (c % 2)], x1 = s[c / 2][2 * (c % 2) + 1];
+        for (int r = 0; r < RT; ++r) {
+            map.slope2 = slope[r];
+            map.template each<8>([&](int i) { return s[r][i / 4][i % 4]; }, [&](int i, float x) { s[r][i / 4][i % 4] = x; },
+                                 [](int i) { return 16 * (i / 4) + i % 4; }, pos[r], tok + 4 * g);
+            if (masked) {
+                const uint32_t seen = (uint32_t)sees[r].mask(tok + 4 * g);
 #pragma unroll
-            for (int t = 0; t < PP; ++t) {
-                part[t][c] = pack_bf16(x0, x1);
-                x0 -= __uint_as_float(part[t][c] << 16);
-                x1 -= __uint_as_float(part[t][c] & 0xffff0000u);
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(seen >> (16 * t + i) & 1u)) s[r][t][i] = -INFINITY;
+            }
+            st[r].weigh(s[r], map.k2);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float x0 = s[r][c / 2][2 * (c % 2)], x1 = s[r][c / 2][2 * (c % 2) + 1];
+#pragma unroll
+                for (int t = 0; t < PP; ++t) {
+                    part[r][t][c] = pack_bf16(x0, x1);
+                    x0 -= __uint_as_float(part[r][t][c] << 16);
+                    x1 -= __uint_as_float(part[r][t][c] & 0xffff0000u);
+                }
             }
         }
         if (masked) {                            // infinities and NaN are taken out (few_join brings them to the rows that see them)
@@ -294,7 +320,10 @@ __device__ __forceinline__ void few_rows_bf16(FewShared<D> &sh, uint32_t *s_row,
             const uint4 op = make_uint4(__builtin_amdgcn_perm(v[0][1][e / 2], v[0][0][e / 2], sel), __builtin_amdgcn_perm(v[0][3][e / 2], v[0][2][e / 2], sel),
                                         __builtin_amdgcn_perm(v[1][1][e / 2], v[1][0][e / 2], sel), __builtin_amdgcn_perm(v[1][3][e / 2], v[1][2][e / 2], sel));
 #pragma unroll
-            for (int t = PP - 1; t >= 0; --t) st.o[e] = few_mfma(op, make_uint4(part[t][0], part[t][1], part[t][2], part[t][3]), st.o[e]);
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int t = PP - 1; t >= 0; --t)
+                    st[r].o[e] = few_mfma(op, make_uint4(part[r][t][0], part[r][t][1], part[r][t][2], part[r][t][3]), st[r].o[e]);
         }
         next(fetch_v);
     };
@@ -304,26 +333,33 @@ __device__ __forceinline__ void few_rows_bf16(FewShared<D> &sh, uint32_t *s_row,
                        fetch_v(rows, tok, nsub);
                    },
                    use);
-    few_join<bf16_t, D>(sh, a, at, seq, steps, kvh, st, map.k2, met_odd);
+    few_join<bf16_t, D, RT>(sh, a, at, seq, steps, kvh, st, map.k2, met_odd);
 }
 
 // fp32: 16 tokens of a wave at a time; a lane's four tokens are the four slices of the second product.
-template <int D, int MODE>
+template <int D, int MODE, int RT>
 __device__ __forceinline__ void few_rows_f32(FewShared<D> &sh, uint32_t *s_row, const ChunkArgs &a, const Place &at, const SeqWork &seq,
                                              const Steps &steps, int kvh)
 {
     constexpr int U = D / 16, E = D / 16, RB = 4 * D;
     const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
-    const RowPlace rp(a, seq, at.unit, kvh, n);
-    float q[U][4];
-    const char *const qp = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * RB + 16 * g;
+    float q[RT][U][4];
+    RowSees sees[RT];
+    int pos[RT];
+    float slope[RT];
 #pragma unroll
-    for (int u = 0; u < U; ++u) Elem<float>::expand(load16(qp + 64 * u), q[u]);
-    const RowSees sees(a, seq, rp.query);
+    for (int r = 0; r < RT; ++r) {
+        const RowPlace rp(a, seq, at.unit, kvh, kFewTile * r + n);
+        const char *const qp = a.q + (seq.n0 + rp.query) * a.q_stride + (int64_t)rp.head * RB + 16 * g;
+#pragma unroll
+        for (int u = 0; u < U; ++u) Elem<float>::expand(load16(qp + 64 * u), q[r][u]);
+        sees[r] = RowSees(a, seq, rp.query);
+        pos[r] = seq.len - seq.nq + rp.query;
+        slope[r] = ScoreMap<MODE, true>::slope_of(a, rp.head);
+    }
     const WaveSees wave(sees);
-    const ScoreMap<MODE, true> map(a, rp.head);
-    const int pos = seq.len - seq.nq + rp.query;
-    FewState<E> st;
+    ScoreMap<MODE, true> map(a);
+    FewState<E> st[RT];
     bool met_odd = false;                        // of the lane
     float k[U][4], v[4][E];
     auto first_row = [&](const BlockRows &rows, int tok) {
@@ -344,25 +380,34 @@ __device__ __forceinline__ void few_rows_f32(FewShared<D> &sh, uint32_t *s_row, 
                 Elem<float>::expand(load16(vp + (uint32_t)(min(4 * g + j, last) * RB + n * 4 * E + 4 * e)), v[j] + e);
     };
     auto use = [&](int tok, auto next) {
-        floatx4 s[1] = {floatx4{}}, s2{};        // two chains
+        floatx4 s[RT][1], s2[RT];                // two chains
+#pragma unroll
+        for (int r = 0; r < RT; ++r) s[r][0] = s2[r] = floatx4{};
 #pragma unroll
         for (int u = 0; u < U; u += 2)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u][c], q[u][c], s[0], 0, 0, 0);
-                s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u + 1][c], q[u + 1][c], s2, 0, 0, 0);
-            }
-        next(fetch_k);
-        s[0] += s2;
-        map.template each<4>([&](int i) { return s[0][i]; }, [&](int i, float x) { s[0][i] = x; }, [](int i) { return i; }, pos, tok + 4 * g);
-        const bool masked = !wave.all(tok, 16);
-        if (masked) {
-            const uint32_t seen = (uint32_t)sees.mask(tok + 4 * g);
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (!(seen >> i & 1u)) s[0][i] = -INFINITY;
+                for (int r = 0; r < RT; ++r) {
+                    s[r][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u][c], q[r][u][c], s[r][0], 0, 0, 0);
+                    s2[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u + 1][c], q[r][u + 1][c], s2[r], 0, 0, 0);
+                }
+        next(fetch_k);
+        const bool masked = !wave.all(tok, 16);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            s[r][0] += s2[r];
+            map.slope2 = slope[r];
+            map.template each<4>([&](int i) { return s[r][0][i]; }, [&](int i, float x) { s[r][0][i] = x; }, [](int i) { return i; }, pos[r],
+                                 tok + 4 * g);
+            if (masked) {
+                const uint32_t seen = (uint32_t)sees[r].mask(tok + 4 * g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(seen >> i & 1u)) s[r][0][i] = -INFINITY;
+            }
+            st[r].weigh(s[r], map.k2);
         }
-        st.weigh(s, map.k2);
         if (masked) {                            // as above
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -376,7 +421,9 @@ __device__ __forceinline__ void few_rows_f32(FewShared<D> &sh, uint32_t *s_row, 
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int e = 0; e < E; ++e) st.o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][e], s[0][j], st.o[e], 0, 0, 0);
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) st[r].o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][e], s[r][0][j], st[r].o[e], 0, 0, 0);
         next(fetch_v);
     };
     few_tokens<16>(s_row, a, at, seq, steps, kvh,
@@ -385,7 +432,7 @@ __device__ __forceinline__ void few_rows_f32(FewShared<D> &sh, uint32_t *s_row, 
                        fetch_v(rows, tok, nsub);
                    },
                    use);
-    few_join<float, D>(sh, a, at, seq, steps, kvh, st, map.k2, met_odd);
+    few_join<float, D, RT>(sh, a, at, seq, steps, kvh, st, map.k2, met_odd);
 }
 
 }  // namespace

@@ -391,7 +391,9 @@ PlanArgs plan_args(const hgca_block_state *t)
     return a;
 }
 
-// Shares of a chunk call (chunk_device.hpp): about this many workgroups, two per compute unit.
+// Shares of a chunk call (chunk_device.hpp): about this many workgroups, two per compute unit; fp32, whose matrix instructions are what takes the time, evens
+// out better in twice as many (four prompts of 758 tokens over 2048: 268 -> 250 us; bf16, one token x 8 over 28 K: 512 : 768 : 1024
+// workgroups 168 : 178 : 171).
 #ifndef HGCA_TARGET_WGS_CHUNK
 #define HGCA_TARGET_WGS_CHUNK 512
 #endif
@@ -404,7 +406,7 @@ ChunkLayout chunk_layout(const hgca_shape *s, int64_t n_tokens, int64_t cap)
 {
     ChunkLayout t{};
     const int64_t units = t.units = n_tokens * group_of(s) / kChunkRows + std::min<int64_t>(n_tokens, s->batch);         // at most
-    t.target = std::max<int64_t>(1, HGCA_TARGET_WGS_CHUNK / s->n_kv_heads);
+    t.target = std::max<int64_t>(1, HGCA_TARGET_WGS_CHUNK * (s->dtype == HGCA_F32 ? 2 : 1) / s->n_kv_heads);
     // a share has 256 tokens at least, so a unit has so many at most, and one where the tier is that short
     const int64_t shares = std::max<int64_t>(1, (cap + 255) / 256);
     t.slots = std::min(t.target + units, units * shares);
