@@ -31,12 +31,11 @@ __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__bui
 
 // ---- the cut ----
 // A sequence of n tokens has u = ceil(n * group / kChunkRows) units, each over at most `steps` steps of its tokens.  Units are cut into shares
-// of at most C steps: s = ceil(steps / C) each.  C is at least kChunkLeast, and the least with which there are no more shares than the
+// of at most C steps: s = ceil(steps / C) each.  C is at least a.least, or all steps where they are no more than a.whole, and the least with which there are no more shares than the
 // `target` that runs at once; where there are more units than that, the steps of all units over the target.  So there are at
 // most target + (number of units) shares, and at most 2 target in units that have several.  One long sequence among many short ones, a
 // prompt among single tokens: a share is as long as any other.  Up to 64 sequences every wave works it out for itself, a lane per
 // sequence, from the lengths on the device; more are worked out by a launch before.
-constexpr int kChunkLeast = 4;
 
 struct SeqWork {
     int n0, nq, len, pre;                        // first row of q, rows, tokens, tokens that all rows see
@@ -60,8 +59,9 @@ struct SeqWork {
 // C, for sums over the sequences of units and of units * steps, the longest steps, and shares(c), the number of shares of at most c steps (saturated, fp32)
 template <typename Shares> __device__ __forceinline__ int share_steps(const ChunkArgs &a, float units, float work, int longest, Shares shares) {
     const float target = (float)a.target;
-    int c = max((int)(work / target), kChunkLeast);
-    if (units > target) return max((int)(work / target * 1.0001f) + 1, kChunkLeast);
+    if (longest <= a.whole) return max(longest, 1);
+    int c = max((int)(work / target), a.least);
+    if (units > target) return max((int)(work / target * 1.0001f) + 1, a.least);
     if (c >= longest || shares(c) <= target) return c;
     // shares(c) <= work / c + units, and one share each is few enough
     int enough = units < target ? (int)min(work / (target - units) * 1.0001f + 1.f, (float)longest) : longest;
@@ -70,7 +70,7 @@ template <typename Shares> __device__ __forceinline__ int share_steps(const Chun
         const int mid = c + (enough - c) / 2;
         if (shares(mid) <= target) enough = mid; else c = mid;
     }
-    return max(enough, kChunkLeast);
+    return max(enough, a.least);
 }
 // 0 for a sequence without new tokens
 __device__ __forceinline__ int shares_of(const SeqWork &q, int c) { return q.units > 0 ? (q.steps + c - 1) / c : 0; }

@@ -318,3 +318,59 @@ def test_beyond_4_gib_of_a_tier(gpu):
         O, Ls = so.chunk(q, [0, 5], K, V, [250], 0.125)
         check(o, lse, O, Ls, *bounds(dtype, "f32", q, K, V, [250], 0.125, T=256), "f32", dtype)
         del k, v, tier
+
+
+def test_no_lengths_and_no_tokens(gpu):
+    """A tier without lengths holds `cap` tokens of every sequence; one of capacity 0 holds none."""
+    torch, hgca = gpu
+    for dtype in ("bf16", "f32"):
+        rng, q, K, V = inputs(12, dtype, [30, 2], 4, 2, 64, 77)
+        shape = hgca.Shape(hgca.F32 if dtype == "f32" else hgca.BF16, 2, 4, 2, 64, 0.125)
+        tier = hgca.Tier(put(torch, K, dtype), put(torch, V, dtype), 77)
+        cu = [0, 30, 32]
+        o, lse = call(gpu, shape, put(torch, q, dtype), cu, tier, "f32")
+        O, L = so.chunk(q, cu, K, V, [77, 77], 0.125)
+        check(o, lse, O, L, *bounds(dtype, "f32", q, K, V, [77, 77], 0.125, T=77), "f32", dtype)
+        tier = hgca.Tier(put(torch, K[:, :, :0], dtype), put(torch, V[:, :, :0], dtype), 0)
+        o, lse = call(gpu, shape, put(torch, q, dtype), cu, tier, "f32")
+        assert (o == 0).all() and torch.isneginf(lse).all()
+
+
+def test_captured_with_many_sequences(gpu):
+    """More sequences than a wave has lanes (a launch of its own works out the shares), captured and replayed with other lengths, counts and rows."""
+    torch, hgca = gpu
+    B, Hq, Hkv, d, T = 70, 4, 2, 64, 900
+    rng = np.random.default_rng(1)
+    shape = hgca.Shape(hgca.BF16, B, Hq, Hkv, d, 0.125)
+    K, V = (do.to_bf16(rng.standard_normal((B, Hkv, T, d))) for _ in "kv")
+    lens = torch.zeros(B, dtype=torch.int32, device=DEV)
+    cu = torch.zeros(B + 1, dtype=torch.int32, device=DEV)
+    tier = hgca.Tier(put(torch, K, "bf16"), put(torch, V, "bf16"), T, lens)
+    q = torch.zeros(400, Hq, d, dtype=torch.bfloat16, device=DEV)
+    outs = [(torch.zeros(400, Hq, d, device=DEV), torch.zeros(400, Hq, device=DEV), hgca.chunk_workspace(shape, 400, T, DEV)) for _ in range(2)]
+    run = lambda i: hgca.chunk_attn(shape, q, cu, tier, *outs[i], window=500)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    for turn in range(5):
+        counts = np.minimum(rng.integers(0, 9, B), 400)
+        counts[turn] = 30
+        n = rng.integers(0, T + 1, B)
+        Q = do.to_bf16(rng.standard_normal((400, Hq, d)))
+        q.copy_(torch.from_numpy(Q))
+        lens.copy_(i32(torch, n))
+        cu.copy_(i32(torch, np.concatenate([[0], np.cumsum(counts)])))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            if turn == 0:
+                run(0)
+            else:
+                if turn == 1:
+                    with torch.cuda.graph(graph, stream=side):
+                        run(0)
+                graph.replay()
+        torch.cuda.synchronize()
+        run(1)
+        torch.cuda.synchronize()
+        at = int(counts.sum())
+        assert torch.equal(outs[0][0][:at], outs[1][0][:at]) and torch.equal(outs[0][1][:at], outs[1][1][:at])
+        O, L = so.chunk(Q[:at], cu.tolist(), K, V, n, 0.125, window=500)
+        check(outs[0][0][:at], outs[0][1][:at], O, L, *bounds("bf16", "f32", Q[:at], K, V, n, 0.125, T=T), "f32")

@@ -181,3 +181,32 @@ def test_strides_and_a_vocabulary_of_one(gpu):
     want = so.verify(target, draft, tokens, u, u_next, parents)
     for a, b in zip((path, cnt, nxt), want):
         assert np.array_equal(a.cpu().numpy(), b)
+
+
+def test_captured_and_replayed(gpu):
+    """One graph, other distributions and random numbers at every replay, eager work between them."""
+    torch, hgca = gpu
+    B, n, V = 5, 7, 5000
+    bufs = dict(target=torch.zeros(B, n, V, device=DEV), draft=torch.zeros(B, n, V, device=DEV), tokens=torch.zeros(B, n, dtype=torch.int32, device=DEV),
+                u=torch.zeros(B, n, device=DEV), u_next=torch.zeros(B, device=DEV), path_out=torch.zeros(B, n, dtype=torch.int32, device=DEV),
+                cnt_out=torch.zeros(B, dtype=torch.int32, device=DEV), next_out=torch.zeros(B, dtype=torch.int32, device=DEV),
+                ws=hgca.verify_workspace(B, V, DEV), parents=torch.zeros(B, n, dtype=torch.int32, device=DEV))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    for turn in range(5):
+        target, draft, tokens, parents, u, u_next = drafted(np.random.default_rng(turn), B, n, V, True, "f32")
+        for k, x in (("target", target), ("draft", draft), ("u", u), ("u_next", u_next), ("tokens", tokens.astype(np.int32)), ("parents", parents.astype(np.int32))):
+            bufs[k].copy_(torch.from_numpy(x))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            if turn == 0:
+                hgca.verify_drafts(**bufs)
+            else:
+                if turn == 1:
+                    with torch.cuda.graph(graph, stream=side):
+                        hgca.verify_drafts(**bufs)
+                graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((bufs["path_out"], bufs["cnt_out"], bufs["next_out"]), so.verify(target, draft, tokens, u, u_next, parents)):
+            assert np.array_equal(a.cpu().numpy(), b)
+        bufs["target"].sum()
+        torch.cuda.synchronize()
