@@ -729,7 +729,7 @@ int hgca_kv8_attn(const hgca_shape *shape, const void *q, int32_t n_q,
 /* Blocks of a paged tier dealt out on the device.  Row b of block_table names the blocks of
  * sequence b, its first held[b] entries are in use and hold lens[b] tokens (held[b] >=
  * ceil(lens[b] / block_size)); free_blocks[0 .. *free_count) are the numbers of the blocks
- * that nobody holds, a stack whose top is the last.  All arrays are device memory; a tier
+ * that nobody holds, a stack whose top is the last; no block is in use twice.  All arrays are device memory; a tier
  * over them is { k, v, lens, block_table, cap, block_size, max_blocks }.  n_blocks *
  * block_size is at most 2^31 - 1.  Calls on one state go one after the other. */
 typedef struct {
@@ -777,7 +777,7 @@ int hgca_kv_release(const hgca_block_state *state, const int32_t *new_lens, void
  * position.  Tokens whose slot is not in [0, n_slots) are left out (n_slots: slots of the
  * tier, its blocks times block_size or B * cap); slots differ from each other.  tier->k, v
  * are written, its lengths and table not read (a contiguous tier has none).  k_in / v_in
- * must not overlap the tier's rows (refused). */
+ * must not overlap the tier's rows, nor its k its v (refused). */
 int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_slots,
                   const int32_t *slots, const void *k_in, int64_t k_token_stride,
                   const void *v_in, int64_t v_token_stride, int32_t n_tokens, void *hip_stream);
@@ -803,7 +803,7 @@ int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_s
  * finite; tier->cap is at most 2^30.  Results do not depend on other calls and repeat bit for
  * bit; where a sequence is cut into shares does depend on the batch.  ws needs
  * hgca_chunk_workspace_bytes(shape, n_tokens, tier->cap), which also serves fewer tokens and
- * smaller capacities. */
+ * smaller capacities.  o_out, lse_out and q must not overlap (refused). */
 enum { HGCA_CHUNK_CAUSAL = 1 };
 size_t hgca_chunk_workspace_bytes(const hgca_shape *shape, int32_t n_tokens, int32_t max_tokens);
 int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stride, const int32_t *cu,
@@ -830,6 +830,7 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
  * Sums are fp64.  path_out ([B, n_drafts]) receives the accepted tokens' indices, root first, then -1,
  * cnt_out ([B]) their number, the path and cnt of hgca_kv_commit; next_out ([B]) the drawn
  * token, -1 where the row has no positive element.  1 <= n_drafts <= HGCA_MAX_DRAFTS, vocab at most 2^30.
+ * Outputs must not overlap each other, tokens, parents, u or u_next (refused).
  * ws (8-byte aligned) needs hgca_verify_workspace_bytes(batch, vocab). */
 size_t hgca_verify_workspace_bytes(int32_t batch, int32_t vocab);
 int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p_dtype,

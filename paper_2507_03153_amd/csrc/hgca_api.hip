@@ -1840,6 +1840,7 @@ int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_s
     // offsets stay far from 2^63, threads of the grid below 2^32
     if (ks > (int64_t(1) << 42) / n_tokens || vs > (int64_t(1) << 42) / n_tokens || n_tokens > 1 << 23) return HGCA_ERR_UNSUPPORTED;
     const int64_t rows = n_slots / per_block * per_block * token;
+    if (Range(tier->k, rows).meets(Range(tier->v, rows))) return HGCA_ERR_INVALID_ARG;
     for (const void *out : {tier->k, tier->v}) {
         const Range to(out, rows);
         if (to.meets(Range(k_in, (n_tokens - 1) * ks + token)) || to.meets(Range(v_in, (n_tokens - 1) * vs + token)) ||
@@ -1890,6 +1891,9 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
     // threads of a flat grid are counted in 32 bits; offsets stay far from 2^63
     if (t.slots * shape->n_kv_heads > int64_t(1) << 23 || qs > (int64_t(1) << 40) / n_tokens) return HGCA_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < t.total || !aligned16(ws)) return HGCA_ERR_WORKSPACE;
+    const Range o(o_out, n_tokens * token * (o_dtype == HGCA_BF16 ? 2 : 4)), lse(lse_out, 4 * (int64_t)n_tokens * shape->n_q_heads);
+    const Range rows(q, ((n_tokens - 1) * qs + token) * e);
+    if (o.meets(rows) || lse.meets(rows) || o.meets(lse)) return HGCA_ERR_INVALID_ARG;
     char *const base = static_cast<char *>(ws);
     ChunkArgs a{};
     a.sh = to_dev(shape);
@@ -1923,7 +1927,8 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
 size_t hgca_verify_workspace_bytes(int32_t batch, int32_t vocab)
 {
     if (batch < 0 || vocab < 1) return 0;
-    return std::max<size_t>(kAlign, align_up((size_t)batch * (((size_t)vocab + kVerifySegment - 1) / kVerifySegment) * sizeof(double)));
+    const size_t sums = (((size_t)vocab + kVerifySegment - 1) / kVerifySegment) * sizeof(double);
+    return std::max<size_t>(kAlign, align_up((size_t)batch * kVerifyPasses * (sums + sizeof(VerifyWalk))));
 }
 
 int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p_dtype, const void *target, int64_t target_row_stride,
@@ -1939,12 +1944,21 @@ int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p
     const uintptr_t e = p_dtype == HGCA_BF16 ? 2 : 4;
     if (reinterpret_cast<uintptr_t>(target) % e != 0 || reinterpret_cast<uintptr_t>(draft) % e != 0) return HGCA_ERR_INVALID_ARG;
     const int64_t tr = target_row_stride ? target_row_stride : vocab, dr = draft_row_stride ? draft_row_stride : vocab;
-    const int64_t most = int64_t(1) << 40;       // offsets stay far from 2^63
+    const int64_t most = int64_t(1) << 40, per_draft = 4 * (int64_t)batch * n_drafts;    // offsets stay far from 2^63
     if (tr < vocab || dr < vocab || target_seq_stride < 0 || draft_seq_stride < 0) return HGCA_ERR_INVALID_ARG;
     if (tr > most / HGCA_MAX_DRAFTS || dr > most / HGCA_MAX_DRAFTS) return HGCA_ERR_UNSUPPORTED;
     const int64_t ts = target_seq_stride ? target_seq_stride : tr * n_drafts, ds = draft_seq_stride ? draft_seq_stride : dr * n_drafts;
     if (ts > most || ds > most) return HGCA_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < hgca_verify_workspace_bytes(batch, vocab) || reinterpret_cast<uintptr_t>(ws) % 8 != 0) return HGCA_ERR_WORKSPACE;
+    // a sequence's results are written while others still read
+    const Range outs[3] = {Range(path_out, per_draft), Range(cnt_out, 4 * (int64_t)batch), Range(next_out, 4 * (int64_t)batch)};
+    const Range ins[4] = {Range(tokens, per_draft), Range(u, per_draft), Range(u_next, 4 * (int64_t)batch), Range(parents, parents ? per_draft : 0)};
+    for (int i = 0; i < 3; ++i) {
+        for (const Range &in : ins)
+            if (in.bytes && outs[i].meets(in)) return HGCA_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (outs[i].meets(outs[j])) return HGCA_ERR_INVALID_ARG;
+    }
     VerifyArgs a{};
     a.target = static_cast<const char *>(target);
     a.draft = static_cast<const char *>(draft);
@@ -1959,10 +1973,18 @@ int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p
     a.path = path_out;
     a.cnt = cnt_out;
     a.next = next_out;
-    a.sums = static_cast<double *>(ws);
     a.batch = batch;
     a.n = n_drafts;
     a.vocab = vocab;
+    // Launches.  Rows of a segment for each wave of a sequence's workgroup: it does everything (five tokens, 1 x 2000 elements 13.9 -> 10.8 us, 8 x
+    // 32 000 15.5 : 15.8, 256 x 32 000 26.9 -> 25.6; 8 x 64 000 14.9 : 17.6).  Longer ones: a launch over the chip for the first sums.  After a refusal
+    // only a tree has another token to try, and with it another pass over the rows: by the sequence's own workgroup it takes 13 us for 128 000
+    // elements, by a launch 8 us for 32 such sequences, and 3 us where no sequence needs it; so launches for long rows, more of them where the
+    // worst of many sequences counts.  Trees of 16, 1 : 3 : 4 launches: 8 sequences 39 : 28 : 31 us, 32 62 : 44 : 40, 128 92 : 76 : 72, all accepted
+    // 16 : 19 : 23; 8 x 64 000, 1 : 3, 25 : 25, all accepted 14 : 19.
+    a.passes = vocab <= kVerifyAlone * kVerifySegment ? 0 : !parents || n_drafts < 3 || vocab <= 32 * kVerifySegment ? 1 : batch < 16 ? kVerifyPasses - 1 : kVerifyPasses;
+    a.walks = static_cast<VerifyWalk *>(ws);
+    a.sums = reinterpret_cast<double *>(a.walks + (size_t)kVerifyPasses * batch);
     return from_hip(launch_verify_drafts(p_dtype, a, static_cast<hipStream_t>(hip_stream)));
 }
 

@@ -348,16 +348,25 @@ struct WriteArgs {
 };
 hipError_t launch_kv_write(const WriteArgs &a, hipStream_t s);
 
+struct VerifyWalk {
+    double c, mass;
+    uint64_t path, gone;
+    int32_t node, tried, refused, pass;   // pass: whose sums are those of the node
+};
 struct VerifyArgs {
     const char *target, *draft;           // [B, n, V] with rows of V elements, strides in elements; draft may be null
     int64_t target_row, target_seq, draft_row, draft_seq;
     const int32_t *tokens, *parents;      // [B, n]; parents may be null (i - 1)
     const float *u, *u_next;   // [B, n], [B]
     int32_t *path, *cnt, *next;           // [B, n], [B], [B]
-    double *sums;              // [B, segments]
+    double *sums;              // [passes, B, segments]
+    VerifyWalk *walks;         // [passes, B]
     int32_t batch, n, vocab;
+    int32_t passes;            // launches that form sums, up to kVerifyPasses; 0: rows of kVerifyAlone segments at most, one launch for all
 };
 constexpr int kVerifySegment = 2048;      // elements of a row that one partial sum covers
+constexpr int kVerifyAlone = 16;          // segments that one workgroup goes through without other launches
+constexpr int kVerifyPasses = 4;          // launches that form sums, at most
 hipError_t launch_verify_drafts(int dtype, const VerifyArgs &a, hipStream_t s);
 
 // Attention of packed new tokens.  The tokens of a sequence, times the heads of a group, are rows; kChunkRows of them are a unit, of

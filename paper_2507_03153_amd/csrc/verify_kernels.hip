@@ -11,9 +11,13 @@
 // Sums are fp64: the order of additions is then in no result that a plain running sum would not give as well but once in some 10^10 draws, and
 // the pass is bound by memory all the same.
 //
-// The first pass is the only one of most sequences, and which row and c it is of is known from single elements: every workgroup of the first
-// launch finds it for itself (walk_first), and leaves the sums of its segments.  The second launch, a workgroup per sequence, goes on from
-// there: more refusals at the same node, or further down, are passes of its own.  The draw takes one more segment.
+// A pass reads two rows of the vocabulary for each sequence, and that and the latency of one dependent load after the other bound it: parents and
+// tokens, elements of the rows, the rows.  So short rows are one workgroup's, a segment a wave, in one launch; for longer ones every workgroup
+// of a launch over the chip finds for itself where the walk first stops (single elements), and leaves the sums of its segments; launches like it
+// follow for trees with long rows, in which other refusals come next, and a last one, a workgroup per sequence, goes through what is
+// left and draws, for which it reads one more segment.  Measured: 8 x 5 tokens, 32 000 elements, fp32, 15.5 us as a call, 32 trees of 16 over 128 000
+// 40.4 (12.4 for the first sums, 33 MB, 7.9 and less for the next three, 7.7 for the rest).  Of a pass's arithmetic the conversions to fp64 take
+// most, 56 cycles an element and wave in all, 1.5 us of those 7.9.
 #include <algorithm>
 
 #include "hgca_launch.hpp"
@@ -80,13 +84,9 @@ struct Nodes {
     }
 };
 
-// Where a walk stands: at `node`, the drafted tokens up to `tried` have been seen to, c and mass (S) of what is left of the target.
-struct Walk {
-    int node, tried;
-    double c, mass;
-    uint64_t path;                               // accepted tokens, a bit each
-    uint64_t gone;                               // without q: refused children of the node
-};
+// Where a walk stands (kept between the launches): at `node`, the drafted tokens up to `tried` have been seen to, c and mass (S) of what is left of the
+// target.  path: accepted tokens, a bit each; gone: without q, the refused children of the node.
+using Walk = VerifyWalk;
 
 __device__ __forceinline__ double lane_value(float x, int lane) {
     return (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
@@ -120,6 +120,14 @@ __device__ __forceinline__ bool walk_on(Walk &w, const Nodes &nodes, bool with_q
         w.gone |= 1ull << j;
         return true;
     }
+}
+
+// Goes on from a refusal, for which `mass` is left of the target; true: sums have to be formed for where the walk stops now, another refusal or the end at a
+// node of which there are none.
+__device__ __forceinline__ bool go_on(Walk &w, const Nodes &nodes, bool with_q, double mass) {
+    w.mass = mass;
+    w.refused = walk_on(w, nodes, with_q);
+    return w.refused || w.c == 0.0;
 }
 
 // 16 bytes of a row as elements.
@@ -234,50 +242,62 @@ struct Rest {
 
 __device__ __forceinline__ int segments_of(const VerifyArgs &a) { return (a.vocab + kVerifySegment - 1) / kVerifySegment; }
 
-// The walk up to its first refusal, or to its end.
-template <typename T> __device__ __forceinline__ bool walk_first(const VerifyArgs &a, int b, Nodes &nodes, Walk &w) {
-    nodes.load<T>(a, b);
-    w = Walk{0, 0, 0.0, 1.0, 1ull, 0};
-    return walk_on(w, nodes, a.draft != nullptr);
+// The sum over all segments' sums, by a wave, in every lane.
+__device__ __forceinline__ double sum_of(const double *sums, int segs) {
+    double s = 0.0;
+    for (int i = threadIdx.x % kWave; i < segs; i += kWave) s += sums[i];
+    return wave_sum64(s);
 }
 
-// The sums of all segments of the row where the walk first stops, a wave per segment.
-template <typename T>
-__global__ __launch_bounds__(kSumBlock) void verify_sums_kernel(VerifyArgs a)
+__device__ __forceinline__ double *pass_sums(const VerifyArgs &a, int b, int pass, int segs) { return a.sums + ((int64_t)pass * a.batch + b) * segs; }
+
+// One pass of a launch: where the walk stops for the PASS-th time (at a refusal or its end) the sums of all segments of the row, a wave per segment.
+// Sequences whose walk has ended before have nothing to do but hand on where.
+template <typename T, bool FIRST>
+__global__ __launch_bounds__(kSumBlock) void verify_sums_kernel(VerifyArgs a, int pass)
 {
     const int b = blockIdx.y, seg = blockIdx.x * kSumWaves + threadIdx.x / kWave, segs = segments_of(a);
     Nodes nodes;
-    Walk w;
-    walk_first<T>(a, b, nodes, w);
-    if (seg >= segs) return;
+    Walk w{0.0, 1.0, 1ull, 0, 0, 0, 0, 0};
+    bool work = true;                            // uniform over the workgroup
+    if (FIRST) {
+        nodes.load<T>(a, b);
+        w.refused = walk_on(w, nodes, a.draft != nullptr);
+    } else {
+        w = a.walks[(int64_t)(pass - 1) * a.batch + b];
+        work = w.refused != 0;
+        if (work) {
+            nodes.load<T>(a, b);
+            work = go_on(w, nodes, a.draft != nullptr, sum_of(pass_sums(a, b, w.pass, segs), segs));
+            if (work) w.pass = pass;
+        }
+    }
+    if (seg == 0 && threadIdx.x == 0) a.walks[(int64_t)pass * a.batch + b] = w;
+    if (!work || seg >= segs) return;
     const Rest<T> rest(a, b, w);
     const double sum = rest.segment(nodes, seg);
-    if (threadIdx.x % kWave == 0) a.sums[(int64_t)b * segs + seg] = sum;
+    if (threadIdx.x % kWave == 0) pass_sums(a, b, pass, segs)[seg] = sum;
 }
 
-template <typename T>
+// The rest of the walk, a workgroup per sequence, and the draw.  ALONE: all of it, without launches before, for rows of kVerifyAlone segments at most.
+template <typename T, bool ALONE>
 __global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
 {
+    __shared__ double s_alone[ALONE ? kVerifyAlone : 1];
     __shared__ double s_sum[kWalkWaves];
     __shared__ int s_hit[kWalkWaves], s_last[kWalkWaves];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, segs = segments_of(a);
-    double *const sums = a.sums + (int64_t)b * segs;
+    Walk w{0.0, 1.0, 1ull, 0, 0, 0, 0, 0};
     Nodes nodes;
-    Walk w;
-    bool refused = walk_first<T>(a, b, nodes, w);
-    // the sum over all segments' sums, in every thread, always in the same order
-    auto whole = [&] {
-        double s = 0.0;
-        for (int i = tid; i < segs; i += kWalkBlock) s += sums[i];
-        s = wave_sum64(s);
-        __syncthreads();
-        if (lane == 0) s_sum[wave] = s;
-        __syncthreads();
-        s = s_sum[0];
-#pragma unroll
-        for (int i = 1; i < kWalkWaves; ++i) s += s_sum[i];
-        return s;
-    };
+    double *sums = s_alone;
+    if (ALONE) {
+        nodes.load<T>(a, b);
+        w.refused = walk_on(w, nodes, a.draft != nullptr);
+    } else {
+        w = a.walks[(int64_t)(a.passes - 1) * a.batch + b];
+        sums = pass_sums(a, b, w.pass, segs);
+        if (w.refused || w.gone) nodes.load<T>(a, b);            // uniform; else nobody asks
+    }
     auto pass = [&] {
         const Rest<T> rest(a, b, w);
         __syncthreads();                         // nobody reads the old sums any more
@@ -286,16 +306,10 @@ __global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
             if (lane == 0) sums[seg] = sum;
         }
         __syncthreads();
-        return whole();
+        return sum_of(sums, segs);
     };
-    double total = whole();
-    while (refused) {                            // (uniform: every wave has the same numbers)
-        w.mass = total;
-        refused = walk_on(w, nodes, a.draft != nullptr);
-        // another refusal, or the end at a node of which no sums are there
-        if (refused || w.c == 0.0) total = pass();
-        if (!refused) break;
-    }
+    double total = ALONE ? pass() : sum_of(sums, segs);
+    while (w.refused && go_on(w, nodes, a.draft != nullptr, total)) total = pass();         // (uniform: every wave has the same numbers)
     if (!(total > 0.0)) {                        // nothing is left: the target itself
         w.c = 0.0;
         w.gone = 0;
@@ -370,17 +384,28 @@ __global__ __launch_bounds__(kWalkBlock) void verify_walk_kernel(VerifyArgs a)
 
 }  // namespace
 
-hipError_t launch_verify_drafts(int dtype, const VerifyArgs &a, hipStream_t s)
+template <typename T> static hipError_t launch_verify(const VerifyArgs &a, hipStream_t s)
 {
     const int segs = (a.vocab + kVerifySegment - 1) / kVerifySegment;
+    if (a.passes == 0) {
+        hipLaunchKernelGGL((verify_walk_kernel<T, true>), dim3(a.batch), dim3(kWalkBlock), 0, s, a);
+        return hipGetLastError();
+    }
     const dim3 grid((segs + kSumWaves - 1) / kSumWaves, a.batch);
-    if (dtype == 0) hipLaunchKernelGGL(verify_sums_kernel<float>, grid, dim3(kSumBlock), 0, s, a);
-    else hipLaunchKernelGGL(verify_sums_kernel<bf16_t>, grid, dim3(kSumBlock), 0, s, a);
+    hipLaunchKernelGGL((verify_sums_kernel<T, true>), grid, dim3(kSumBlock), 0, s, a, 0);
     hipError_t rc = hipGetLastError();
+    for (int pass = 1; pass < a.passes && rc == hipSuccess; ++pass) {
+        hipLaunchKernelGGL((verify_sums_kernel<T, false>), grid, dim3(kSumBlock), 0, s, a, pass);
+        rc = hipGetLastError();
+    }
     if (rc != hipSuccess) return rc;
-    if (dtype == 0) hipLaunchKernelGGL(verify_walk_kernel<float>, dim3(a.batch), dim3(kWalkBlock), 0, s, a);
-    else hipLaunchKernelGGL(verify_walk_kernel<bf16_t>, dim3(a.batch), dim3(kWalkBlock), 0, s, a);
+    hipLaunchKernelGGL((verify_walk_kernel<T, false>), dim3(a.batch), dim3(kWalkBlock), 0, s, a);
     return hipGetLastError();
+}
+
+hipError_t launch_verify_drafts(int dtype, const VerifyArgs &a, hipStream_t s)
+{
+    return dtype == 0 ? launch_verify<float>(a, s) : launch_verify<bf16_t>(a, s);
 }
 
 }  // namespace hgca

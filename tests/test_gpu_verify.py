@@ -210,3 +210,27 @@ def test_captured_and_replayed(gpu):
             assert np.array_equal(a.cpu().numpy(), b)
         bufs["target"].sum()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("with_q", [True, False])
+@pytest.mark.parametrize("dtype,B", [("f32", 5), ("bf16", 20)])
+def test_refusals_over_a_large_vocabulary(gpu, dtype, B, with_q):
+    """Rows of more than 65536 elements: four children of every node, with random numbers that refuse none, one, ... all of them, here and at the
+    accepted child, the same token twice; from no pass over the rows but the last to more than there are launches for."""
+    rng = np.random.default_rng(B)
+    n, V = 13, 66003
+    target, draft, tokens, _, u, u_next = drafted(rng, B, n, V, True, dtype, sharp=1.5)
+    parents = np.tile(np.array([0, 0, 0, 0, 0, 1, 1, 1, 3, 3, 3, 9, 9]), (B, 1))
+    for j in range(1, n):
+        tokens[:, j] = [np.argsort(-target[b, parents[b, j]])[(3 * j + b) % 7] for b in range(B)]
+    tokens[::2, 4] = tokens[::2, 2]
+    for b in range(B):
+        u[b, 1:1 + b % 5] = 0.9999                                             # the root's first b % 5 children are refused
+        u[b, 1 + b % 5:5] = 1e-9
+        u[b, 5:8] = u[b, 8:] = 0.9999 if b % 3 else 1e-9
+    draft = draft if with_q else None
+    want = so.verify(target, draft, tokens, u, u_next, parents)
+    got = call(gpu, target, draft, tokens, u, u_next, parents, dtype, 5)
+    print(f"\n[case] {dtype} B={B} q={with_q}: cnt {want[1].tolist()}, margin {want[3]:.1e}", flush=True)
+    for a, b in zip(got, want):
+        assert np.array_equal(a, b)

@@ -144,6 +144,21 @@ def test_verify_refusals(hg):
     assert verify(hg, B=0, t=None) == hg.OK
 
 
+def test_overlaps(hg):
+    """Arrays that a call writes while it reads others; a byte behind the other's end is no overlap."""
+    I, W = hg.ERR_INVALID_ARG, hg.ERR_WORKSPACE
+    assert verify(hg, path=at(2)) == verify(hg, cnt=at(2) + 28) == verify(hg, nxt=at(4)) == verify(hg, path=at(3) - 4) == verify(hg, cnt=at(6), nxt=at(6) + 4) == I
+    assert verify(hg, par=at(9), cnt=at(9)) == verify(hg, path=at(5), nxt=at(5) + 28) == I
+    assert verify(hg, cnt=at(2) + 32, ws=None) == verify(hg, nxt=at(6) + 8, ws=None) == W          # (checked before the overlaps)
+    q, o, lse = 1 << 30, 1 << 31, 1 << 32        # 10 tokens of 8 x 128 bf16: 20 480 bytes; fp32 O 40 960, lse 320
+    args = dict(T=10, sh=shape(hg, B=1, Hq=8, Hkv=2, d=128), od=0)
+    for bad in (dict(q=q, o=q, lse=lse), dict(q=q, o=q + 20464, lse=lse), dict(q=q, o=o, lse=o + 40956), dict(q=q, o=o, lse=q + 16), dict(q=q, o=q - 40944, lse=lse)):
+        assert chunk(hg, **args, **bad) == I, bad
+    sh, k = shape(hg, B=1, Hq=2, Hkv=2, d=64), 1 << 30               # 100 slots of 2 x 64 bf16: 25 600 bytes
+    two = lambda v: hg.lib().hgca_kv_write(ctypes.byref(sh), ctypes.byref(view(hg, k=k, v=v, cap=100)), 100, 1 << 33, 1 << 34, 0, 1 << 35, 0, 1, None)
+    assert two(k) == two(k + 25584) == two(k - 25584) == I
+
+
 # ---- the oracle's pins ----
 
 def test_plan_pin():
