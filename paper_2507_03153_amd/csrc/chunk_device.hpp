@@ -37,6 +37,8 @@ __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__bui
 // prompt among single tokens: a share is as long as any other.  Up to 64 sequences every wave works it out for itself, a lane per
 // sequence, from the lengths on the device; more are worked out by a launch before.
 
+constexpr int kFewTile = 16;                     // rows that are worked on straight from memory (chunk_few.hpp)
+
 struct SeqWork {
     int n0, nq, len, pre;                        // first row of q, rows, tokens, tokens that all rows see
     int units, steps;
@@ -50,6 +52,8 @@ struct SeqWork {
         if (a.causal) tokens = min(tokens, (int64_t)a.window + kChunkRows / a.sh.group + pre + 3 * kChunkStep);
         steps = max((int)((tokens + kChunkStep - 1) / kChunkStep), 1);
     }
+    // Its shares come before those of sequences with a few rows: these take less time, and fill what the last ones of a round leave.
+    __device__ __forceinline__ bool whole_units(const ChunkArgs &a) const { return (int64_t)nq * a.sh.group > kFewTile; }
     // all lanes have the same: the compiler is told so, and keeps them, and what follows from them, in scalar registers
     __device__ __forceinline__ void unify() {
         for (int *x : {&n0, &nq, &len, &pre, &units, &steps}) *x = __builtin_amdgcn_readfirstlane(*x);
@@ -101,8 +105,10 @@ struct Place {
         if (B <= kWave) {
             units = n_shares = 0;
             int steps = 0;
+            bool whole = false;
             if (lane < B) {
                 const SeqWork q(a, lane);
+                whole = q.whole_units(a);
                 units = q.units;
                 steps = units > 0 ? q.steps : 0;
             }
@@ -110,8 +116,13 @@ struct Place {
                                       [&](int c) { return wave_sum((float)units * (float)((steps + c - 1) / c)); });
             const int shares = units > 0 ? (steps + c - 1) / c : 0, slots = units * shares, several = shares > 1 ? slots : 0;
             const int parts = (int)wave_inclusive_scan((uint32_t)several) - several;
-            const int mine = FOLD ? (shares > 1 ? units : 0) : slots, upto = (int)wave_inclusive_scan((uint32_t)mine);
-            const uint64_t behind = __ballot(upto > x);
+            int mine = FOLD ? (shares > 1 ? units : 0) : whole ? slots : 0, upto = (int)wave_inclusive_scan((uint32_t)mine);
+            const int before = __builtin_amdgcn_readlane(upto, kWave - 1);
+            if (!FOLD && x >= before) {          // uniform over the wave
+                mine = whole ? 0 : slots;
+                upto = before + (int)wave_inclusive_scan((uint32_t)mine);
+            }
+            const uint64_t behind = __ballot(upto > x && mine > 0);
             if (behind == 0) return;
             b = __builtin_ctzll(behind);
             inside = x - (__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(mine, b));
@@ -119,8 +130,12 @@ struct Place {
             n_shares = __builtin_amdgcn_readlane(shares, b);
             part = __builtin_amdgcn_readlane(parts, b);
         } else {
-            const int32_t *const slots = a.cut + 1, *const parts = slots + B + 1, *const several = parts + B + 1;
-            const int32_t *const list = FOLD ? several : slots;
+            const int32_t *const slots = a.cut + 1, *const parts = slots + B + 1, *const several = parts + B + 1, *const later = several + B + 1;
+            const int32_t *list = FOLD ? several : slots;
+            if (!FOLD && x >= slots[B]) {
+                x -= slots[B];
+                list = later;
+            }
             b = wave_search(list, B, x);
             if (b < 0) return;
             inside = x - list[b];

@@ -13,7 +13,7 @@ namespace hgca {
 
 namespace {
 
-constexpr int kFewRows = 32, kFewTile = 16;
+constexpr int kFewRows = 32;
 
 __device__ __forceinline__ floatx4 few_mfma(const uint4 &a, const uint4 &b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);

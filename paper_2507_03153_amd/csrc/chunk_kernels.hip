@@ -271,7 +271,7 @@ constexpr int kCutBlock = 1024, kCutWaves = kCutBlock / kWave;
 __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
 {
     __shared__ float s_work[kCutWaves];
-    __shared__ uint32_t s_sum[3][kCutWaves];
+    __shared__ uint32_t s_sum[4][kCutWaves];
     const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, B = a.sh.batch;
     auto over_all = [&](float x, bool largest) { // a workgroup's sum or maximum, in every thread
         x = largest ? wave_max(x) : wave_sum(x);
@@ -299,27 +299,29 @@ __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
         }
         return over_all(n, false);
     });
-    int32_t *const lists = a.cut + 1;            // three lists of B + 1 beginnings: slots, partials, units with several shares
+    int32_t *const lists = a.cut + 1;            // four lists of B + 1 beginnings: slots, partials, units with several shares, later slots
     if (tid == 0) a.cut[0] = c;
-    if (tid < 3) lists[tid * (B + 1)] = 0;
-    uint32_t base[3] = {0, 0, 0};
+    if (tid < 4) lists[tid * (B + 1)] = 0;
+    uint32_t base[4] = {0, 0, 0, 0};
     for (int b0 = 0; b0 < B; b0 += kCutBlock) {
         const int b = b0 + tid;
-        uint32_t v[3] = {0, 0, 0};
+        uint32_t v[4] = {0, 0, 0, 0};
         if (b < B) {
             const SeqWork q(a, b);
             const int n = shares_of(q, c);
-            v[0] = (uint32_t)q.units * n;
-            v[1] = n > 1 ? v[0] : 0;
+            const uint32_t all = (uint32_t)q.units * n;
+            v[0] = q.whole_units(a) ? all : 0;
+            v[1] = n > 1 ? all : 0;
             v[2] = n > 1 ? q.units : 0;
+            v[3] = all - v[0];
         }
         __syncthreads();
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < 4; ++k) {
             v[k] = wave_inclusive_scan(v[k]);
             if (lane == kWave - 1) s_sum[k][w] = v[k];
         }
         __syncthreads();
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < 4; ++k) {
             uint32_t before = base[k];
             for (int i = 0; i < kCutWaves; ++i) {
                 before += i < w ? s_sum[k][i] : 0;

@@ -422,7 +422,7 @@ ChunkLayout chunk_layout(const hgca_shape *s, int64_t n_tokens, int64_t cap)
     t.part_m = align_up(rows * s->head_dim * sizeof(float));
     t.part_l = t.part_m + align_up(rows * sizeof(float));
     t.cut = t.part_l + align_up(rows * sizeof(float));
-    t.total = t.cut + align_up((3 * (size_t)s->batch + 4) * sizeof(int32_t));
+    t.total = t.cut + align_up((4 * (size_t)s->batch + 5) * sizeof(int32_t));
     return t;
 }
 

@@ -391,7 +391,7 @@ struct ChunkArgs {
     int32_t slots, parts, units;          // per KV head: slots of the launch; those of them that leave partials, and units, at most
     int32_t target;            // shares that all units together aim at, per KV head
     int32_t least, whole;      // steps of a share at least, and steps up to which no unit is cut
-    int32_t *cut;              // more than 64 sequences: what chunk_cut_kernel worked out, [3 B + 4]
+    int32_t *cut;              // more than 64 sequences: what chunk_cut_kernel worked out, [4 B + 5]
     float *part_o, *part_m, *part_l;      // [parts, Hkv, kChunkRows (, d)]
 };
 hipError_t launch_chunk_attn(int dtype, int head_dim, const ChunkArgs &a, hipStream_t s);
