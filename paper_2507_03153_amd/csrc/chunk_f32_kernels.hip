@@ -48,6 +48,27 @@ __device__ __forceinline__ void load_half_step(const KvDev &kv, const BlockRows 
     }
 }
 
+// Takes infinities and NaN out of a half step's V rows, for all waves; true if there were any (settle_odd brings them to the rows that see them).
+// Called by waves of which some row does not see all of it; one that reads the rows before or while they change has sums that are not
+// finite.
+template <int D> __device__ __forceinline__ bool clean_half_stage(char *v_stage)
+{
+    constexpr int kPieces = kHalfStep * D / 4;
+    bool odd = false;
+#pragma unroll 4
+    for (int i = threadIdx.x % kWave; i < kPieces; i += kWave) {
+        const float4 x = *reinterpret_cast<const float4 *>(v_stage + 16 * i);
+        odd = odd || !(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w))) < INFINITY) || x.x != x.x || x.y != x.y || x.z != x.z || x.w != x.w;
+    }
+    if (!any_lane(odd)) return false;
+    auto finite = [](float x) { return fabsf(x) < INFINITY ? x : 0.f; };
+    for (int i = threadIdx.x % kWave; i < kPieces; i += kWave) {
+        float4 &x = *reinterpret_cast<float4 *>(v_stage + 16 * i);
+        x = make_float4(finite(x.x), finite(x.y), finite(x.z), finite(x.w));
+    }
+    return true;
+}
+
 template <int D, int MODE>
 __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArgs a)
 {
@@ -98,7 +119,8 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = floatx16{};
 
-    auto body = [&](const char *stage, int tok) {
+    auto body = [&](char *stage, int tok) {
+        const bool masked = !wave.all(tok, kHalfStep);           // uniform over the wave
         floatx16 c[1] = {floatx16{}};
 #pragma unroll
         for (int j = 0; j < KP; ++j) {
@@ -109,7 +131,8 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
             c[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, qop[j].w, c[0], 0, 0, 0);
         }
         map.apply(c, pos, tok + 4 * hw);
-        if (!wave.all(tok, kHalfStep)) {         // uniform over the wave
+        if (masked) {
+            met_odd = clean_half_stage<D>(stage + kV) || met_odd;
             const uint64_t seen = sees.mask(tok + 4 * hw);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
@@ -117,7 +140,6 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
         }
         run.update(c, map.k2, acc);
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        bool odd = false;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float p = __builtin_amdgcn_exp2f(fmaf(c[0][r], map.k2, run.shift));            // masked scores give 0
@@ -125,15 +147,11 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_f32_kernel(ChunkArg
             // piece 8 dt + n / 4 of row 8 (r / 4) + 4 hw + r % 4 lies at their exclusive or
             const char *const v = stage + kV + 8 * (r / 4) * S::kRowBytes + v_lane[r % 4];
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {    // infinities and NaN are taken out (settle_odd brings them to the rows that see them)
-                float x = *reinterpret_cast<const float *>(v + 128 * (dt ^ (r / 4) % (S::kPieces / 8)));
-                const bool bad = !(fabsf(x) < INFINITY);
-                odd = odd || bad;
-                x = bad ? 0.f : x;
+            for (int dt = 0; dt < DT; ++dt) {
+                const float x = *reinterpret_cast<const float *>(v + 128 * (dt ^ (r / 4) % (S::kPieces / 8)));
                 acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p, acc[dt], 0, 0, 0);
             }
         }
-        met_odd = met_odd || any_lane(odd);
         run.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
 
