@@ -130,11 +130,14 @@ __device__ __forceinline__ bool go_on(Walk &w, const Nodes &nodes, bool with_q, 
     return w.refused || w.c == 0.0;
 }
 
-// 16 bytes of a row as elements.
+// 16 bytes of a row as elements.  Rows begin where they do: an odd vocabulary's are not aligned to 16 bytes, which the loads do not ask for.
+struct __attribute__((packed, aligned(2))) AnyPiece {
+    uint4 raw;
+};
 template <typename T> struct Piece {
     static constexpr int kPer = Elem<T>::kPerLoad;
     uint4 raw;
-    __device__ __forceinline__ void load(const char *row, int i) { raw = load16(row + (int64_t)i * (int)sizeof(T)); }
+    __device__ __forceinline__ void load(const char *row, int i) { raw = reinterpret_cast<const AnyPiece *>(row + (int64_t)i * (int)sizeof(T))->raw; }
     __device__ __forceinline__ void expand(float *x) const { Elem<T>::expand(raw, x); }
     // below kAllSane if every element counts as it is: neither negative nor infinite or NaN
     __device__ __forceinline__ uint32_t look(uint32_t so_far) const {
@@ -159,14 +162,12 @@ struct Rest {
     double c;
     uint64_t gone;
     int vocab;
-    bool aligned;                                // both rows begin at 16 bytes' alignment
     __device__ __forceinline__ Rest(const VerifyArgs &a, int b, const Walk &w) {
         p = Nodes::target_row(a, b, w.node, sizeof(T));
         q = a.draft && w.c > 0.0 ? Nodes::draft_row(a, b, w.node, sizeof(T)) : nullptr;
         c = w.c;
         gone = a.draft ? 0 : w.gone;
         vocab = a.vocab;
-        aligned = ((uintptr_t)p | (uintptr_t)q) % 16 == 0;
     }
     __device__ __forceinline__ double one(const Nodes &nodes, int i) const {
         if (i >= vocab) return 0.0;
@@ -188,53 +189,42 @@ struct Rest {
         return gone ? segment_of<true>(nodes, seg) : segment_of<false>(nodes, seg);
     }
     template <bool GONE> __device__ __forceinline__ double segment_of(const Nodes &nodes, int seg) const {
-        const int lane = threadIdx.x % kWave, first = seg * kVerifySegment;
+        constexpr int kPer = Piece<T>::kPer, kRounds = kVerifySegment / (kPer * kWave);
+        const int lane = threadIdx.x % kWave, i0 = seg * kVerifySegment + kPer * lane;
         double s[4] = {0.0, 0.0, 0.0, 0.0};
-        bool done = false;
-        if (aligned && first + kVerifySegment <= vocab) {        // uniform over the wave
-            constexpr int kPer = Piece<T>::kPer, kRounds = kVerifySegment / (kPer * kWave);
-            Piece<T> pv[kRounds], pd[kRounds];
-            const int i0 = first + kPer * lane;
+        if (vocab < kPer) return wave_sum64(one(nodes, lane));
+        // The last pieces of a row begin where they end with it: `skip` of their elements belong to the piece before.
+        const bool whole = (seg + 1) * kVerifySegment <= vocab;  // uniform over the wave
+        auto at = [&](int r) { return whole ? i0 + r * kPer * kWave : min(i0 + r * kPer * kWave, vocab - kPer); };
+        Piece<T> pv[kRounds], pd[kRounds];
 #pragma unroll
-            for (int r = 0; r < kRounds; ++r) pv[r].load(p, i0 + r * kPer * kWave);
-            if (q) {
+        for (int r = 0; r < kRounds; ++r) pv[r].load(p, at(r));
+        if (q) {
 #pragma unroll
-                for (int r = 0; r < kRounds; ++r) pd[r].load(q, i0 + r * kPer * kWave);
-            } else {
+            for (int r = 0; r < kRounds; ++r) pd[r].load(q, at(r));
+        } else {
 #pragma unroll
-                for (int r = 0; r < kRounds; ++r) pd[r].raw = make_uint4(0, 0, 0, 0);
-            }
-            uint32_t most = 0;
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) most = pd[r].look(pv[r].look(most));
-            if (__builtin_amdgcn_ballot_w64(most >= kAllSane) == 0) {            // else element by element
-                done = true;
-#pragma unroll
-                for (int r = 0; r < kRounds; ++r) {
-                    float v[kPer], d[kPer];
-                    pv[r].expand(v);
-                    pd[r].expand(d);
-#pragma unroll
-                    for (int k = 0; k < kPer; ++k) s[k % 4] += left<GONE>(nodes, v[k], d[k], i0 + r * kPer * kWave + k);
-                }
-            }
+            for (int r = 0; r < kRounds; ++r) pd[r].raw = make_uint4(0, 0, 0, 0);
         }
-        if (!done) {                             // rows of any alignment, the last segment
-            constexpr int kRounds = 16;
-            for (int i0 = first + lane; i0 < first + kVerifySegment; i0 += kRounds * kWave) {
-                float v[kRounds], d[kRounds];
+        uint32_t most = 0;
 #pragma unroll
-                for (int r = 0; r < kRounds; ++r) {
-                    const int i = min(i0 + r * kWave, vocab - 1);
-                    v[r] = element<T>(p, i);
-                    d[r] = q ? element<T>(q, i) : 0.f;
-                }
+        for (int r = 0; r < kRounds; ++r) most = pd[r].look(pv[r].look(most));
+        const bool all_sane = __builtin_amdgcn_ballot_w64(most >= kAllSane) == 0;
 #pragma unroll
-                for (int r = 0; r < kRounds; ++r) {
-                    const int i = i0 + r * kWave;
-                    s[r % 4] += i < vocab ? left<GONE>(nodes, v[r], d[r], i) : 0.0;
+        for (int r = 0; r < kRounds; ++r) {
+            float v[kPer], d[kPer];
+            pv[r].expand(v);
+            pd[r].expand(d);
+            if (!(all_sane && whole)) {          // uniform over the wave
+                const int skip = i0 + r * kPer * kWave - at(r);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    v[k] = k < skip ? 0.f : sane(v[k]);
+                    d[k] = sane(d[k]);
                 }
             }
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) s[k % 4] += left<GONE>(nodes, v[k], d[k], at(r) + k);
         }
         return wave_sum64((s[0] + s[1]) + (s[2] + s[3]));
     }
