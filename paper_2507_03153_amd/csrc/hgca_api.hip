@@ -1976,13 +1976,13 @@ int hgca_verify_drafts(int32_t batch, int32_t n_drafts, int32_t vocab, int32_t p
     a.batch = batch;
     a.n = n_drafts;
     a.vocab = vocab;
-    // Launches.  Rows of a segment for each wave of a sequence's workgroup: it does everything (five tokens, 1 x 2000 elements 13.9 -> 10.8 us, 8 x
-    // 32 000 15.5 : 15.8, 256 x 32 000 26.9 -> 25.6; 8 x 64 000 14.9 : 17.6).  Longer ones: a launch over the chip for the first sums.  After a refusal
-    // only a tree has another token to try, and with it another pass over the rows: by the sequence's own workgroup it takes 13 us for 128 000
-    // elements, by a launch 8 us for 32 such sequences, and 3 us where no sequence needs it; so launches for long rows, more of them where the
-    // worst of many sequences counts.  Trees of 16, 1 : 3 : 4 launches: 8 sequences 39 : 28 : 31 us, 32 62 : 44 : 40, 128 92 : 76 : 72, all accepted
-    // 16 : 19 : 23; 8 x 64 000, 1 : 3, 25 : 25, all accepted 14 : 19.
-    a.passes = vocab <= kVerifyAlone * kVerifySegment ? 0 : !parents || n_drafts < 3 || vocab <= 32 * kVerifySegment ? 1 : batch < 16 ? kVerifyPasses - 1 : kVerifyPasses;
+    // Launches (times in a captured graph, us).  Rows of two segments for each wave of a sequence's workgroup: it does everything (five tokens, 8 x
+    // 16 000 elements 9.3 : 10.5, 8 x 32 000 10.9 : 10.5, 256 x 32 000 17.0 : 19.7, 8 x 64 000 13.9 : 10.8; eager calls save a launch besides).  Longer ones: a
+    // launch over the chip for the first sums.  After a refusal only a tree has another token to try, and with it another pass over the rows,
+    // which a launch does in a fraction of the time that one workgroup takes; 2 us where no sequence needs it.  So launches for long rows, more of them
+    // where the worst of many sequences counts.  Trees of 16, 1 : 2 : 3 : 4 launches: 8 x 64 000 18.8 : 15.4 : 17.7 : 19.2, all accepted 10.0 : 11.7 : 13.5 : 15.3;
+    // 8 x 128 000 30 : 22 : 19 : 22, 32 x 47 : 40 : 31 : 28, 128 x 73 : 68 : 58 : 57, all accepted (32 x) 14 : 15 : 17 : 19.
+    a.passes = vocab <= kVerifyAlone * kVerifySegment ? 0 : !parents || n_drafts < 3 ? 1 : vocab <= 64 * kVerifySegment ? 2 : batch < 16 ? 3 : kVerifyPasses;
     a.walks = static_cast<VerifyWalk *>(ws);
     a.sums = reinterpret_cast<double *>(a.walks + (size_t)kVerifyPasses * batch);
     return from_hip(launch_verify_drafts(p_dtype, a, static_cast<hipStream_t>(hip_stream)));

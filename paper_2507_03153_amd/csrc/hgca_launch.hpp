@@ -364,8 +364,8 @@ struct VerifyArgs {
     int32_t batch, n, vocab;
     int32_t passes;            // launches that form sums, up to kVerifyPasses; 0: rows of kVerifyAlone segments at most, one launch for all
 };
-constexpr int kVerifySegment = 2048;      // elements of a row that one partial sum covers
-constexpr int kVerifyAlone = 16;          // segments that one workgroup goes through without other launches
+constexpr int kVerifySegment = 1024;      // elements of a row that one partial sum covers
+constexpr int kVerifyAlone = 32;          // segments that one workgroup goes through without other launches
 constexpr int kVerifyPasses = 4;          // launches that form sums, at most
 hipError_t launch_verify_drafts(int dtype, const VerifyArgs &a, hipStream_t s);
 

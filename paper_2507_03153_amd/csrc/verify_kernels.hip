@@ -12,12 +12,12 @@
 // the pass is bound by memory all the same.
 //
 // A pass reads two rows of the vocabulary for each sequence, and that and the latency of one dependent load after the other bound it: parents and
-// tokens, elements of the rows, the rows.  So short rows are one workgroup's, a segment a wave, in one launch; for longer ones every workgroup
+// tokens, elements of the rows, the rows.  So short rows are one workgroup's, two segments a wave, in one launch; for longer ones every workgroup
 // of a launch over the chip finds for itself where the walk first stops (single elements), and leaves the sums of its segments; launches like it
 // follow for trees with long rows, in which other refusals come next, and a last one, a workgroup per sequence, goes through what is
-// left and draws, for which it reads one more segment.  Measured: 8 x 5 tokens, 32 000 elements, fp32, 15.5 us as a call, 32 trees of 16 over 128 000
-// 40.4 (12.4 for the first sums, 33 MB, 7.9 and less for the next three, 7.7 for the rest).  Of a pass's arithmetic the conversions to fp64 take
-// most, 56 cycles an element and wave in all, 1.5 us of those 7.9.
+// left and draws, for which it reads one more segment.  Measured in a captured graph: 8 x 5 tokens, 32 000 elements,
+// fp32, 10.9 us, 32 trees of 16 over 128 000 28.3 (33 MB a pass; 46.7 with one launch before the last), over 128 003, whose rows are of all
+// alignments, 30.1.  Of a pass's arithmetic the conversions to fp64 take most, 56 cycles an element and wave in all.
 #include <algorithm>
 
 #include "hgca_launch.hpp"
@@ -131,13 +131,14 @@ __device__ __forceinline__ bool go_on(Walk &w, const Nodes &nodes, bool with_q, 
 }
 
 // 16 bytes of a row as elements.  Rows begin where they do: an odd vocabulary's are not aligned to 16 bytes, which the loads do not ask for.
-struct __attribute__((packed, aligned(2))) AnyPiece {
-    uint4 raw;
-};
+typedef uint32_t AnyPiece __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T> struct Piece {
     static constexpr int kPer = Elem<T>::kPerLoad;
     uint4 raw;
-    __device__ __forceinline__ void load(const char *row, int i) { raw = reinterpret_cast<const AnyPiece *>(row + (int64_t)i * (int)sizeof(T))->raw; }
+    __device__ __forceinline__ void load(const char *row, int i) {
+        const AnyPiece x = *reinterpret_cast<const AnyPiece *>(row + (int64_t)i * (int)sizeof(T));
+        raw = make_uint4(x[0], x[1], x[2], x[3]);
+    }
     __device__ __forceinline__ void expand(float *x) const { Elem<T>::expand(raw, x); }
     // below kAllSane if every element counts as it is: neither negative nor infinite or NaN
     __device__ __forceinline__ uint32_t look(uint32_t so_far) const {
@@ -183,8 +184,9 @@ struct Rest {
         for (uint64_t m = gone; m; m &= m - 1) out = out || i == __builtin_amdgcn_readlane(nodes.token, __builtin_ctzll(m));
         return out ? 0.0 : (double)v;
     }
-    // Sum of a segment, in every lane of the wave.  All of the lane's loads are under way before the first is waited for: a wave has a segment to
-    // itself, and one load after the other would take eight times memory's latency (a pass of one workgroup over 128 000 elements 17 us).
+    // Sum of a segment, in every lane of the wave.  All of the lane's loads are under way before the first is waited for: one load
+    // after the other would take so many times memory's latency.  (Segments of 2048: 64 registers of loads, which the walk's kernel does not have,
+    // 30.9 : 28.7 us for 32 trees over 128 000.)
     __device__ __forceinline__ double segment(const Nodes &nodes, int seg) const {
         return gone ? segment_of<true>(nodes, seg) : segment_of<false>(nodes, seg);
     }
