@@ -234,3 +234,26 @@ def test_refusals_over_a_large_vocabulary(gpu, dtype, B, with_q):
     print(f"\n[case] {dtype} B={B} q={with_q}: cnt {want[1].tolist()}, margin {want[3]:.1e}", flush=True)
     for a, b in zip(got, want):
         assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2, 3, 4, 5, 7, 8, 9, 250, 1022, 1023, 1024, 1025, 1027, 2050, 33001, 66005])
+def test_ends_of_rows_and_odd_elements(gpu, dtype, V):
+    """Rows of every alignment, ends inside a load, elements that do not count among them; draws from the first to the last token of the row, with a chain
+    that stops anywhere in it."""
+    rng = np.random.default_rng(V)
+    B, n = 24, 4
+    target, draft, tokens, _, u, u_next = drafted(rng, B, n, V, False, dtype, sharp=1.0)
+    for x in (target, draft):
+        where = rng.random(x.shape) < min(0.1, 20 / V)
+        x[where] = rng.choice(np.array([-1.0, -0.0, np.inf, -np.inf, np.nan, -1e-30], np.float32), int(where.sum()))
+    target[:, :, -1] = 0.25                      # drawn by the numbers near 1
+    u[:, 1:] = np.where(rng.random((B, n - 1)) < 0.5, 0.999, u[:, 1:])
+    u_next[:8] = 1 - 2.0 ** -np.arange(1, 9)
+    u_next[8] = 0
+    for q in (draft, None):
+        want = so.verify(target, q, tokens, u, u_next)
+        got = call(gpu, target, q, tokens, u, u_next, None, dtype, wide=int(rng.integers(0, 4)))
+        print(f"\n[case] V={V} {dtype}: cnt {np.bincount(want[1]).tolist()}, last token {int((want[2] == V - 1).sum())}, margin {want[3]:.1e}", flush=True)
+        for a, b in zip(got, want):
+            assert np.array_equal(a, b)
