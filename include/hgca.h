@@ -801,7 +801,8 @@ int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_s
  * bf16 (2^-9 of a weight, at random: as much again as O's own rounding), the sum that divides them does not.
  * sm_scale must be positive and finite (1e-30 at least with slopes), scaled scores at most 2^126 in magnitude, softcap
  * finite; tier->cap is at most 2^30.  Results do not depend on other calls and repeat bit for
- * bit; where a sequence is cut into shares does depend on the batch.  ws needs
+ * bit; where a sequence is cut into shares does depend on the batch, n_tokens and tier->cap.
+ * ws needs
  * hgca_chunk_workspace_bytes(shape, n_tokens, tier->cap), which also serves fewer tokens and
  * smaller capacities.  o_out, lse_out and q must not overlap (refused). */
 enum { HGCA_CHUNK_CAUSAL = 1 };
