@@ -374,3 +374,55 @@ def test_captured_with_many_sequences(gpu):
         assert torch.equal(outs[0][0][:at], outs[1][0][:at]) and torch.equal(outs[0][1][:at], outs[1][1][:at])
         O, L = so.chunk(Q[:at], cu.tolist(), K, V, n, 0.125, window=500)
         check(outs[0][0][:at], outs[0][1][:at], O, L, *bounds("bf16", "f32", Q[:at], K, V, n, 0.125, T=T), "f32")
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_calls_at_random(gpu, seed):
+    """Types, heads, blocks, counts, lengths, masks and scores as they come; single tokens and whole prompts in one call, up to 100 sequences, tiers that are cut and
+    that are not; in half of them values of V that are infinite or NaN, which are in the columns of the rows that see them and nowhere else."""
+    torch, hgca = gpu
+    rng = np.random.default_rng(seed)
+    pick = lambda *x: x[int(rng.integers(len(x)))]
+    dtype, d, Hkv, group, B = pick("f32", "bf16"), pick(64, 128), pick(1, 2, 8), pick(1, 4, 8), pick(1, 3, 9, 66, 100)
+    out, block, Hq = "f32" if dtype == "f32" else pick("f32", "bf16"), pick(0, 16, 48, 128), Hkv * group
+    T = pick(64, 300, 700, 1500) if B < 20 else pick(64, 200, 700)
+    counts = [int(x) for x in rng.integers(0, pick(1, 4, 20, 150) + 1 if B < 20 else 5, B)]
+    counts[0] = pick(1, 30, min(600, T, 16384 // Hq))
+    lens = [min(T, max(int(x), c)) if rng.random() < 0.8 else int(x) for x, c in zip(rng.integers(0, T + 1, B), counts)]
+    opt = dict(causal=rng.random() < 0.8)
+    if rng.random() < 0.4:
+        opt["window"] = pick(1, 17, 64, 300, 5000)
+    if rng.random() < 0.4:
+        opt["cap"] = pick(5.0, 30.0, 50.0)
+    if rng.random() < 0.4:
+        opt["slopes"] = slopes_of(Hq)
+    if rng.random() < 0.4:
+        opt["prefix_lens"] = rng.integers(0, T, B)
+    if rng.random() < 0.4:
+        opt["first"] = np.concatenate([np.sort(rng.integers(-3, L + 2, n)) for n, L in zip(counts, lens)])
+    r, q, K, V = inputs(seed, dtype, counts, Hq, Hkv, d, T, pick(1.0, 3.0))
+    clean = V.copy()
+    odd = [(int(rng.integers(B)), int(rng.integers(Hkv)), int(rng.integers(T)), int(rng.integers(d)), pick(np.inf, -np.inf, np.nan)) for _ in range(5)] if seed % 2 else []
+    for b, h, t, c, x in odd:
+        V[b, h, t, c], clean[b, h, t, c] = x, 0
+    print(f"\n[case] {dtype} {out} d={d} {Hq}/{Hkv} B={B} T={T} block={block} tokens={sum(counts)} {sorted(opt)} odd={len(odd)}", flush=True)
+    scale = float(np.float32(d ** -0.5))
+    cu = np.concatenate([[0], np.cumsum(counts)])
+    shape = hgca.Shape(hgca.F32 if dtype == "f32" else hgca.BF16, B, Hq, Hkv, d, scale)
+    o, lse = call(gpu, shape, put(torch, q, dtype), cu, tier_of(gpu, r, dtype, K, V, lens, block), out, pad=3, wide=pick(0, d), **dict(opt))
+    kw = dict(opt)
+    prefix = kw.pop("prefix_lens", None)
+    O, L = so.chunk(q, cu, K, clean, lens, scale, prefix=prefix, **kw)
+    kinds = np.zeros(O.shape, int)
+    for b, h, t, c, _ in odd:
+        if t >= lens[b]:
+            continue
+        rows = slice(cu[b], cu[b + 1])
+        seen = so.sees(counts[b], lens[b], opt["causal"], opt.get("window", 0), 0 if prefix is None else int(prefix[b]),
+                       None if "first" not in opt else opt["first"][rows])[:, t]
+        x = V[b, h, t, c]                        # (a place may have been drawn twice)
+        kinds[rows, h * group:(h + 1) * group, c] |= np.where(seen, 1 if x == np.inf else 2 if x == -np.inf else 4, 0)[:, None]
+    got = o.double().cpu().numpy()
+    assert np.array_equal(got == np.inf, kinds == 1) and np.array_equal(got == -np.inf, kinds == 2) and np.array_equal(np.isnan(got), kinds > 2)
+    o = torch.where(torch.from_numpy(kinds > 0).to(DEV), torch.zeros_like(o), o)
+    check(o, lse, np.where(kinds > 0, 0, O), L, *bounds(dtype, out, q, K, clean, lens, scale, opt.get("cap", 0.0), opt.get("slopes"), T), out, dtype)
