@@ -277,30 +277,44 @@ enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
 
 // tanh x.  Up to kTanhNear it is x P(x^2), P fitted to the least largest relative error (3.0e-7 of degree 4, 1.4e-8 of degree 5); beyond, 1 - 2 / (1 +
 // e^2x), whose rounding is then small against the result.  The factors before and behind are in P's coefficients: six instructions a
-// score.  (Four more for the other form, two of them slow; steps in which no score is beyond are the rule.)
+// score.  (Four more for the other form, two of them slow; steps in which no score is beyond are the rule.)  The last coefficient has the tenth power
+// of sm_scale / cap: where it would leave the range of ordinary numbers (heads of 128, scale 1 / sqrt(d): caps above 260 and below 2e-5) the factors
+// stay outside.  The one behind P is then the score's own, in * out as one number, so that no cap is too large: P is 1 where the cap does nothing.
 constexpr float kTanhNear = 0.7f;
 template <bool FINE> struct TanhNear {
     static constexpr int kTerms = FINE ? 6 : 5;
     float a[kTerms];
-    bool usable;                                 // the coefficients are ordinary numbers
-    __device__ __forceinline__ TanhNear() : usable(false) {}
-    __device__ __forceinline__ TanhNear(float in, float out) {   // of out * tanh(in * x)
+    float before, behind;                        // 1 where they are in the coefficients
+    __device__ __forceinline__ TanhNear() {}
+    __device__ __forceinline__ TanhNear(float in, float in_out) {        // of in_out / in * tanh(in * x)
         constexpr float kFine[6] = {1.f, -0.33333131671f, 0.13328415155f, -0.05352601036f, 0.02002445795f, -0.00508833630f};
         constexpr float kCoarse[6] = {0.99999970198f, -0.33330214024f, 0.13281112909f, -0.05083623528f, 0.01377371047f, 0.f};
-        float power = in * out;
+        float power = in_out;
 #pragma unroll
         for (int i = 0; i < kTerms; ++i) {
-            a[i] = uniform((FINE ? kFine[i] : kCoarse[i]) * power);
+            a[i] = (FINE ? kFine[i] : kCoarse[i]) * power;
             power *= in * in;
         }
-        usable = in >= 1e-4f && in <= 1e4f;      // (in^11 is one)
+        // they are a geometric series but for factors around 1: the first and the last say for all
+        auto ordinary = [](float x) { return fabsf(x) >= 1.2e-38f && fabsf(x) <= 1e37f; };
+        const bool folded = ordinary(a[0]) && ordinary(a[kTerms - 1]);
+#pragma unroll
+        for (int i = 0; i < kTerms; ++i) a[i] = uniform(folded ? a[i] : FINE ? kFine[i] : kCoarse[i]);
+        before = uniform(folded ? 1.f : in);
+        behind = uniform(folded ? 1.f : in_out);
     }
-    __device__ __forceinline__ float operator()(float x) const {
-        const float z = x * x;
+    __device__ __forceinline__ bool folded() const { return before == 1.f && behind == 1.f; }
+    __device__ __forceinline__ float polynomial(float z) const {
         float p = a[kTerms - 1];
 #pragma unroll
         for (int i = kTerms - 2; i >= 0; --i) p = fmaf(z, p, a[i]);
-        return x * p;
+        return p;
+    }
+    // folded() only; the same number as operator()
+    __device__ __forceinline__ float quick(float x) const { return x * polynomial(x * x); }
+    __device__ __forceinline__ float operator()(float x) const {
+        const float t = x * before;
+        return x * behind * polynomial(t * t);
     }
 };
 __device__ __forceinline__ float tanh_far(float x) {
@@ -323,7 +337,7 @@ template <int MODE, bool FINE> struct ScoreMap {
         kx = kCaps ? uniform(a.sh.sm_scale / a.cap) : 0.f;
         cap2 = uniform(a.cap * kTreeLog2e);
         k2 = kCaps ? 1.f : scale2;
-        if (kCaps) near_zero = TanhNear<FINE>(kx, cap2);
+        if (kCaps) near_zero = TanhNear<FINE>(kx, scale2);
     }
     // The N values of a lane, get(i) and set(i, x): products with tokens first + off(i) of a row at position pos.
     template <int N, typename Get, typename Set, typename Off>
@@ -339,14 +353,14 @@ template <int MODE, bool FINE> struct ScoreMap {
             float most = 0.f;
 #pragma unroll
             for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(get(i)));
-            if (near_zero.usable && !any_lane(!(most * kx <= kTanhNear))) {          // uniform over the wave
+            if (near_zero.folded() && !any_lane(!(most * kx <= kTanhNear))) {        // uniform over the wave
 #pragma unroll
-                for (int i = 0; i < N; ++i) set(i, biased(near_zero(get(i)), i));
+                for (int i = 0; i < N; ++i) set(i, biased(near_zero.quick(get(i)), i));
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const float x = get(i) * kx;
-                    set(i, biased(near_zero.usable && fabsf(x) <= kTanhNear ? near_zero(get(i)) : cap2 * tanh_far(x), i));
+                    set(i, biased(fabsf(x) <= kTanhNear ? near_zero(get(i)) : cap2 * tanh_far(x), i));
                 }
             }
         }
