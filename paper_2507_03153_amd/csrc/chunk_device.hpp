@@ -275,7 +275,7 @@ struct GranuleRows {
 // units of ln 2.  kBiased: the product less slope / sm_scale * distance, kCapped + kBiased: the capped score less slope * distance.
 enum { kPlainScores = 0, kCapped = 1, kBiased = 2 };
 
-// tanh x.  Up to kTanhNear it is x P(x^2), P fitted to the least largest relative error (3.0e-7 of degree 4, 1.4e-8 of degree 5); beyond, 1 - 2 / (1 +
+// tanh x.  Up to kTanhNear it is x P(x^2), P fitted to the least largest relative error (3.1e-7 of degree 4, 2.7e-8 of degree 5); beyond, 1 - 2 / (1 +
 // e^2x), whose rounding is then small against the result.  The factors before and behind are in P's coefficients: six instructions a
 // score.  (Four more for the other form, two of them slow; steps in which no score is beyond are the rule.)  The last coefficient has the tenth power
 // of sm_scale / cap: where it would leave the range of ordinary numbers (heads of 128, scale 1 / sqrt(d): caps above 260 and below 2e-5) the factors
