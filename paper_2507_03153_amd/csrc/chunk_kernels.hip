@@ -14,8 +14,9 @@
 // 2.0 GHz of 2.4 on long prompts: two of 4096 tokens, 64 / 8 heads, 562 GFLOP, 645 to 680 us, 830 to 870 TFLOP/s, matrix units busy 37 % of the
 // cycles at 2.4, vector units 48 %.  Capped scores cost seven instructions each (four prompts of 864 tokens seeing 4096: 306 us, 392 capped).  32 rows
 // per wave: with 64 the compiler has no registers left (640 -> 995 us); four waves per workgroup, two workgroups per compute unit: eight waves and
-// 256 rows read K and V half as often (661 : 679).  Weights enter the second product as one bf16 part for bf16 O, whose rounding is as large, as
-// three for fp32 O.
+// 256 rows read K and V half as often (661 : 679).  (These with weights of one part.)  Weights enter the second product as two bf16 parts for bf16 O, 16 bits, far
+// below its rounding, as three for fp32 O.  One part, 2^-9 of a weight and with it as much error again as the rounding of O, is there for callers that ask for it: prompts
+// 825 -> 670 us, mixed step 515 -> 424, documents 515 -> 438; single tokens, whose bound is memory, 169 : 169.
 #include <algorithm>
 
 #include "chunk_few.hpp"
@@ -425,9 +426,12 @@ hipError_t launch_chunk_rows_bf16(int head_dim, const ChunkArgs &a, hipStream_t 
         else if (mode == kBiased) hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kBiased>), grid, block, 0, s, a);   \
         else hipLaunchKernelGGL((chunk_attn_kernel<D, PP, kCapped + kBiased>), grid, block, 0, s, a);              \
     } while (0)
-    if (head_dim == 64 && a.o_bf16) HGCA_CHUNK(64, 1);
+    const int parts = !a.o_bf16 ? 3 : a.one_part ? 1 : 2;
+    if (head_dim == 64 && parts == 1) HGCA_CHUNK(64, 1);
+    else if (head_dim == 64 && parts == 2) HGCA_CHUNK(64, 2);
     else if (head_dim == 64) HGCA_CHUNK(64, 3);
-    else if (a.o_bf16) HGCA_CHUNK(128, 1);
+    else if (parts == 1) HGCA_CHUNK(128, 1);
+    else if (parts == 2) HGCA_CHUNK(128, 2);
     else HGCA_CHUNK(128, 3);
 #undef HGCA_CHUNK
     return hipGetLastError();

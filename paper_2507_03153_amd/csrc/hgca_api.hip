@@ -1877,7 +1877,7 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
     int rc = check_shape(shape);
     if (rc != HGCA_OK) return rc;
     if ((rc = check_view(shape, tier, true)) != HGCA_OK) return rc;
-    if (n_tokens < 0 || (flags & ~HGCA_CHUNK_CAUSAL) || window < 0 || !(softcap >= 0.f) || softcap > 2.0e38f) return HGCA_ERR_INVALID_ARG;
+    if (n_tokens < 0 || (flags & ~(HGCA_CHUNK_CAUSAL | HGCA_CHUNK_ONE_PART_P)) || window < 0 || !(softcap >= 0.f) || softcap > 2.0e38f) return HGCA_ERR_INVALID_ARG;
     if (!(shape->sm_scale > 0.f) || shape->sm_scale > 2.0e38f) return HGCA_ERR_INVALID_ARG;
     if (slopes && shape->sm_scale < 1e-30f) return HGCA_ERR_UNSUPPORTED;         // (slopes are divided by it)
     if (softcap > 0.f && !(shape->sm_scale / softcap > 0.f && shape->sm_scale / softcap < 2.0e38f)) return HGCA_ERR_INVALID_ARG;
@@ -1909,6 +1909,7 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
     a.prefix = prefix_lens;
     a.first = first;
     a.o_bf16 = o_dtype == HGCA_BF16;
+    a.one_part = flags & HGCA_CHUNK_ONE_PART_P ? 1 : 0;
     a.o = o_out;
     a.lse = lse_out;
     a.slots = (int32_t)t.slots;

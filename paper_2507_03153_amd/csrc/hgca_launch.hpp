@@ -386,6 +386,7 @@ struct ChunkArgs {
     const int32_t *prefix;     // [B] or null
     const int32_t *first;      // [T] or null
     int32_t o_bf16;
+    int32_t one_part;          // bf16 O of bf16 inputs: weights as one bf16 part, else two
     void *o;                   // [T, Hq, d]
     float *lse;                // [T, Hq]
     int32_t slots, parts, units;          // per KV head: slots of the launch; those of them that leave partials, and units, at most

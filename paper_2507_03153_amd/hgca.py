@@ -838,7 +838,7 @@ def kv8_attn(shape: Shape, q, tier: Kv8Tier, o_out, lse_out, ws, stream=None) ->
 
 # ---- a server's step: requests of different size, packed one behind the other ----
 
-CHUNK_CAUSAL = 1
+CHUNK_CAUSAL, CHUNK_ONE_PART_P = 1, 4
 
 
 @dataclass
@@ -931,11 +931,12 @@ def chunk_workspace(shape: Shape, n_tokens: int, max_tokens: int, device) -> tor
 
 
 def chunk_attn(shape: Shape, q, cu, tier: Tier, o_out, lse_out, ws, causal: bool = True, window: int = 0, cap: float = 0.0, slopes=None,
-               prefix_lens=None, first=None, stream=None) -> None:
+               prefix_lens=None, first=None, one_part_p: bool = False, stream=None) -> None:
     """Attention of packed new tokens q [T,Hq,d] (may be parts of wider rows), sequence b's in rows cu[b] .. cu[b+1] - 1 (int32 [B+1]),
     which are the last tokens of the tier.  A row sees tokens below prefix_lens[b] (int32 [B]) and those from first[t] (int32 [T]) on that
     are no later than itself (causal) and less than `window` tokens back (0: any); scores are capped to cap * tanh(s / cap) (0: not) and
-    lose slopes[h] (fp32 [Hq]) per token of distance.  o_out [T,Hq,d] fp32 or bf16, lse_out [T,Hq] fp32."""
+    lose slopes[h] (fp32 [Hq]) per token of distance.  o_out [T,Hq,d] fp32 or bf16, lse_out [T,Hq] fp32; one_part_p: for bf16 o_out weights of
+    8 bits instead of 16, faster for prompts."""
     B, Hq, Hkv, d, dt = _heads(shape)
     dev, T = _gpu_of(q), q.shape[0]
     qs = _packed("q", q, dt, (T, Hq, d), dev)
@@ -951,7 +952,7 @@ def chunk_attn(shape: Shape, q, cu, tier: Tier, o_out, lse_out, ws, causal: bool
         _need("first", first, torch.int32, (T,), dev)
     kv = _tier_view(tier, B, Hkv, d, dt, dev)
     _launch("hgca_chunk_attn", stream, dev, ctypes.byref(shape), q.data_ptr(), qs, cu.data_ptr(), T, ctypes.byref(kv),
-            CHUNK_CAUSAL if causal else 0, int(window), cap, _ptr(slopes), _ptr(prefix_lens), _ptr(first), o_out.data_ptr(),
+            (CHUNK_CAUSAL if causal else 0) | (CHUNK_ONE_PART_P if one_part_p else 0), int(window), cap, _ptr(slopes), _ptr(prefix_lens), _ptr(first), o_out.data_ptr(),
             _dtype_code(o_out), lse_out.data_ptr(), ws.data_ptr(), ws.numel())
 
 
