@@ -1839,7 +1839,7 @@ int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_s
     if (ks < token || vs < token || ks % 16 != 0 || vs % 16 != 0) return HGCA_ERR_INVALID_ARG;
     // offsets stay far from 2^63, threads of the grid below 2^32
     if (ks > (int64_t(1) << 42) / n_tokens || vs > (int64_t(1) << 42) / n_tokens || n_tokens > 1 << 23) return HGCA_ERR_UNSUPPORTED;
-    const int64_t rows = n_slots / per_block * per_block * token;
+    const int64_t rows = (n_slots + per_block - 1) / per_block * per_block * token;      // (the heads of a block lie one behind the other)
     if (Range(tier->k, rows).meets(Range(tier->v, rows))) return HGCA_ERR_INVALID_ARG;
     for (const void *out : {tier->k, tier->v}) {
         const Range to(out, rows);
@@ -1859,7 +1859,7 @@ int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_s
     a.n_kv_heads = shape->n_kv_heads;
     a.row_bytes = (int32_t)row;
     a.per_block = (int32_t)per_block;
-    a.n_slots = (int32_t)(n_slots / per_block * per_block);      // whole blocks
+    a.n_slots = (int32_t)n_slots;
     return from_hip(launch_kv_write(a, static_cast<hipStream_t>(hip_stream)));
 }
 
