@@ -69,7 +69,7 @@ template <typename Shares> __device__ __forceinline__ int share_steps(const Chun
     const float rows = (float)min(max(a.cu[a.sh.batch], 0), a.n_tokens) * (float)a.sh.group;
     if (longest <= 2 * a.whole && 2.f * units >= target && rows >= (float)(kChunkRows / 2) * units) return longest;
     int c = max((int)(work / target), a.least);
-    if (units > target) return max((int)(work / target * 1.0001f) + 1, a.least);
+    if (units > target) return max((int)fminf(work / target * 1.0001f, (float)longest) + 1, a.least);
     if (c >= longest || shares(c) <= target) return c;
     // shares(c) <= work / c + units, and one share each is few enough
     int enough = units < target ? (int)min(work / (target - units) * 1.0001f + 1.f, (float)longest) : longest;
