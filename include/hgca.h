@@ -820,8 +820,15 @@ int hgca_chunk_attn(const hgca_shape *shape, const void *q, int64_t q_token_stri
                     void *ws, size_t ws_bytes, void *hip_stream);
 
 /* Which of n_drafts drafted tokens per sequence stay, by the target's probabilities, and the
- * token that follows them (speculative sampling: what comes out is distributed as the
- * target's own samples).  tokens is device int32 [B, n_drafts]; drafted token 0, the root, is taken
+ * token that follows them (speculative sampling).  What comes out is distributed as the
+ * target's own samples where rows sum to 1 and the tokens that follow a token are independent
+ * draws, with replacement, from its row of draft, or were chosen without chance (the draft's
+ * likeliest ones, say) and draft is NULL.  Tokens drawn without replacement, or the likeliest
+ * ones given together with draft, come out biased.  Rows are taken as they are, also where
+ * they do not sum to 1 (large vocabularies rounded to bf16): before the first refusal at a
+ * token the target's sum counts as 1, and an accepted token is as far from the target's
+ * distribution as the two sums are from 1.
+ * tokens is device int32 [B, n_drafts]; drafted token 0, the root, is taken
  * as accepted (the token sampled last).  parents (device int32 [B, n_drafts], NULL: i - 1) names
  * the token that each one follows; a token whose parent is not an earlier one, or which
  * is not in [0, vocab), is in no tree.  target[b, i] and draft[b, i] are the distributions
