@@ -760,7 +760,7 @@ enum {
  * (HGCA_CACHE_TOKENS_FULL); what a sequence without room for it in its row asks for does
  * not count.  The k-th granted block, in order of the sequences, is
  * free_blocks[*free_count - 1 - k].  Entries of a row behind those in use stay as they
- * are.  block_size of 1 and more. */
+ * are.  block_size of 1 and more.  A batch of 0 writes nothing. */
 int hgca_kv_plan(const hgca_block_state *state, const int32_t *n_new, int32_t max_tokens,
                  int32_t *cu_out, int32_t *positions_out, int32_t *slots_out, void *hip_stream);
 
