@@ -311,9 +311,10 @@ __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
     int32_t *const lists = a.cut + 1;            // four lists of B + 1 beginnings: slots, partials, units with several shares, later slots
     if (tid == 0) a.cut[0] = c;
     if (tid < 4) lists[tid * (B + 1)] = 0;
-    // Beginnings that do not ascend may count the same rows for every sequence: sums that no 32 bits hold, which end at kMost.
-    constexpr uint64_t kMost = 1u << 30;
-    uint64_t base[4] = {0, 0, 0, 0};
+    // Beginnings that do not ascend may count the same rows for every sequence: sums that no 32 bits hold.  A wave's end at kMost, which is beyond any slot
+    // of a launch (2^23 at most), those before at 16 of them.  (A sequence has at most 2^24 shares.)
+    constexpr uint32_t kMost = 1u << 26;
+    uint32_t base[4] = {0, 0, 0, 0};
     for (int b0 = 0; b0 < B; b0 += kCutBlock) {
         const int b = b0 + tid;
         uint32_t v[4] = {0, 0, 0, 0};
@@ -328,17 +329,18 @@ __global__ __launch_bounds__(kCutBlock) void chunk_cut_kernel(ChunkArgs a)
         }
         __syncthreads();
         for (int k = 0; k < 4; ++k) {
-            v[k] = wave_inclusive_scan(v[k]);
+            v[k] = min(wave_inclusive_scan(v[k]), kMost);
             if (lane == kWave - 1) s_sum[k][w] = v[k];
         }
         __syncthreads();
         for (int k = 0; k < 4; ++k) {
-            uint64_t before = base[k];
+            uint32_t before = base[k];
             for (int i = 0; i < kCutWaves; ++i) {
                 before += i < w ? s_sum[k][i] : 0;
                 base[k] += s_sum[k][i];
             }
-            if (b < B) lists[k * (B + 1) + b + 1] = (int32_t)min(before + v[k], kMost);
+            base[k] = min(base[k], kCutWaves * kMost);
+            if (b < B) lists[k * (B + 1) + b + 1] = (int32_t)min(before + v[k], kCutWaves * kMost);
         }
     }
 }
