@@ -799,11 +799,11 @@ int hgca_kv_write(const hgca_shape *shape, const hgca_kv_view *tier, int64_t n_s
  * it sees is in its O, infinities of both signs or a NaN make NaN.  fp32 O is accurate to
  * fp32.  For bf16 O of bf16 inputs the weights enter the second product with 16 bits (2e-6
  * of O, below its one rounding of 2^-9), or, with HGCA_CHUNK_ONE_PART_P, rounded once to bf16 (2^-9 of a
- * weight, at random: as much again as O's own rounding; the sum that divides them is not rounded), which takes a sixth
- * less time for prompts and as long for single tokens.  (The flag is ignored for fp32 O and fp32 inputs.)
+ * weight, at random: as much again as O's own rounding; the sum that divides them is not rounded), which takes a sixth to a
+ * quarter less time for prompts and as long for single tokens.  (The flag is ignored for fp32 O and fp32 inputs.)
  * Other bits of flags are rejected.
  * sm_scale must be positive and finite (1e-30 at least with slopes), scaled scores at most 2^126 in magnitude, softcap
- * finite; tier->cap is at most 2^30.  Results do not depend on other calls and repeat bit for
+ * any finite number whose quotient sm_scale / softcap is neither 0 nor beyond 2e38 in fp32; tier->cap is at most 2^30.  Results do not depend on other calls and repeat bit for
  * bit; where a sequence is cut into shares does depend on the batch, n_tokens and tier->cap.
  * ws needs
  * hgca_chunk_workspace_bytes(shape, n_tokens, tier->cap), which also serves fewer tokens and

@@ -6,8 +6,8 @@
 // scores is token 8 (r / 4) + 4 hw + r % 4, the two tokens of an instruction.
 //
 // What bounds it: the matrix cores, 64 cycles of a SIMD for 32 x 32 x 2.  A prompt of 4096 tokens, 32 / 8 heads, 137 GFLOP, 1220 us, 113 TFLOP/s of the 154
-// that a large product reaches; four prompts, 758 tokens over 2048, 219 us, of which the fold is 15: matrix units are busy 58 % of the time that
-// the compute units are, shares of five steps having a start and an end of their own.  (Operands read two pairs of pieces ahead: level, the
+// that a large product reaches; four prompts, 758 tokens over 2048, 197 to 219 us, of which the fold is 15: matrix units are busy 69 % of the time that
+// the compute units have work, which they have 81 % of the time, shares of five steps having a start and an end of their own.  (Operands read two pairs of pieces ahead: level, the
 // other workgroup's waves fill the gaps.)
 #include <algorithm>
 

@@ -9,7 +9,7 @@
 // What bounds it: memory.  One token of 8 sequences over 28 672, 32 / 8 heads of 128, bf16: 940 MB in 163 us, 5.8 TB/s, and 5 for the fold (through
 // LDS 174; heads of 64 89 : 102; a mixed step, whose single tokens it is, 441 : 488).  Units of 9 to 16 rows are
 // level (171 : 167).  17 to 32 rows in bf16 lose (169 -> 177), in fp32 they gain, as a unit through LDS does the arithmetic of 128 rows (8 tokens x
-// 8 over 14 K, groups of 4: 377 -> 196).
+// 8 over 14 K, groups of 4: 377 -> 196).  (bf16 figures with weights of one part; with two the units of up to 16 rows take 164 and 174 us.)
 #pragma once
 
 #include "chunk_device.hpp"

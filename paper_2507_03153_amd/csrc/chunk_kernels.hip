@@ -10,13 +10,14 @@
 // out of the first product are the operand of the second.
 // A wave tells by its rows' ranges which steps all of them see (no mask), and which none (left out).
 //
-// What bounds it: matrix and vector instructions (a weight is an exponential, five others and half a conversion for 512 products), and power, at
-// 2.0 GHz of 2.4 on long prompts: two of 4096 tokens, 64 / 8 heads, 562 GFLOP, 645 to 680 us, 830 to 870 TFLOP/s, matrix units busy 37 % of the
-// cycles at 2.4, vector units 48 %.  Capped scores cost seven instructions each (four prompts of 864 tokens seeing 4096: 306 us, 392 capped).  32 rows
+// What bounds it: matrix and vector instructions (a weight is an exponential, nine others and a conversion for 768 products), and power, at
+// 2.0 GHz of 2.4 on long prompts: two of 4096 tokens, 64 / 8 heads, 562 GFLOP, 795 to 825 us, 680 to 710 TFLOP/s, matrix units busy 48 % of the
+// cycles, vector units 54 %.  Capped scores cost eight instructions each (four prompts of 864 tokens over 4096: 329 us, 411 capped; heads of 128 then need all
+// 256 registers, and three to eight values wait in scratch memory, outside of the loops).  32 rows
 // per wave: with 64 the compiler has no registers left (640 -> 995 us); four waves per workgroup, two workgroups per compute unit: eight waves and
 // 256 rows read K and V half as often (661 : 679).  (These with weights of one part.)  Weights enter the second product as two bf16 parts for bf16 O, 16 bits, far
-// below its rounding, as three for fp32 O.  One part, 2^-9 of a weight and with it as much error again as the rounding of O, is there for callers that ask for it: prompts
-// 825 -> 670 us, mixed step 515 -> 424, documents 515 -> 438; single tokens, whose bound is memory, 169 : 169.
+// below its rounding, as three for fp32 O (the same prompts 953 us).  One part, 2^-9 of a weight and with it as much error again as the rounding of O, is there for
+// callers that ask for it: prompts 795 -> 655 us (38 % and 49 % busy), mixed step 502 -> 408, documents 495 -> 417; single tokens, whose bound is memory, 169 : 169.
 #include <algorithm>
 
 #include "chunk_few.hpp"

@@ -393,7 +393,7 @@ PlanArgs plan_args(const hgca_block_state *t)
 
 // Shares of a chunk call (chunk_device.hpp): about this many workgroups, two per compute unit; fp32, whose matrix instructions are what takes the time, evens
 // out better in twice as many (four prompts of 758 tokens over 2048: 268 -> 250 us; bf16, one token x 8 over 28 K: 512 : 768 : 1024
-// workgroups 168 : 178 : 171).
+// workgroups 168 : 178 : 171; bf16 figures here and below are with weights of one part).
 #ifndef HGCA_TARGET_WGS_CHUNK
 #define HGCA_TARGET_WGS_CHUNK 512
 #endif
