@@ -73,3 +73,29 @@ def test_one_part_is_for_bf16_outputs_of_bf16(gpu, dtype, out):  # noqa: F811
     run, _, _ = case(gpu, 128, 8, 2, 16, [40, 1], [300, 100], dict(cap=30.0), dtype)
     for x, y in zip(run(out, one_part_p=True), run(out)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("one_part", [False, True])
+@pytest.mark.parametrize("d,counts,lens", [(128, [150, 3], [400, 300]), (64, [90, 40], [90, 2000]), (128, [1, 2], [6000, 77])])
+def test_infinities_and_nan_of_v(gpu, d, counts, lens, one_part):  # noqa: F811
+    """A further part of a weight may be negative or 0: an infinity or NaN of V is in the columns of the rows that see it, and nowhere else."""
+    torch, hgca = gpu
+    rng, q, K, V = inputs(d + lens[0], "bf16", counts, 4, 2, d, max(lens))
+    clean = V.copy()
+    odd = [(b, h, int(rng.integers(n)), int(rng.integers(d)), x) for b, n in enumerate(lens) for h in range(2) for x in (np.inf, -np.inf, np.nan)]
+    for b, h, t, c, x in odd:
+        V[b, h, t, c], clean[b, h, t, c] = x, 0
+    cu, scale = np.concatenate([[0], np.cumsum(counts)]), float(np.float32(d ** -0.5))
+    shape = hgca.Shape(hgca.BF16, 2, 4, 2, d, scale)
+    tier = tier_of(gpu, rng, "bf16", K, V, lens, 16)
+    o, _ = call(gpu, shape, put(torch, q, "bf16"), cu, tier, "bf16", window=200, one_part_p=one_part)
+    O, _ = so.chunk(q, cu, K, clean, lens, scale, window=200)
+    kinds = np.zeros(O.shape, int)
+    for b, h, t, c, _ in odd:
+        rows, x = slice(cu[b], cu[b + 1]), V[b, h, t, c]
+        seen = so.sees(counts[b], lens[b], True, 200)[:, t]
+        kinds[rows, 2 * h:2 * h + 2, c] |= np.where(seen, 1 if x == np.inf else 2 if x == -np.inf else 4, 0)[:, None]
+    got = o.double().cpu().numpy()
+    assert np.array_equal(got == np.inf, kinds == 1) and np.array_equal(got == -np.inf, kinds == 2) and np.array_equal(np.isnan(got), kinds > 2)
+    err = np.abs(np.where(kinds > 0, 0, got) - np.where(kinds > 0, 0, O))
+    assert (err <= 2.0 ** -8 * np.abs(O) + ((2.0 ** -9 if one_part else 0) + 2e-4) * np.abs(clean).max()).all()
